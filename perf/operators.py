@@ -132,7 +132,7 @@ def prepare(case, seed):
             s["m"], s["v"] = m, r * r
         else:
             s["m"], s["m_scale"] = _to8(m)
-            s["v"], s["v_scale"] = _to8(r)
+            s["v"], s["v_scale"] = _to8(r, E4M3_TINY)  # a second moment that is not zero is not stored as zero
         if case["master"]:
             s["w"] = s["p"].float() + 1e-4 * normal(n) * s["p"].float().abs()
             s["p"] = s["w"].to(io)
@@ -165,14 +165,14 @@ def prepare(case, seed):
     return s
 
 
-def _to8(x):
-    """Blocks of 256 values as float8 e4m3 and their scales; a positive value never becomes zero beside its block."""
+def _to8(x, floor=0.0):
+    """Blocks of 256 values as float8 e4m3 and their scales; a positive value is stored as no less than `floor`."""
     x = x.view(-1, BLOCK)
     top = x.abs().amax(1)
     scale = top / E4M3_MAX
     inverse = torch.where(top > 0, E4M3_MAX / top, torch.zeros_like(top)).clamp(max=torch.finfo(torch.float32).max)
     y = x * inverse[:, None]
-    y = torch.where((x > 0) & (y < E4M3_TINY), torch.full_like(y, E4M3_TINY), y)
+    y = torch.where((x > 0) & (y < floor), torch.full_like(y, floor), y)
     return y.to(torch.float8_e4m3fn).view(-1), scale
 
 
@@ -309,8 +309,8 @@ def _plain_adamw(state):
         state["m"].copy_(m)
         state["v"].copy_(v)
     else:
-        for name, x in (("m", m), ("v", root)):
-            values, scale = _to8(x)
+        for name, x, floor in (("m", m, 0.0), ("v", root, E4M3_TINY)):
+            values, scale = _to8(x, floor)
             state[name].copy_(values)
             state[name + "_scale"].copy_(scale)
     state["p"].copy_(w)
@@ -376,11 +376,11 @@ def _exact_adamw(state):
         if case["bits"] == 32:
             out["m"][b:b + n], out["v"][b:b + n] = m, v
             continue
-        for name, x in (("m", m), ("v", v.sqrt())):
+        for name, x, floor in (("m", m, 0.0), ("v", v.sqrt(), E4M3_TINY)):
             blocks = -(-n // BLOCK)
             top = torch.zeros(blocks, dtype=torch.float64, device="cuda").scatter_reduce(0, where, x.abs(), "amax")
             code = x / (top / E4M3_MAX).clamp(min=1e-300)[where]
-            code = torch.where(x > 0, code.clamp(min=E4M3_TINY), code)
+            code = torch.where(x > 0, code.clamp(min=floor), code)
             out[name][b:b + n] = code.float().to(torch.float8_e4m3fn).double()
             out[name + "_scale"][b // BLOCK:b // BLOCK + blocks] = top / E4M3_MAX
     return out
