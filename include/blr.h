@@ -350,6 +350,138 @@ BLR_API blr_status blr_scan_fwd_noalloc(const blr_desc* desc, const void* x, con
 BLR_API blr_status blr_selftest_wait_timeout(const blr_desc* desc, void* ws, size_t ws_bytes,
                                      uint64_t timeout_ns, blr_stream_t stream);
 
+/*
+ * The gated delta rule: the matrix-state relative of the recurrence above. A
+ * value head keeps a state S (Dk x Dv) and per step
+ *     S~  = exp(g_t) S_{t-1}
+ *     u_t = beta_t (v_t - S~^T k_t)
+ *     S_t = S~ + k_t u_t^T
+ *     o_t = scale S_t^T q_t
+ * (the decay forgets, the delta rule replaces what the state holds under k_t).
+ *
+ * Conventions of the blr_gdr entry points
+ * ---------------------------------------
+ * Layout   q, k (B, L, Hk, Dk); v, o (B, L, Hv, Dv); g, beta (B, L, Hv); states
+ *          (B, Hv, Dk, Dv). Value head h reads key head h / (Hv / Hk). q, k and v
+ *          may be slices of wider rows: ldq, ldk, ldv are the elements between
+ *          consecutive steps (0: contiguous; rows of the batch are L steps
+ *          apart). Everything else is contiguous.
+ * Dtypes   q, k, v, g, beta, o and their gradients use `io`; states and their
+ *          gradients are float32.
+ * Domain   finite inputs; g <= 0 (the log of the decay; values below -120 act
+ *          as -120, a decay of zero in float32).
+ * Sizes    Dk 64 or 128; Dv 64, 128, 192 or 256; Hv a multiple of Hk.
+ * Lengths  NULL, or (B) int32 on the device: row b is its last lengths[b] steps
+ *          (values outside [0, L] are clamped). The padding before them is never
+ *          read; o and the gradients are zero there. s_last of an empty row is
+ *          its s0.
+ * Precision  Sums, decays and states are float32. With io == BLR_F32, or with
+ *          BLR_GDR_STATE (a float32 state goes in or out), or with fewer than 16
+ *          steps, every operand of a matrix product is carried as two bfloat16 terms (16 significant
+ *          bits). Without, products round their operands to bfloat16, as the
+ *          bfloat16 inputs are.
+ * Checks, streams, errors: as above; q, k, v, o, states and gradients 16-byte
+ *          aligned (ldq, ldk, ldv multiples of 8), the others to their element.
+ */
+typedef struct {
+  int64_t B, L;          /* rows, steps */
+  int64_t Hk, Hv;        /* key heads, value heads */
+  int64_t Dk, Dv;        /* channels of a key head, of a value head */
+  int64_t ldq, ldk, ldv; /* elements between steps of q, k, v; 0: contiguous */
+  blr_dtype io;
+  float scale;
+} blr_gdr_desc;
+
+#define BLR_GDR_TRAIN 1 /* the forward keeps what blr_gdr_bwd needs */
+#define BLR_GDR_STATE 2 /* s0, s_last, ds_last or ds0 may be given */
+
+/* Workspace bytes of blr_gdr_fwd / blr_gdr_bwd; 0 when invalid or empty. */
+BLR_API size_t blr_gdr_workspace_bytes(const blr_gdr_desc* desc, int flags);
+
+/*
+ * Forward over whole sequences, in chunks of 64 steps.
+ * flags    BLR_GDR_TRAIN | BLR_GDR_STATE; without BLR_GDR_STATE s0 and s_last
+ *          must be NULL
+ * s0       (B, Hv, Dk, Dv) or NULL (zero)
+ * o        (B, L, Hv, Dv) output
+ * s_last   (B, Hv, Dk, Dv) output or NULL
+ * ws       16-byte aligned, blr_gdr_workspace_bytes(desc, flags) bytes; previous
+ *          contents are ignored. With BLR_GDR_TRAIN it then holds what
+ *          blr_gdr_bwd consumes.
+ */
+BLR_API blr_status blr_gdr_fwd(const blr_gdr_desc* desc, int flags, const int32_t* lengths,
+                               const void* q, const void* k, const void* v, const void* g,
+                               const void* beta, const float* s0, void* o, float* s_last, void* ws,
+                               size_t ws_bytes, blr_stream_t stream);
+
+/*
+ * Backward of blr_gdr_fwd for the loss sum d_o o + sum ds_last s_last.
+ * flags, lengths, q .. s0: exactly the forward's (flags with BLR_GDR_TRAIN)
+ * d_o      (B, L, Hv, Dv); not read on the padding
+ * ds_last  (B, Hv, Dk, Dv) or NULL (zero)
+ * dq, dk   (B, L, Hk, Dk), summed over the value heads that share a key head
+ * dv       (B, L, Hv, Dv)
+ * dg, dbeta (B, L, Hv)
+ * ds0      (B, Hv, Dk, Dv) or NULL. dq .. dbeta are contiguous.
+ * ws       the workspace the forward filled; it may be used for another
+ *          backward of the same forward.
+ */
+BLR_API blr_status blr_gdr_bwd(const blr_gdr_desc* desc, int flags, const int32_t* lengths,
+                               const void* d_o, const float* ds_last, const void* q, const void* k,
+                               const void* v, const void* g, const void* beta, const float* s0,
+                               void* dq, void* dk, void* dv, void* dg, void* dbeta, float* ds0,
+                               void* ws, size_t ws_bytes, blr_stream_t stream);
+
+/*
+ * desc->L recurrent steps on the states of desc->B rows (serving), in float32
+ * arithmetic step by step. Needs no workspace.
+ * state    dtype of s_prev and s_out: BLR_F32, or BLR_BF16 to halve the states'
+ *          memory (rounded to nearest-even once, after the last step)
+ * s_prev   (B, Hv, Dk, Dv) or NULL (zero)
+ * s_out    (B, Hv, Dk, Dv); may be s_prev
+ * o        (B, L, Hv, Dv) or NULL
+ * L == 0 copies s_prev to s_out.
+ */
+BLR_API blr_status blr_gdr_steps(const blr_gdr_desc* desc, blr_dtype state, const void* s_prev,
+                                 const void* q, const void* k, const void* v, const void* g,
+                                 const void* beta, void* s_out, void* o, blr_stream_t stream);
+
+/*
+ * One AdamW step over many tensors (few launches for all of them). Per value, in float32:
+ *     m = beta1 m + (1 - beta1) g,   r2 = beta2 r2 + (1 - beta2) g^2
+ *     w = w (1 - lr weight_decay) - lr / (1 - beta1^step) m / (sqrt(r2) / sqrt(1 - beta2^step) + eps)
+ * with g the gradient times *grad_scale.
+ * tensors      HOST array of `count` records; their pointers are device pointers
+ *   p, g       n values in `io`: parameter (updated) and gradient
+ *   m, v       bits == 32: float32 first and second moments (updated).
+ *              bits == 8: float8 e4m3 codes of m and of the second moment's ROOT,
+ *              each block of 256 values over a float32 scale (its largest
+ *              magnitude / 448); a root that is not zero is stored as no less
+ *              than the smallest code, so that no step divides by eps alone.
+ *   w          io == BLR_BF16: float32 master weights (updated; p becomes their
+ *              rounding), in all records or in none (NULL: w is p itself)
+ *   m_scale, v_scale  ceil(n / 256) scales (updated); bits == 8 only
+ * step         1 for the first step
+ * grad_scale   float32 on the device, or NULL (1): a clipping or unscaling factor
+ * Pointers are aligned to their element. Tensors whose pointers are 32-byte
+ * aligned (16 for 2-byte, 8 for 1-byte values) move in wide loads.
+ */
+typedef struct {
+  void* p;
+  const void* g;
+  void* m;
+  void* v;
+  float* w;
+  float* m_scale;
+  float* v_scale;
+  int64_t n;
+} blr_adamw_tensor;
+
+BLR_API blr_status blr_adamw_step(int64_t count, const blr_adamw_tensor* tensors, blr_dtype io,
+                                  int bits, double lr, double beta1, double beta2, double eps,
+                                  double weight_decay, int64_t step, const float* grad_scale,
+                                  blr_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

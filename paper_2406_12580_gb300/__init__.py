@@ -21,13 +21,25 @@ The gated recurrent layer's merge y = h SiLU(z) (Alg. 1) fused into the scan:
                        dlam, dh0, ws)
 
 ``BDLRUScan`` wraps the forward and backward in a torch.autograd.Function.
+
+The gated delta rule, the matrix-state relative of the recurrence (``delta.py``
+has its autograd operator and a layer), and the AdamW step of a whole model
+(``optim.py`` has the optimizer):
+
+    desc = GDRDesc(B, L, Hk, Hv, Dk, Dv, io=BLR_BF16, scale=Dk ** -0.5)
+    blr_gdr_fwd(desc, BLR_GDR_TRAIN, lengths, q, k, v, g, beta, None, o, None, ws)
+    blr_gdr_bwd(desc, BLR_GDR_TRAIN, lengths, do, None, q, k, v, g, beta, None, dq, dk, dv, dg, dbeta,
+                None, ws)
+    blr_gdr_steps(desc, BLR_F32, s_prev, q, k, v, g, beta, s_out, o)
+    blr_adamw_step(params, grads, m, v, lr=1e-3, step=1)
 """
 from __future__ import annotations
 
 import ctypes
 
 from ._lib import (BLR_BF16, BLR_ERR_CUDA, BLR_ERR_INVALID_ARG, BLR_ERR_TIMEOUT,  # noqa: F401
-                   BLR_ERR_UNSUPPORTED, BLR_ERR_WORKSPACE, BLR_F32, BLR_OK, blr_desc, load)
+                   BLR_ERR_UNSUPPORTED, BLR_ERR_WORKSPACE, BLR_F32, BLR_OK, blr_desc, blr_gdr_desc,
+                   load)
 
 __all__ = [
     "BLR_F32", "BLR_BF16", "Desc", "BLRError", "blr_workspace_bytes", "blr_scan_fwd",
@@ -36,6 +48,8 @@ __all__ = [
     "blr_steps", "blr_scan_fwd_varlen", "blr_scan_bwd_varlen", "blr_scan_family",
     "FAMILY_NONE", "FAMILY_TILED", "FAMILY_SERIAL", "FAMILY_SEGMENTED",
     "BDLRUScan", "library_loaded",
+    "GDRDesc", "BLR_GDR_TRAIN", "BLR_GDR_STATE", "blr_gdr_workspace_bytes", "blr_gdr_fwd",
+    "blr_gdr_bwd", "blr_gdr_steps", "blr_adamw_step",
 ]
 
 
@@ -215,6 +229,109 @@ def blr_scan_fwd_noalloc(desc, x, gate_logits, lam, h0, h, h_last, stream=None):
 
 def blr_status_string(status: int) -> str:
     return load().blr_status_string(status).decode()
+
+
+# flags of the blr_gdr entry points
+BLR_GDR_TRAIN, BLR_GDR_STATE = 1, 2
+
+
+def GDRDesc(B: int, L: int, Hk: int, Hv: int, Dk: int, Dv: int, ldq: int = 0, ldk: int = 0, ldv: int = 0,
+            io: int = BLR_F32, scale: float = 1.0) -> blr_gdr_desc:
+    return blr_gdr_desc(B, L, Hk, Hv, Dk, Dv, ldq, ldk, ldv, io, scale)
+
+
+def _row_ptr(t, name: str):
+    """_ptr of a tensor that may be a slice of wider rows (its strides are the descriptor's)."""
+    if t is None or isinstance(t, int):
+        return t
+    import torch
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: expected a CUDA tensor, an int pointer or None")
+    if t.numel() == 0:
+        return None
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name}: tensor must be on the current CUDA device")
+    if t.stride(-1) != 1:
+        raise ValueError(f"{name}: the last dimension must be contiguous")
+    return t.data_ptr()
+
+
+def _ws_bytes(ws) -> int:
+    return ws.numel() * ws.element_size() if ws is not None else 0
+
+
+def blr_gdr_workspace_bytes(desc: blr_gdr_desc, flags: int) -> int:
+    return int(load().blr_gdr_workspace_bytes(ctypes.byref(desc), flags))
+
+
+def blr_gdr_fwd(desc, flags, lengths, q, k, v, g, beta, s0, o, s_last, ws, stream=None):
+    """Gated delta rule over whole sequences (see include/blr.h)."""
+    _check(load().blr_gdr_fwd(ctypes.byref(desc), flags, _ptr(lengths, "lengths"), _row_ptr(q, "q"),
+                              _row_ptr(k, "k"), _row_ptr(v, "v"), _ptr(g, "g"), _ptr(beta, "beta"),
+                              _ptr(s0, "s0"), _ptr(o, "o"), _ptr(s_last, "s_last"), _ptr(ws, "ws"),
+                              _ws_bytes(ws), _stream(stream)),
+           "blr_gdr_fwd")
+
+
+def blr_gdr_bwd(desc, flags, lengths, d_o, ds_last, q, k, v, g, beta, s0, dq, dk, dv, dg, dbeta, ds0, ws,
+                stream=None):
+    _check(load().blr_gdr_bwd(ctypes.byref(desc), flags, _ptr(lengths, "lengths"), _ptr(d_o, "d_o"),
+                              _ptr(ds_last, "ds_last"), _row_ptr(q, "q"), _row_ptr(k, "k"),
+                              _row_ptr(v, "v"), _ptr(g, "g"), _ptr(beta, "beta"), _ptr(s0, "s0"),
+                              _ptr(dq, "dq"), _ptr(dk, "dk"), _ptr(dv, "dv"), _ptr(dg, "dg"),
+                              _ptr(dbeta, "dbeta"), _ptr(ds0, "ds0"), _ptr(ws, "ws"), _ws_bytes(ws),
+                              _stream(stream)),
+           "blr_gdr_bwd")
+
+
+def blr_gdr_steps(desc, state, s_prev, q, k, v, g, beta, s_out, o=None, stream=None):
+    """desc.L recurrent steps per row (state dtype `state`, BLR_F32 or BLR_BF16); s_out may be s_prev."""
+    _check(load().blr_gdr_steps(ctypes.byref(desc), state, _ptr(s_prev, "s_prev"), _row_ptr(q, "q"),
+                                _row_ptr(k, "k"), _row_ptr(v, "v"), _ptr(g, "g"), _ptr(beta, "beta"),
+                                _ptr(s_out, "s_out"), _ptr(o, "o"), _stream(stream)),
+           "blr_gdr_steps")
+
+
+def blr_adamw_step(params, grads, m, v, *, lr: float, step: int, beta1: float = 0.9, beta2: float = 0.999,
+                   eps: float = 1e-8, weight_decay: float = 0.0, masters=None, m_scales=None, v_scales=None,
+                   grad_scale=None, stream=None):
+    """One AdamW step, in place, over lists of contiguous tensors (see include/blr.h).
+
+    params and grads float32 or bfloat16; m and v float32, or float8_e4m3fn (v then holds the second
+    moment's root) with float32 m_scales and v_scales of ceil(n / 256) values each; masters: float32
+    weights beside bfloat16 params; grad_scale: a float32 tensor of one value, or None."""
+    import numpy as np
+    import torch
+    n = len(params)
+    lists = {"params": params, "grads": grads, "m": m, "v": v, "masters": masters, "m_scales": m_scales,
+             "v_scales": v_scales}
+    if n == 0:
+        return
+    io = _dtype_code(params[0])
+    eight = m[0].dtype == torch.float8_e4m3fn
+    if eight != (m_scales is not None) or eight != (v_scales is not None):
+        raise ValueError("m_scales and v_scales go with float8_e4m3fn moments")
+    dtypes = {"params": params[0].dtype, "grads": params[0].dtype, "m": m[0].dtype, "v": m[0].dtype}
+    if dtypes["m"] not in (torch.float32, torch.float8_e4m3fn):
+        raise TypeError("moments are float32 or float8_e4m3fn")
+    device = params[0].device
+    if device.type != "cuda" or device.index != torch.cuda.current_device():
+        raise ValueError("tensors must be on the current CUDA device")
+    table = np.zeros((n, 8), dtype=np.int64)
+    sizes = [t.numel() for t in params]
+    blocks = [-(-x // 256) for x in sizes] if eight else None
+    for column, (name, ts) in enumerate(lists.items()):
+        if ts is None:
+            continue
+        dtype, want = dtypes.get(name, torch.float32), blocks if "scales" in name else sizes
+        if (len(ts) != n or any(t.dtype != dtype or t.device != device for t in ts)
+                or not all([t.is_contiguous() for t in ts]) or [t.numel() for t in ts] != want):
+            raise ValueError(f"{name}: {n} contiguous {dtype} tensors of the parameters' sizes on {device} are wanted")
+        table[:, column] = [t.data_ptr() for t in ts]
+    table[:, 7] = sizes
+    _check(load().blr_adamw_step(n, table.ctypes.data, io, 8 if eight else 32, lr, beta1, beta2, eps,
+                                 weight_decay, step, _ptr(grad_scale, "grad_scale"), _stream(stream)),
+           "blr_adamw_step")
 
 
 def _autograd():

@@ -27,10 +27,17 @@ class blr_desc(ctypes.Structure):
                 ("io", ctypes.c_int), ("c", ctypes.c_float)]
 
 
+class blr_gdr_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("B", "L", "Hk", "Hv", "Dk", "Dv", "ldq", "ldk", "ldv")] + [
+        ("io", ctypes.c_int), ("scale", ctypes.c_float)]
+
+
 _VP = ctypes.c_void_p
 _SZ = ctypes.c_size_t
 _ST = ctypes.c_int
 _DESC_P = ctypes.POINTER(blr_desc)
+_GDR_P = ctypes.POINTER(blr_gdr_desc)
+_F64 = ctypes.c_double
 
 # name -> (restype, argtypes); the argument order of include/blr.h
 SIGNATURES = {
@@ -53,6 +60,12 @@ SIGNATURES = {
     "blr_scan_fwd_gated": (_ST, [_DESC_P, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _SZ, _VP]),
     "blr_scan_bwd_gated": (_ST, [_DESC_P, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP,
                                  _VP, _VP, _SZ, _VP]),
+    "blr_gdr_workspace_bytes": (_SZ, [_GDR_P, ctypes.c_int]),
+    "blr_gdr_fwd": (_ST, [_GDR_P, ctypes.c_int] + [_VP] * 10 + [_SZ, _VP]),
+    "blr_gdr_bwd": (_ST, [_GDR_P, ctypes.c_int] + [_VP] * 16 + [_SZ, _VP]),
+    "blr_gdr_steps": (_ST, [_GDR_P, ctypes.c_int] + [_VP] * 9),
+    "blr_adamw_step": (_ST, [ctypes.c_int64, _VP, ctypes.c_int, ctypes.c_int, _F64, _F64, _F64, _F64,
+                             _F64, ctypes.c_int64, _VP, _VP]),
 }
 
 _lock = threading.Lock()

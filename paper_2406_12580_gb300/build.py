@@ -4,6 +4,7 @@
 """
 from __future__ import annotations
 
+import concurrent.futures
 import os
 import shutil
 import subprocess
@@ -15,7 +16,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIBRARY = os.path.join(PKG, "libblr.so")
-SOURCES = [os.path.join(CSRC, "blr_api.cu")]
+SOURCES = sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".cu"))
 DEPENDS = SOURCES + [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".cuh", ".h"))] + [
     os.path.join(INCLUDE, "blr.h")]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
@@ -30,7 +31,7 @@ def nvcc_path() -> str:
 
 def nvcc_flags(verbose: bool = False) -> list:
     cuda_lib = os.path.join(os.path.dirname(os.path.dirname(nvcc_path())), "lib64")
-    flags = [*ARCH, "-O3", "-lineinfo", "-std=c++17", "-shared", "-Xcompiler", "-fPIC",
+    flags = [*ARCH, "-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC",
              "-Xcompiler", "-fvisibility=hidden", "-cudart", "shared", "-I", INCLUDE, "-I", CSRC,
              "-Xlinker", f"-rpath,{cuda_lib}"]
     if verbose:
@@ -49,19 +50,27 @@ def build(verbose: bool = False, force: bool = True) -> str:
     """Compile the library (atomically replacing any previous build)."""
     if not force and not stale():
         return LIBRARY
-    fd, tmp = tempfile.mkstemp(suffix=".so", dir=PKG)
-    os.close(fd)
+    tmp = tempfile.mkdtemp(dir=PKG)
     try:
-        cmd = [nvcc_path(), *nvcc_flags(verbose), *SOURCES, "-o", tmp]
-        res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
-        if res.returncode != 0:
-            raise RuntimeError("nvcc failed:\n" + res.stdout)
+        flags = nvcc_flags(verbose)
+
+        def run(args: list) -> str:
+            res = subprocess.run([nvcc_path(), *flags, *args], stdout=subprocess.PIPE,
+                                 stderr=subprocess.STDOUT, text=True)
+            if res.returncode != 0:
+                raise RuntimeError("nvcc failed:\n" + res.stdout)
+            return res.stdout
+
+        objects = [os.path.join(tmp, os.path.basename(f)[:-3] + ".o") for f in SOURCES]
+        with concurrent.futures.ThreadPoolExecutor() as pool:  # one nvcc per source file
+            texts = list(pool.map(lambda fo: run(["-c", fo[0], "-o", fo[1]]), zip(SOURCES, objects)))
+        linked = os.path.join(tmp, "libblr.so")
+        texts.append(run(["-shared", *objects, "-o", linked]))
         if verbose:
-            sys.stdout.write(res.stdout)
-        os.replace(tmp, LIBRARY)
+            sys.stdout.write("".join(texts))
+        os.replace(linked, LIBRARY)
     finally:
-        if os.path.exists(tmp):
-            os.unlink(tmp)
+        shutil.rmtree(tmp, ignore_errors=True)
     return LIBRARY
 
 

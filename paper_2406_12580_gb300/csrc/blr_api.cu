@@ -14,12 +14,11 @@
 #include "blr.h"
 #include "blr_chain.cuh"
 #include "blr_chain_bwd.cuh"
+#include "blr_host.h"
 #include "blr_merge.cuh"
 #include "blr_seq.cuh"
 
-namespace {
-
-using blr::Plan;
+namespace blr {
 
 thread_local char g_last_error[512] = "";
 
@@ -36,7 +35,16 @@ blr_status cuda_check(cudaError_t e, const char* what) {
   return fail(BLR_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
 }
 
-bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
+}  // namespace blr
+
+namespace {
+
+using blr::cuda_check;
+using blr::fail;
+using blr::g_last_error;
+using blr::need;
+using blr::optional;
+using blr::Plan;
 
 // Shared checks of the problem description; fills `plan` when B, L, D > 0.
 blr_status check_desc(const blr_desc* d, Plan* plan, bool* empty_bd) {
@@ -68,24 +76,6 @@ blr_status check_desc(const blr_desc* d, Plan* plan, bool* empty_bd) {
     return fail(BLR_ERR_UNSUPPORTED, "too many chains (%lld)", (long long)plan->n_chain);
   return BLR_OK;
 }
-
-blr_status need(const void* p, const char* name, size_t align) {
-  if (p == nullptr) return fail(BLR_ERR_INVALID_ARG, "%s is NULL", name);
-  if (!aligned(p, align)) return fail(BLR_ERR_INVALID_ARG, "%s is not %zu-byte aligned", name, align);
-  return BLR_OK;
-}
-
-blr_status optional(const void* p, const char* name, size_t align) {
-  if (p != nullptr && !aligned(p, align))
-    return fail(BLR_ERR_INVALID_ARG, "%s is not %zu-byte aligned", name, align);
-  return BLR_OK;
-}
-
-#define BLR_TRY(expr)                  \
-  do {                                 \
-    blr_status s_ = (expr);            \
-    if (s_ != BLR_OK) return s_;       \
-  } while (0)
 
 blr_status check_ws(const Plan& plan, const void* ws, size_t ws_bytes) {
   BLR_TRY(need(ws, "ws", 16));

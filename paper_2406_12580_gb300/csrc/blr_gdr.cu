@@ -1,0 +1,165 @@
+// Host side of blr_gdr_fwd and blr_gdr_bwd (declared in blr.h): checks, the workspace's layout, launches.
+#include "blr_gdr.h"
+#include "blr_gdr_launch.h"
+
+namespace {
+
+using blr::fail;
+using blr::GdrSizes;
+using blr::gdr::Problem;
+
+constexpr int64_t kC = 64;
+// Under this many steps a gradient is a sum of so few products that the rounding of a single score
+// shows in the whole row (one step: 5e-3 of dq, against 3e-3 from 64 steps on): operands take two planes.
+constexpr int64_t kFewSteps = 16;
+
+// The workspace: for every chunk of every value head, tiles of 64 rows in `np` planes.
+struct Layout {
+  int64_t n, nc;
+  int np;
+  size_t gates, W, U, S, T, dU, dS, pq, pk, bytes;
+};
+
+size_t up(size_t v) { return (v + 255) / 256 * 256; }
+
+blr_status make_layout(const blr_gdr_desc* d, int flags, const GdrSizes& s, Layout* l) {
+  if (flags & ~(BLR_GDR_TRAIN | BLR_GDR_STATE)) return fail(BLR_ERR_INVALID_ARG, "unknown flags %d", flags);
+  l->n = (s.L + kC - 1) / kC;
+  l->nc = s.B * s.Hv * l->n;
+  // One block a chunk; a state's columns and a tensor's offsets are counted in 64 bits.
+  if (l->nc >= 0x7fffffff || s.B * s.Hv * (s.Dv / 64) >= 0x7fffffff)
+    return fail(BLR_ERR_UNSUPPORTED, "too many chunks (%lld)", (long long)l->nc);
+  l->np = d->io == BLR_F32 || (flags & BLR_GDR_STATE) || s.L < kFewSteps ? 2 : 1;
+  const size_t tile = (size_t)l->nc * l->np * 64 * 2;  // bytes per column of a tile
+  const size_t dk = (size_t)s.Dk, dv = (size_t)s.Dv;
+  size_t o = 0;
+  const auto take = [&](size_t* at, size_t bytes) {
+    *at = o;
+    o = up(o + bytes);
+  };
+  take(&l->gates, (size_t)l->nc * blr::gdr::kGates * 4);
+  take(&l->W, tile * dk);
+  take(&l->U, tile * dv);
+  take(&l->S, tile / 64 * dv * dk);
+  l->T = l->dU = l->dS = l->pq = l->pk = 0;
+  if (flags & BLR_GDR_TRAIN) {
+    take(&l->T, tile * 64);
+    take(&l->dU, tile * dv);
+    take(&l->dS, tile / 64 * dv * dk);
+    if (s.Hv != s.Hk) {
+      take(&l->pq, (size_t)s.B * s.L * s.Hv * dk * 4);
+      take(&l->pk, (size_t)s.B * s.L * s.Hv * dk * 4);
+    }
+  }
+  l->bytes = o;
+  return BLR_OK;
+}
+
+Problem make_problem(const blr_gdr_desc* d, const GdrSizes& s, const Layout& l, const int32_t* lengths, void* ws) {
+  char* w = static_cast<char*>(ws);
+  Problem p;
+  p.B = s.B;
+  p.L = s.L;
+  p.n = l.n;
+  p.Hk = (int)s.Hk;
+  p.Hv = (int)s.Hv;
+  p.Dv = (int)s.Dv;
+  p.ldq = s.ldq;
+  p.ldk = s.ldk;
+  p.ldv = s.ldv;
+  p.scale = d->scale;
+  p.lengths = lengths;
+  p.gates = reinterpret_cast<float*>(w + l.gates);
+  p.W = w + l.W;
+  p.U = w + l.U;
+  p.S = w + l.S;
+  p.T = w + l.T;
+  p.dU = w + l.dU;
+  p.dS = w + l.dS;
+  p.pq = reinterpret_cast<float*>(w + l.pq);
+  p.pk = reinterpret_cast<float*>(w + l.pk);
+  return p;
+}
+
+blr_status check_inputs(const blr_gdr_desc* d, int flags, const int32_t* lengths, const void* q, const void* k,
+                        const void* v, const void* g, const void* beta, const float* s0, const void* ws,
+                        size_t ws_bytes, size_t wanted) {
+  const size_t e = d->io == BLR_F32 ? 4 : 2;
+  BLR_TRY(blr::optional(lengths, "lengths", 4));
+  BLR_TRY(blr::need(q, "q", 16));
+  BLR_TRY(blr::need(k, "k", 16));
+  BLR_TRY(blr::need(v, "v", 16));
+  BLR_TRY(blr::need(g, "g", e));
+  BLR_TRY(blr::need(beta, "beta", e));
+  BLR_TRY(blr::need(ws, "ws", 16));
+  if (ws_bytes < wanted) return fail(BLR_ERR_INVALID_ARG, "ws_bytes=%zu < required %zu", ws_bytes, wanted);
+  return BLR_OK;
+}
+
+blr_status check_states(int flags, const float* a, const char* an, const float* b, const char* bn) {
+  if (!(flags & BLR_GDR_STATE) && (a != nullptr || b != nullptr))
+    return fail(BLR_ERR_INVALID_ARG, "%s needs BLR_GDR_STATE", a != nullptr ? an : bn);
+  BLR_TRY(blr::optional(a, an, 16));
+  return blr::optional(b, bn, 16);
+}
+
+blr_status copy_state(const GdrSizes& s, const float* from, float* to, cudaStream_t stream) {
+  if (to == nullptr) return BLR_OK;
+  const size_t bytes = (size_t)s.B * s.Hv * s.Dk * s.Dv * 4;
+  if (from == nullptr) return blr::cuda_check(cudaMemsetAsync(to, 0, bytes, stream), "cudaMemsetAsync");
+  return blr::cuda_check(cudaMemcpyAsync(to, from, bytes, cudaMemcpyDeviceToDevice, stream), "cudaMemcpyAsync");
+}
+
+}  // namespace
+
+size_t blr_gdr_workspace_bytes(const blr_gdr_desc* desc, int flags) {
+  GdrSizes s;
+  Layout l;
+  if (blr::gdr_check(desc, &s) != BLR_OK || s.empty || s.L == 0) return 0;
+  return make_layout(desc, flags, s, &l) == BLR_OK ? l.bytes : 0;
+}
+
+blr_status blr_gdr_fwd(const blr_gdr_desc* desc, int flags, const int32_t* lengths, const void* q, const void* k,
+                       const void* v, const void* g, const void* beta, const float* s0, void* o, float* s_last,
+                       void* ws, size_t ws_bytes, blr_stream_t stream) {
+  GdrSizes s;
+  Layout l;
+  BLR_TRY(blr::gdr_check(desc, &s));
+  BLR_TRY(make_layout(desc, flags, s, &l));
+  BLR_TRY(check_states(flags, s0, "s0", s_last, "s_last"));
+  if (s.empty) return BLR_OK;
+  if (s.L == 0) return copy_state(s, s0, s_last, stream);
+  BLR_TRY(check_inputs(desc, flags, lengths, q, k, v, g, beta, s0, ws, ws_bytes, l.bytes));
+  BLR_TRY(blr::need(o, "o", 16));
+  const Problem p = make_problem(desc, s, l, lengths, ws);
+  const blr::gdr::FwdCall c{(int)s.Dk, (flags & BLR_GDR_TRAIN) != 0, q, k, v, g, beta, s0, o, s_last, stream};
+  if (desc->io == BLR_F32) return blr::gdr::fwd_f32(p, c);
+  return l.np == 2 ? blr::gdr::fwd_bf16_state(p, c) : blr::gdr::fwd_bf16(p, c);
+}
+
+blr_status blr_gdr_bwd(const blr_gdr_desc* desc, int flags, const int32_t* lengths, const void* d_o,
+                       const float* ds_last, const void* q, const void* k, const void* v, const void* g,
+                       const void* beta, const float* s0, void* dq, void* dk, void* dv, void* dg, void* dbeta,
+                       float* ds0, void* ws, size_t ws_bytes, blr_stream_t stream) {
+  GdrSizes s;
+  Layout l;
+  BLR_TRY(blr::gdr_check(desc, &s));
+  BLR_TRY(make_layout(desc, flags, s, &l));
+  if (!(flags & BLR_GDR_TRAIN)) return fail(BLR_ERR_INVALID_ARG, "the backward needs BLR_GDR_TRAIN");
+  BLR_TRY(check_states(flags, ds_last, "ds_last", ds0, "ds0"));
+  BLR_TRY(check_states(flags, s0, "s0", nullptr, ""));
+  if (s.empty) return BLR_OK;
+  if (s.L == 0) return copy_state(s, ds_last, ds0, stream);
+  BLR_TRY(check_inputs(desc, flags, lengths, q, k, v, g, beta, s0, ws, ws_bytes, l.bytes));
+  const size_t e = desc->io == BLR_F32 ? 4 : 2;
+  BLR_TRY(blr::need(d_o, "d_o", 16));
+  BLR_TRY(blr::need(dq, "dq", 16));
+  BLR_TRY(blr::need(dk, "dk", 16));
+  BLR_TRY(blr::need(dv, "dv", 16));
+  BLR_TRY(blr::need(dg, "dg", e));
+  BLR_TRY(blr::need(dbeta, "dbeta", e));
+  const Problem p = make_problem(desc, s, l, lengths, ws);
+  const blr::gdr::BwdCall c{(int)s.Dk, d_o, ds_last, q, k, v, dq, dk, dv, dg, dbeta, ds0, stream};
+  if (desc->io == BLR_F32) return blr::gdr::bwd_f32(p, c);
+  return l.np == 2 ? blr::gdr::bwd_bf16_state(p, c) : blr::gdr::bwd_bf16(p, c);
+}

@@ -1,0 +1,11 @@
+// The gated delta rule's kernels for blr_gdr_fwd and blr_gdr_bwd: bf16.
+#include "blr_gdr_launch.cuh"
+
+namespace blr {
+namespace gdr {
+
+blr_status fwd_bf16(const Problem& p, const FwdCall& c) { return fwd<__nv_bfloat16, 1, 1>(p, c); }
+blr_status bwd_bf16(const Problem& p, const BwdCall& c) { return bwd<__nv_bfloat16, 1, 1>(p, c); }
+
+}  // namespace gdr
+}  // namespace blr

@@ -1,0 +1,570 @@
+// Backward kernels of the gated delta rule (the forward's notation; D_ij = e^{G_i - G_j}):
+//     dU = scale P^T dO + diag(e^{G_C - G}) K dS'
+//     dS = gamma_C dS' + scale (diag(gamma) Q)^T dO - W^T dU      (the serial part)
+//     dR = T^T dU,  dV = diag(beta) dR,  dA = -dR U^T,  dP = dO U^T (lower triangles)
+//     dQ = scale diag(gamma) dO S^T + scale (dP o D) K
+//     dK = scale (dP o D)^T Q + diag(e^{G_C - G}) U dS'^T - diag(beta gamma) dR S^T + M K + M^T K,
+//          M_ij = beta_i dA_ij D_ij
+//     dbeta_i = dR_i.v_i - gamma_i (dR S^T)_i.k_i + sum_j dA_ij D_ij k_i.k_j
+// and the cumulative decay's gradient from every factor that holds it; each of its terms is a row
+// product of what the sums above already need.
+#pragma once
+
+#include "blr_gdr_tile.cuh"
+
+namespace blr {
+namespace gdr {
+
+template <int DK, int NI>
+struct DuSmem {
+  static constexpr int kQ = Tile<DK / 8, NI>::kBytes, kO = Tile<8, NI>::kBytes;
+  static constexpr int kBytes = 2 * kQ + kO + kGates * 4;
+};
+
+// The part of dU that does not hang on later chunks, scale P^T dO, for all chunks at once.
+template <typename TI, int DK, int NI, int NM>
+__global__ void __launch_bounds__(128)
+du_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k, const TI* __restrict__ d_o) {
+  extern __shared__ __align__(128) unsigned char smem[];
+  using L = DuSmem<DK, NI>;
+  const Where w = locate(P, blockIdx.x / P.n, blockIdx.x % P.n);
+  if (w.rows <= 0) return;
+  const uint32_t base = smem_u32(smem);
+  const Tile<DK / 8, NI> tq{base}, tk{base + L::kQ};
+  const Tile<8, NI> to{base + 2 * L::kQ};
+  float* G = reinterpret_cast<float*>(smem + 2 * L::kQ + L::kO);
+  const int tid = threadIdx.x, warp = tid >> 5, l = tid & 31;
+  const int64_t row0 = w.b * P.L + w.first, ldo = (int64_t)P.Hv * P.Dv;
+  const TI* src = d_o + row0 * ldo + (int64_t)w.h * P.Dv;
+  load_rows(tq, q + row0 * P.ldq + w.hk * DK, P.ldq, w.rows, tid, 128);
+  load_rows(tk, k + row0 * P.ldk + w.hk * DK, P.ldk, w.rows, tid, 128);
+  load_rows(to, src, ldo, w.rows, tid, 128);
+  copy_ws(smem_u32(G), P.gates + w.nc * kGates, 4 * kGateFloats<NM>, tid, 128);
+  cp_async_commit();
+  cp_async_wait<0>();
+  __syncthreads();
+  const int r0 = 16 * warp + (l >> 2), c0 = 2 * (l & 3);
+  uint32_t p[4][NM][4];  // scale P^T: rows j (this warp's), columns i >= j
+  {
+    float acc[8][4] = {};
+#pragma unroll
+    for (int kk = 0; kk < DK / 16; ++kk) {
+      uint32_t a[NI][4];
+      tk.a(2 * warp, 2 * kk, a);
+#pragma unroll
+      for (int nn = 0; nn < 4; ++nn)
+        if (nn >= warp) {
+          uint32_t b[2][NI][2];
+          tq.b_t(2 * nn, 2 * kk, b);
+          mma_p<NI, NI>(acc[2 * nn], a, b[0]);
+          mma_p<NI, NI>(acc[2 * nn + 1], a, b[1]);
+        }
+    }
+#pragma unroll
+    for (int nb = 0; nb < 8; ++nb)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int j = r0 + 8 * (e >> 1), i = 8 * nb + c0 + (e & 1);
+        acc[nb][e] = i >= j ? P.scale * acc[nb][e] * decay_between<NM>(G, i, j) : 0.0f;
+      }
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk) to_a<NM>(acc[2 * kk], acc[2 * kk + 1], p[kk]);
+  }
+  const int dvb = P.Dv / 64;
+  for (int part = 0; part < dvb; ++part) {
+    if (part > 0) {
+      __syncthreads();
+      load_rows(to, src + 64 * part, ldo, w.rows, tid, 128);
+      cp_async_commit();
+      cp_async_wait<0>();
+      __syncthreads();
+    }
+    float acc[8][4] = {};
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk)
+      if (kk >= warp) {
+#pragma unroll
+        for (int nn = 0; nn < 4; ++nn) {
+          uint32_t b[2][NI][2];
+          to.b(2 * nn, 2 * kk, b);
+          mma_p<NM, NI>(acc[2 * nn], p[kk], b[0]);
+          mma_p<NM, NI>(acc[2 * nn + 1], p[kk], b[1]);
+        }
+      }
+    char* out = P.dU + (w.nc * dvb + part) * Tile<8, NM>::kBytes;
+#pragma unroll
+    for (int nb = 0; nb < 8; ++nb) {
+      store_block<8, NM>(out, 2 * warp, nb, acc[nb][0], acc[nb][1]);
+      store_block<8, NM>(out, 2 * warp + 1, nb, acc[nb][2], acc[nb][3]);
+    }
+  }
+}
+
+template <int DK, int NI, int NM>
+struct BackSmem {
+  static constexpr int kW = Tile<DK / 8, NM>::kBytes, kK = Tile<DK / 8, NI>::kBytes, kO = Tile<8, NI>::kBytes,
+                       kU = Tile<8, NM>::kBytes;
+  static constexpr int kStage = kW + 2 * kK + kO + kU + kGates * 4;
+  static constexpr int kStages = 2 * kStage <= 227 * 1024 ? 2 : 1;
+  static constexpr int kBytes = kStages * kStage;
+};
+
+// The states' gradients from chunk to chunk, last to first: as chain_kernel, a warp holds dS^T of 16
+// columns in accumulators.
+template <typename TI, int DK, int NI, int NM>
+__global__ void __launch_bounds__(128)
+back_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k, const TI* __restrict__ d_o,
+            const float* __restrict__ ds_last, float* __restrict__ ds0) {
+  extern __shared__ __align__(128) unsigned char smem[];
+  using L = BackSmem<DK, NI, NM>;
+  const int dvb = P.Dv / 64;
+  const int64_t bh = blockIdx.x / dvb;
+  const int part = blockIdx.x % dvb;
+  const int tid = threadIdx.x, warp = tid >> 5, l = tid & 31;
+  const int64_t chunks = (locate(P, bh, 0).len + kC - 1) / kC;
+  const int col = 64 * part + 16 * warp + (l >> 2), row = 2 * (l & 3);
+  const int64_t ldo = (int64_t)P.Hv * P.Dv;
+  float S[DK / 8][4];
+#pragma unroll
+  for (int nb = 0; nb < DK / 8; ++nb)
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      S[nb][e] = ds_last == nullptr ? 0.0f : ds_last[(bh * DK + 8 * nb + row + (e & 1)) * P.Dv + col + 8 * (e >> 1)];
+  const auto load = [&](int64_t c) {
+    if (c >= 0) {
+      const Where w = locate(P, bh, c);
+      const uint32_t st = smem_u32(smem) + (uint32_t)(c % L::kStages) * L::kStage;
+      const int64_t row0 = w.b * P.L + w.first;
+      copy_ws(st, P.W + w.nc * L::kW, L::kW, tid, 128);
+      load_rows(Tile<DK / 8, NI>{st + L::kW}, k + row0 * P.ldk + w.hk * DK, P.ldk, w.rows, tid, 128);
+      load_rows(Tile<DK / 8, NI>{st + L::kW + L::kK}, q + row0 * P.ldq + w.hk * DK, P.ldq, w.rows, tid, 128);
+      load_rows(Tile<8, NI>{st + L::kW + 2 * L::kK}, d_o + row0 * ldo + (int64_t)w.h * P.Dv + 64 * part, ldo, w.rows,
+                tid, 128);
+      copy_ws(st + L::kW + 2 * L::kK + L::kO, P.dU + (w.nc * dvb + part) * L::kU, L::kU, tid, 128);
+      copy_ws(st + L::kW + 2 * L::kK + L::kO + L::kU, P.gates + w.nc * kGates, 4 * kGateFloats<NM>, tid, 128);
+    }
+    cp_async_commit();
+  };
+  for (int i = 0; i < L::kStages - 1; ++i) load(chunks - 1 - i);
+  for (int64_t c = chunks - 1; c >= 0; --c) {
+    load(c - (L::kStages - 1));
+    cp_async_wait<L::kStages - 1>();
+    __syncthreads();
+    const int s = (int)(c % L::kStages);
+    const uint32_t st = smem_u32(smem) + s * L::kStage;
+    const Tile<DK / 8, NM> tw{st};
+    const Tile<DK / 8, NI> tk{st + L::kW}, tq{st + L::kW + L::kK};
+    const Tile<8, NI> to{st + L::kW + 2 * L::kK};
+    const Tile<8, NM> tu{st + L::kW + 2 * L::kK + L::kO};
+    const float* G = reinterpret_cast<const float*>(smem + s * L::kStage + L::kW + 2 * L::kK + L::kO + L::kU);
+    const int64_t nc = bh * P.n + c;
+    // K dS': columns are the chunk's steps
+    float u[8][4] = {};
+    char* so = P.dS + (nc * dvb + part) * Tile<DK / 8, NM>::kBytes;
+#pragma unroll
+    for (int kk = 0; kk < DK / 16; ++kk) {
+      uint32_t a[NM][4];
+      to_a<NM>(S[2 * kk], S[2 * kk + 1], a);
+#pragma unroll
+      for (int p = 0; p < NM; ++p)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          *reinterpret_cast<uint32_t*>(so + p * Tile<DK / 8, NM>::kPlane +
+                                       ((2 * warp + (e & 1)) * (DK / 8) + 2 * kk + (e >> 1)) * 128 + l * 4) = a[p][e];
+#pragma unroll
+      for (int nn = 0; nn < 4; ++nn) {
+        uint32_t b[2][NI][2];
+        tk.b_t(2 * nn, 2 * kk, b);
+        mma_p<NM, NI>(u[2 * nn], a, b[0]);
+        mma_p<NM, NI>(u[2 * nn + 1], a, b[1]);
+      }
+    }
+    const float decay = exp_p<NM>(G[63]);
+#pragma unroll
+    for (int nb = 0; nb < DK / 8; ++nb)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) S[nb][e] *= decay;
+    char* uo = P.dU + (nc * dvb + part) * L::kU;
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk) {
+      // this chunk's dU^T, 16 steps of it: the decayed sum and the part computed before
+      uint32_t f[2][NM][2];
+      const int i = l >> 3;
+#pragma unroll
+      for (int p = 0; p < NM; ++p)
+        ldsm_t(tu.at(p, 2 * kk + (i >> 1), 2 * warp + (i & 1)) + (l & 7) * 16, f[0][p][0], f[0][p][1], f[1][p][0],
+               f[1][p][1]);
+      // dO^T of these steps, scaled by scale gamma
+      uint32_t fo[NI][4], ao[NM][4];
+      to.a_t(2 * warp, 2 * kk, fo);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float2 gg = *reinterpret_cast<const float2*>(&G[16 * kk + 8 * h + row]);
+        const float e0 = decay_between<NM>(G, 63, 16 * kk + 8 * h + row);
+        const float e1 = decay_between<NM>(G, 63, 16 * kk + 8 * h + row + 1);
+        const float y0 = P.scale * exp_p<NM>(gg.x), y1 = P.scale * exp_p<NM>(gg.y);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          uint32_t x[NM], xo[NI], yo[NM];
+#pragma unroll
+          for (int p = 0; p < NM; ++p) x[p] = f[h][p][e];
+          const float2 v = join2<NM>(x);
+          u[2 * kk + h][2 * e] = fmaf(u[2 * kk + h][2 * e], e0, v.x);
+          u[2 * kk + h][2 * e + 1] = fmaf(u[2 * kk + h][2 * e + 1], e1, v.y);
+          store_block_t<8, NM>(uo, 2 * kk + h, 2 * warp + e, u[2 * kk + h][2 * e], u[2 * kk + h][2 * e + 1]);
+#pragma unroll
+          for (int p = 0; p < NI; ++p) xo[p] = fo[p][2 * h + e];
+          const float2 ov = join2<NI>(xo);
+          split2<NM>(ov.x * y0, ov.y * y1, yo);
+#pragma unroll
+          for (int p = 0; p < NM; ++p) ao[p][2 * h + e] = yo[p];
+        }
+      }
+      uint32_t a[NM][4];
+      to_a<NM>(u[2 * kk], u[2 * kk + 1], a);
+#pragma unroll
+      for (int nn = 0; nn < DK / 16; ++nn) {
+        uint32_t b[2][NM][2], bq[2][NI][2];
+        tw.b(2 * nn, 2 * kk, b);  // holds -W
+        tq.b(2 * nn, 2 * kk, bq);
+        mma_p<NM, NM>(S[2 * nn], a, b[0]);
+        mma_p<NM, NM>(S[2 * nn + 1], a, b[1]);
+        mma_p<NM, NI>(S[2 * nn], ao, bq[0]);
+        mma_p<NM, NI>(S[2 * nn + 1], ao, bq[1]);
+      }
+    }
+    __syncthreads();
+  }
+  if (ds0 != nullptr) {
+#pragma unroll
+    for (int nb = 0; nb < DK / 8; ++nb)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        ds0[(bh * DK + 8 * nb + row + (e & 1)) * P.Dv + col + 8 * (e >> 1)] = S[nb][e];
+  }
+}
+
+template <int DK, int NI, int NM>
+struct GradSmem {
+  static constexpr int kQ = Tile<DK / 8, NI>::kBytes, kI = Tile<8, NI>::kBytes, kM = Tile<8, NM>::kBytes,
+                       kS = Tile<DK / 8, NM>::kBytes;
+  static constexpr int kTiles = 2 * kQ + kM /*T*/ + 2 * kI /*V, dO*/ + 2 * kM /*U, dU*/ + 2 * kS;
+  static constexpr int kFloats = kGates + 2 * 5 * 64 /*row sums by half*/ + 4 * 64 /*column sums by row group*/ + 16;
+  static constexpr int kBytes = kTiles + 4 * kFloats;
+};
+
+__device__ __forceinline__ float quad_sum(float x) {  // over the 4 lanes of a fragment row
+  x += __shfl_xor_sync(0xffffffffu, x, 1);
+  return x + __shfl_xor_sync(0xffffffffu, x, 2);
+}
+
+// Everything else, for all chunks at once. Warp (rg, hf) of 8 holds rows 16 rg .. of the chunk and half
+// of the columns of each product.
+template <typename TI, typename TG, int DK, int NI, int NM>
+__global__ void __launch_bounds__(256, 1)
+grad_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k, const TI* __restrict__ v,
+            const TI* __restrict__ d_o, TG* __restrict__ dq, TG* __restrict__ dk, int64_t heads, TI* __restrict__ dv,
+            TI* __restrict__ dg, TI* __restrict__ dbeta) {
+  // dq, dk: `heads` heads a step (the key heads, or the value heads where a later kernel sums them)
+  extern __shared__ __align__(128) unsigned char smem[];
+  using L = GradSmem<DK, NI, NM>;
+  constexpr int NB = DK / 16;  // 8-column blocks in a warp's half of Dk
+  const Where w = locate(P, blockIdx.x / P.n, blockIdx.x % P.n);
+  const int tid = threadIdx.x, warp = tid >> 5, l = tid & 31, rg = warp & 3, hf = warp >> 2;
+  const int64_t hq = heads == P.Hk ? w.hk : w.h;
+  if (w.rows < kC && w.len < P.L) {
+    for (int i = 0; i < kC; ++i) {
+      const int64_t t = padding_step(P, w, i);
+      if (t < 0) continue;
+      const int64_t at = w.b * P.L + t;
+      for (int j = tid; j < DK / 2; j += 256) {
+        store_pair(dq + (at * heads + hq) * DK + 2 * j, 0.0f, 0.0f);
+        store_pair(dk + (at * heads + hq) * DK + 2 * j, 0.0f, 0.0f);
+      }
+      for (int j = tid; j < P.Dv / 2; j += 256) store_pair(dv + (at * P.Hv + w.h) * P.Dv + 2 * j, 0.0f, 0.0f);
+      if (tid == 0) {
+        store_one(dg + at * P.Hv + w.h, 0.0f);
+        store_one(dbeta + at * P.Hv + w.h, 0.0f);
+      }
+    }
+  }
+  if (w.rows <= 0) return;
+  uint32_t at = smem_u32(smem);
+  const Tile<DK / 8, NI> tq{at}, tk{at + L::kQ};
+  const Tile<8, NM> tt{at + 2 * L::kQ}, tu{at + 2 * L::kQ + L::kM}, tdu{at + 2 * L::kQ + 2 * L::kM};
+  at += 2 * L::kQ + 3 * L::kM;
+  const Tile<8, NI> tv{at}, to{at + L::kI};
+  const Tile<DK / 8, NM> ts{at + 2 * L::kI}, tds{at + 2 * L::kI + L::kS};
+  float* G = reinterpret_cast<float*>(smem + L::kTiles);
+  float* bt = G + 64;
+  float* rows = G + kGates;         // [half][5][64]: dbeta without S, x1.q, x2.k, x3.k, row sums less none
+  float* cols = rows + 2 * 5 * 64;  // [rg][64]
+  float* dots = cols + 4 * 64;   // per warp: part of <S, dS'>
+  const int64_t row0 = w.b * P.L + w.first, ldo = (int64_t)P.Hv * P.Dv;
+  const int dvb = P.Dv / 64;
+  load_rows(tq, q + row0 * P.ldq + w.hk * DK, P.ldq, w.rows, tid, 256);
+  load_rows(tk, k + row0 * P.ldk + w.hk * DK, P.ldk, w.rows, tid, 256);
+  copy_ws(tt.base, P.T + w.nc * L::kM, L::kM, tid, 256);
+  copy_ws(smem_u32(G), P.gates + w.nc * kGates, 4 * kGateFloats<NM>, tid, 256);
+  const int rr = l >> 2, c0 = 2 * (l & 3), r0 = 16 * rg + rr;
+  float x1[NB][4] = {}, x2[NB][4] = {}, x3[NB][4] = {}, dp[4][4] = {}, da[4][4] = {};
+  float vdot[2] = {0.0f, 0.0f}, sdot = 0.0f;
+  for (int part = 0; part < dvb; ++part) {
+    if (part > 0) __syncthreads();
+    load_rows(tv, v + row0 * P.ldv + (int64_t)w.h * P.Dv + 64 * part, P.ldv, w.rows, tid, 256);
+    load_rows(to, d_o + row0 * ldo + (int64_t)w.h * P.Dv + 64 * part, ldo, w.rows, tid, 256);
+    const int64_t at8 = w.nc * dvb + part;
+    copy_ws(tu.base, P.U + at8 * L::kM, L::kM, tid, 256);
+    copy_ws(tdu.base, P.dU + at8 * L::kM, L::kM, tid, 256);
+    copy_ws(ts.base, P.S + at8 * L::kS, L::kS, tid, 256);
+    copy_ws(tds.base, P.dS + at8 * L::kS, L::kS, tid, 256);
+    cp_async_commit();
+    cp_async_wait<0>();
+    __syncthreads();
+    {  // dR, dV
+      float r[4][4] = {};
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk)
+        if (kk >= rg) {
+          uint32_t a[NM][4];
+          tt.a_t(2 * rg, 2 * kk, a);
+#pragma unroll
+          for (int nn = 0; nn < 2; ++nn) {
+            uint32_t b[2][NM][2];
+            tdu.b(4 * hf + 2 * nn, 2 * kk, b);
+            mma_p<NM, NM>(r[2 * nn], a, b[0]);
+            mma_p<NM, NM>(r[2 * nn + 1], a, b[1]);
+          }
+        }
+      const float b0 = bt[r0], b1 = bt[r0 + 8];
+      TI* out = dv + ((row0 + r0) * P.Hv + w.h) * P.Dv + 64 * part + 32 * hf + c0;
+#pragma unroll
+      for (int nb = 0; nb < 4; ++nb) {
+        const float2 va = tv.pair(2 * rg, 4 * hf + nb), vb = tv.pair(2 * rg + 1, 4 * hf + nb);
+        vdot[0] += r[nb][0] * va.x + r[nb][1] * va.y;
+        vdot[1] += r[nb][2] * vb.x + r[nb][3] * vb.y;
+        if (r0 < w.rows) store_pair(out + 8 * nb, b0 * r[nb][0], b0 * r[nb][1]);
+        if (r0 + 8 < w.rows) store_pair(out + 8 * ldo + 8 * nb, b1 * r[nb][2], b1 * r[nb][3]);
+      }
+      __syncthreads();  // dU has been read: dR takes its place
+#pragma unroll
+      for (int nb = 0; nb < 4; ++nb) {
+        tdu.put(2 * rg, 4 * hf + nb, r[nb][0], r[nb][1]);
+        tdu.put(2 * rg + 1, 4 * hf + nb, r[nb][2], r[nb][3]);
+      }
+    }
+    for (int i = tid; i < Tile<DK / 8, NM>::kPlane / 4; i += 256) {
+      uint32_t a[NM], b[NM];
+#pragma unroll
+      for (int p = 0; p < NM; ++p) {
+        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(a[p]) : "r"(ts.base + p * Tile<DK / 8, NM>::kPlane + 4 * i));
+        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(b[p]) : "r"(tds.base + p * Tile<DK / 8, NM>::kPlane + 4 * i));
+      }
+      const float2 x = join2<NM>(a), y = join2<NM>(b);
+      sdot += x.x * y.x + x.y * y.y;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk) {
+      uint32_t ao[NI][4], au[NM][4], ar[NM][4];
+      to.a(2 * rg, 2 * kk, ao);
+      tu.a(2 * rg, 2 * kk, au);
+      tdu.a(2 * rg, 2 * kk, ar);
+#pragma unroll
+      for (int nn = 0; nn < NB / 2; ++nn) {
+        uint32_t b[2][NM][2];
+        ts.b(NB * hf + 2 * nn, 2 * kk, b);
+        mma_p<NI, NM>(x1[2 * nn], ao, b[0]);
+        mma_p<NI, NM>(x1[2 * nn + 1], ao, b[1]);
+        mma_p<NM, NM>(x3[2 * nn], ar, b[0]);
+        mma_p<NM, NM>(x3[2 * nn + 1], ar, b[1]);
+        tds.b(NB * hf + 2 * nn, 2 * kk, b);
+        mma_p<NM, NM>(x2[2 * nn], au, b[0]);
+        mma_p<NM, NM>(x2[2 * nn + 1], au, b[1]);
+      }
+#pragma unroll
+      for (int nn = 0; nn < 2; ++nn) {
+        uint32_t b[2][NM][2];
+        tu.b_t(4 * hf + 2 * nn, 2 * kk, b);
+        mma_p<NI, NM>(dp[2 * nn], ao, b[0]);
+        mma_p<NI, NM>(dp[2 * nn + 1], ao, b[1]);
+        mma_p<NM, NM>(da[2 * nn], ar, b[0]);
+        mma_p<NM, NM>(da[2 * nn + 1], ar, b[1]);
+      }
+    }
+  }
+  __syncthreads();  // U and dR have been read: scale dP o D and M take their places
+  {
+    float qk[4][4] = {}, kk_[4][4] = {};
+#pragma unroll
+    for (int kk = 0; kk < DK / 16; ++kk) {
+      uint32_t aq[NI][4], ak[NI][4];
+      tq.a(2 * rg, 2 * kk, aq);
+      tk.a(2 * rg, 2 * kk, ak);
+#pragma unroll
+      for (int nn = 0; nn < 2; ++nn) {
+        uint32_t b[2][NI][2];
+        tk.b_t(4 * hf + 2 * nn, 2 * kk, b);
+        mma_p<NI, NI>(qk[2 * nn], aq, b[0]);
+        mma_p<NI, NI>(qk[2 * nn + 1], aq, b[1]);
+        mma_p<NI, NI>(kk_[2 * nn], ak, b[0]);
+        mma_p<NI, NI>(kk_[2 * nn + 1], ak, b[1]);
+      }
+    }
+    float rs[2] = {0.0f, 0.0f}, bs[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int nb = 0; nb < 4; ++nb) {
+      float cs[2] = {0.0f, 0.0f};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int i = r0 + 8 * (e >> 1), j = 32 * hf + 8 * nb + c0 + (e & 1);
+        const float d = j <= i ? decay_between<NM>(G, i, j) : 0.0f;
+        const float p = P.scale * dp[nb][e] * d;
+        const float m0 = j < i ? -da[nb][e] * d : 0.0f, mk = m0 * kk_[nb][e], b = bt[i];
+        const float sum = p * qk[nb][e] + b * mk;
+        rs[e >> 1] += sum;
+        bs[e >> 1] += mk;
+        cs[e & 1] += sum;
+        dp[nb][e] = p;
+        da[nb][e] = b * m0;
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        tu.put(2 * rg + e, 4 * hf + nb, dp[nb][2 * e], dp[nb][2 * e + 1]);
+        tdu.put(2 * rg + e, 4 * hf + nb, da[nb][2 * e], da[nb][2 * e + 1]);
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) cs[e] += __shfl_xor_sync(0xffffffffu, cs[e], d);
+        if (l < 4) cols[rg * 64 + 32 * hf + 8 * nb + c0 + e] = cs[e];
+      }
+    }
+    // row products, on this warp's columns
+    float y1[2] = {0.0f, 0.0f}, y2[2] = {0.0f, 0.0f}, y3[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float2 qv = tq.pair(2 * rg + e, NB * hf + nb), kv = tk.pair(2 * rg + e, NB * hf + nb);
+        y1[e] += x1[nb][2 * e] * qv.x + x1[nb][2 * e + 1] * qv.y;
+        y2[e] += x2[nb][2 * e] * kv.x + x2[nb][2 * e + 1] * kv.y;
+        y3[e] += x3[nb][2 * e] * kv.x + x3[nb][2 * e + 1] * kv.y;
+      }
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const float a[5] = {quad_sum(vdot[e] + bs[e]), quad_sum(y1[e]), quad_sum(y2[e]), quad_sum(y3[e]),
+                          quad_sum(rs[e])};
+      if ((l & 3) == 0) {
+#pragma unroll
+        for (int i = 0; i < 5; ++i) rows[(hf * 5 + i) * 64 + r0 + 8 * e] = a[i];
+      }
+    }
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) sdot += __shfl_xor_sync(0xffffffffu, sdot, d);
+    if (l == 0) dots[warp] = sdot;
+  }
+  __syncthreads();
+  if (warp == 0) {  // dbeta, and dg: the cumulative decay's gradient summed from the end
+    float dG[2], add = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int i = 2 * l + e;
+      float a[5];
+#pragma unroll
+      for (int x = 0; x < 5; ++x) a[x] = rows[x * 64 + i] + rows[(5 + x) * 64 + i];
+      const float up = exp_p<NM>(G[i]), down = decay_between<NM>(G, 63, i);
+      const float col = (cols[i] + cols[64 + i]) + (cols[128 + i] + cols[192 + i]);
+      dG[e] = P.scale * up * a[1] - bt[i] * up * a[3] - down * a[2] + a[4] - col;
+      add += down * a[2];
+      if (i < w.rows) store_one(dbeta + (row0 + i) * P.Hv + w.h, a[0] - up * a[3]);
+    }
+    const float all = ((dots[0] + dots[1]) + (dots[2] + dots[3])) + ((dots[4] + dots[5]) + (dots[6] + dots[7]));
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) add += __shfl_xor_sync(0xffffffffu, add, d);
+    if (l == 31) dG[1] += add + exp_p<NM>(G[63]) * all;
+    float s = dG[0] + dG[1];
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const float o = __shfl_down_sync(0xffffffffu, s, d);
+      if (l + d < 32) s += o;
+    }
+    if (2 * l < w.rows) store_one(dg + (row0 + 2 * l) * P.Hv + w.h, s);
+    if (2 * l + 1 < w.rows) store_one(dg + (row0 + 2 * l + 1) * P.Hv + w.h, s - dG[0]);
+  }
+  const float up0 = exp_p<NM>(G[r0]), up1 = exp_p<NM>(G[r0 + 8]);
+  const float dn0 = decay_between<NM>(G, 63, r0), dn1 = decay_between<NM>(G, 63, r0 + 8);
+  const float b0 = bt[r0] * up0, b1 = bt[r0 + 8] * up1;
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      x1[nb][e] *= P.scale * (e < 2 ? up0 : up1);
+      x2[nb][e] = x2[nb][e] * (e < 2 ? dn0 : dn1) - x3[nb][e] * (e < 2 ? b0 : b1);
+    }
+#pragma unroll
+  for (int kk = 0; kk < 4; ++kk) {
+    if (kk <= rg) {  // rows of scale dP o D and of M against K
+      uint32_t ap[NM][4], am[NM][4];
+      tu.a(2 * rg, 2 * kk, ap);
+      tdu.a(2 * rg, 2 * kk, am);
+#pragma unroll
+      for (int nn = 0; nn < NB / 2; ++nn) {
+        uint32_t b[2][NI][2];
+        tk.b(NB * hf + 2 * nn, 2 * kk, b);
+        mma_p<NM, NI>(x1[2 * nn], ap, b[0]);
+        mma_p<NM, NI>(x1[2 * nn + 1], ap, b[1]);
+        mma_p<NM, NI>(x2[2 * nn], am, b[0]);
+        mma_p<NM, NI>(x2[2 * nn + 1], am, b[1]);
+      }
+    }
+    if (kk >= rg) {  // their columns against Q and K
+      uint32_t ap[NM][4], am[NM][4];
+      tu.a_t(2 * rg, 2 * kk, ap);
+      tdu.a_t(2 * rg, 2 * kk, am);
+#pragma unroll
+      for (int nn = 0; nn < NB / 2; ++nn) {
+        uint32_t b[2][NI][2];
+        tq.b(NB * hf + 2 * nn, 2 * kk, b);
+        mma_p<NM, NI>(x2[2 * nn], ap, b[0]);
+        mma_p<NM, NI>(x2[2 * nn + 1], ap, b[1]);
+        tk.b(NB * hf + 2 * nn, 2 * kk, b);
+        mma_p<NM, NI>(x2[2 * nn], am, b[0]);
+        mma_p<NM, NI>(x2[2 * nn + 1], am, b[1]);
+      }
+    }
+  }
+  TG* oq = dq + ((row0 + r0) * heads + hq) * DK + 8 * NB * hf + c0;
+  TG* ok = dk + ((row0 + r0) * heads + hq) * DK + 8 * NB * hf + c0;
+#pragma unroll
+  for (int e = 0; e < 2; ++e)
+    if (r0 + 8 * e < w.rows) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        store_pair(oq + 8 * e * heads * DK + 8 * nb, x1[nb][2 * e], x1[nb][2 * e + 1]);
+        store_pair(ok + 8 * e * heads * DK + 8 * nb, x2[nb][2 * e], x2[nb][2 * e + 1]);
+      }
+    }
+}
+
+// Gradients of shared key heads: the sum over their value heads, in head order.
+template <typename TI>
+__global__ void __launch_bounds__(256)
+share_kernel(const float* __restrict__ pq, const float* __restrict__ pk, TI* __restrict__ dq, TI* __restrict__ dk,
+             int64_t pairs, int group, int half_dk) {  // pairs of values of dq (and of dk)
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < pairs; i += (int64_t)gridDim.x * 256) {
+    const int64_t head = i / half_dk;
+    const int d = (int)(i % half_dk) * 2;
+    float2 a = make_float2(0.0f, 0.0f), b = a;
+    for (int j = 0; j < group; ++j) {
+      const int64_t at = (head * group + j) * half_dk * 2 + d;
+      const float2 x = __ldcs(reinterpret_cast<const float2*>(pq + at)), y = __ldcs(reinterpret_cast<const float2*>(pk + at));
+      a.x += x.x;
+      a.y += x.y;
+      b.x += y.x;
+      b.y += y.y;
+    }
+    store_pair(dq + 2 * i, a.x, a.y);
+    store_pair(dk + 2 * i, b.x, b.y);
+  }
+}
+
+}  // namespace gdr
+}  // namespace blr

@@ -1,0 +1,65 @@
+// The launches that blr_gdr_launch.h declares, for one choice of types.
+#pragma once
+
+#include "blr_gdr_bwd.cuh"
+#include "blr_gdr_fwd.cuh"
+#include "blr_gdr_launch.h"
+
+namespace blr {
+namespace gdr {
+
+// Lets the kernel use `bytes` of shared memory (a call of a microsecond, on the current device).
+template <typename K, typename... A>
+blr_status start(const char* name, K kernel, int64_t blocks, int threads, int bytes, cudaStream_t stream, A... args) {
+  if (bytes > 48 * 1024)
+    BLR_TRY(cuda_check(cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel),
+                                            cudaFuncAttributeMaxDynamicSharedMemorySize, bytes), name));
+  kernel<<<(unsigned)blocks, threads, bytes, stream>>>(args...);
+  return cuda_check(cudaGetLastError(), name);
+}
+
+template <typename TI, int DK, int NI, int NM>
+blr_status fwd_dk(const Problem& p, const FwdCall& c) {
+  const int64_t chunks = p.B * p.Hv * p.n;
+  const TI *q = static_cast<const TI*>(c.q), *k = static_cast<const TI*>(c.k), *v = static_cast<const TI*>(c.v),
+           *g = static_cast<const TI*>(c.g), *beta = static_cast<const TI*>(c.beta);
+  BLR_TRY(start("prepare", c.train ? prepare_kernel<TI, DK, NI, NM, true> : prepare_kernel<TI, DK, NI, NM, false>,
+                chunks, 128, PrepareSmem<DK, NI, NM>::kBytes, c.stream, p, k, v, g, beta));
+  BLR_TRY(start("chain", chain_kernel<TI, DK, NI, NM>, p.B * p.Hv * (p.Dv / 64), 128, ChainSmem<DK, NI, NM>::kBytes,
+                c.stream, p, k, c.s0, c.s_last));
+  return start("output", output_kernel<TI, DK, NI, NM>, chunks, 128, OutputSmem<DK, NI, NM>::kBytes, c.stream, p, q, k,
+               static_cast<TI*>(c.o));
+}
+
+template <typename TI, int DK, int NI, int NM>
+blr_status bwd_dk(const Problem& p, const BwdCall& c) {
+  const int64_t chunks = p.B * p.Hv * p.n;
+  const TI *q = static_cast<const TI*>(c.q), *k = static_cast<const TI*>(c.k), *v = static_cast<const TI*>(c.v),
+           *d_o = static_cast<const TI*>(c.d_o);
+  TI *dq = static_cast<TI*>(c.dq), *dk = static_cast<TI*>(c.dk_out), *dv = static_cast<TI*>(c.dv),
+     *dg = static_cast<TI*>(c.dg), *dbeta = static_cast<TI*>(c.dbeta);
+  BLR_TRY(start("du", du_kernel<TI, DK, NI, NM>, chunks, 128, DuSmem<DK, NI>::kBytes, c.stream, p, q, k, d_o));
+  BLR_TRY(start("back", back_kernel<TI, DK, NI, NM>, p.B * p.Hv * (p.Dv / 64), 128, BackSmem<DK, NI, NM>::kBytes,
+                c.stream, p, q, k, d_o, c.ds_last, c.ds0));
+  constexpr int bytes = GradSmem<DK, NI, NM>::kBytes;
+  if (p.Hk == p.Hv)
+    return start("grad", grad_kernel<TI, TI, DK, NI, NM>, chunks, 256, bytes, c.stream, p, q, k, v, d_o, dq, dk,
+                 (int64_t)p.Hk, dv, dg, dbeta);
+  BLR_TRY(start("grad", grad_kernel<TI, float, DK, NI, NM>, chunks, 256, bytes, c.stream, p, q, k, v, d_o, p.pq, p.pk,
+                (int64_t)p.Hv, dv, dg, dbeta));
+  const int64_t pairs = p.B * p.L * p.Hk * (DK / 2), blocks = (pairs + 255) / 256;
+  return start("share", share_kernel<TI>, blocks < 152 * 16 ? blocks : 152 * 16, 256, 0, c.stream,
+               (const float*)p.pq, (const float*)p.pk, dq, dk, pairs, p.Hv / p.Hk, DK / 2);
+}
+
+template <typename TI, int NI, int NM>
+blr_status fwd(const Problem& p, const FwdCall& c) {
+  return c.dk == 64 ? fwd_dk<TI, 64, NI, NM>(p, c) : fwd_dk<TI, 128, NI, NM>(p, c);
+}
+template <typename TI, int NI, int NM>
+blr_status bwd(const Problem& p, const BwdCall& c) {
+  return c.dk == 64 ? bwd_dk<TI, 64, NI, NM>(p, c) : bwd_dk<TI, 128, NI, NM>(p, c);
+}
+
+}  // namespace gdr
+}  // namespace blr

@@ -1,0 +1,38 @@
+// Launches of the gated delta rule's kernels, by type of the tensors and of the operands: float32,
+// bfloat16 with float32 states, bfloat16. Each is instantiated in a source file of its own.
+#pragma once
+
+#include "blr_gdr_tile.cuh"
+#include "blr_host.h"
+
+namespace blr {
+namespace gdr {
+
+struct FwdCall {
+  int dk;
+  bool train;
+  const void *q, *k, *v, *g, *beta;
+  const float* s0;
+  void* o;
+  float* s_last;
+  cudaStream_t stream;
+};
+struct BwdCall {
+  int dk;
+  const void* d_o;
+  const float* ds_last;
+  const void *q, *k, *v;
+  void *dq, *dk_out, *dv, *dg, *dbeta;
+  float* ds0;
+  cudaStream_t stream;
+};
+
+blr_status fwd_f32(const Problem& p, const FwdCall& c);
+blr_status fwd_bf16_state(const Problem& p, const FwdCall& c);
+blr_status fwd_bf16(const Problem& p, const FwdCall& c);
+blr_status bwd_f32(const Problem& p, const BwdCall& c);
+blr_status bwd_bf16_state(const Problem& p, const BwdCall& c);
+blr_status bwd_bf16(const Problem& p, const BwdCall& c);
+
+}  // namespace gdr
+}  // namespace blr

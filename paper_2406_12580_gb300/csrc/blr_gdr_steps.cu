@@ -1,0 +1,182 @@
+// Recurrent steps of the gated delta rule (blr_gdr_steps in blr.h).
+//
+// The state S (Dk x Dv) of a (row, head) is read once, taken through the K
+// steps in registers and written once:
+//     r = a S^T k,  u = beta (v - r),  S = a S + k u^T,  o = scale S^T q.
+// Bound by memory: 8 Dk Dv bytes a (row, head) with float32 states, against
+// 3 K Dk Dv multiply-adds.
+//
+// The columns of S are independent but for the shared k and q, so a warp takes
+// 16 columns and all Dk rows: lane (rg, c) holds rows [rg Dk/8, (rg + 1) Dk/8)
+// x 4 columns, in 16-byte loads whose 4 neighbours fill 64 bytes of a row. The
+// two sums over rows are then 3 shuffles each; no warp waits for another.
+#include <cuda_bf16.h>
+
+#include "blr_gdr.h"
+
+namespace {
+
+using blr::fail;
+
+constexpr int kWarps = 4;  // 64 columns a block
+
+__device__ __forceinline__ float to_f(float x) { return x; }
+__device__ __forceinline__ float to_f(__nv_bfloat16 x) { return __bfloat162float(x); }
+
+__device__ __forceinline__ float4 load4(const float* p) { return __ldcs(reinterpret_cast<const float4*>(p)); }
+__device__ __forceinline__ float4 load4(const __nv_bfloat16* p) {
+  const uint2 r = __ldcs(reinterpret_cast<const uint2*>(p));
+  return make_float4(__uint_as_float(r.x << 16), __uint_as_float(r.x & 0xffff0000u),
+                     __uint_as_float(r.y << 16), __uint_as_float(r.y & 0xffff0000u));
+}
+__device__ __forceinline__ void store4(float* p, float4 x) { __stcs(reinterpret_cast<float4*>(p), x); }
+__device__ __forceinline__ void store4(__nv_bfloat16* p, float4 x) {
+  const __nv_bfloat162 a = __floats2bfloat162_rn(x.x, x.y), b = __floats2bfloat162_rn(x.z, x.w);
+  __stcs(reinterpret_cast<uint2*>(p),
+         make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b)));
+}
+
+// 8 consecutive values of q or k
+__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
+  const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
+  x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+  x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+}
+__device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&x)[8]) {
+  const uint4 r = __ldg(reinterpret_cast<const uint4*>(p));
+  const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = __uint_as_float(w[i] << 16);
+    x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+}
+
+__device__ __forceinline__ float4 sum_rows(float4 x) {  // over the 8 row groups (lane bits 2..4)
+#pragma unroll
+  for (int d = 4; d <= 16; d <<= 1) {
+    x.x += __shfl_xor_sync(0xffffffffu, x.x, d);
+    x.y += __shfl_xor_sync(0xffffffffu, x.y, d);
+    x.z += __shfl_xor_sync(0xffffffffu, x.z, d);
+    x.w += __shfl_xor_sync(0xffffffffu, x.w, d);
+  }
+  return x;
+}
+
+template <typename T, typename TS, int DK>
+__global__ void __launch_bounds__(kWarps * 32)
+gdr_steps_kernel(int64_t K, int Hk, int Hv, int Dv, int64_t ldq, int64_t ldk, int64_t ldv, float scale,
+                 const TS* s_prev, const T* __restrict__ q, const T* __restrict__ k,
+                 const T* __restrict__ v, const T* __restrict__ g, const T* __restrict__ beta, TS* s_out,
+                 T* __restrict__ o) {
+  constexpr int R = DK / 8;
+  const int parts = Dv / (16 * kWarps);
+  const int64_t bh = blockIdx.x / parts;
+  const int part = blockIdx.x % parts;
+  const int64_t b = bh / Hv;
+  const int h = (int)(bh % Hv), hk = h / (Hv / Hk);
+  const int lane = threadIdx.x & 31, rg = lane >> 2;
+  const int col = (part * kWarps + (threadIdx.x >> 5)) * 16 + (lane & 3) * 4;
+  const int64_t base = (bh * DK + rg * R) * Dv + col;
+  float4 S[R];
+  if (s_prev != nullptr) {
+#pragma unroll
+    for (int i = 0; i < R; ++i) S[i] = load4(s_prev + base + (int64_t)i * Dv);
+  } else {
+#pragma unroll
+    for (int i = 0; i < R; ++i) S[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  }
+  for (int64_t t = 0; t < K; ++t) {
+    const int64_t at = b * K + t;
+    const float a = expf(fmaxf(to_f(g[at * Hv + h]), -120.0f)), bt = to_f(beta[at * Hv + h]);
+    const T* kp = k + at * ldk + hk * DK + rg * R;
+    const T* qp = q + at * ldq + hk * DK + rg * R;
+    const T* vp = v + at * ldv + (int64_t)h * Dv + col;
+    float kk[R];
+#pragma unroll
+    for (int i = 0; i < R; i += 8) load8(kp + i, *reinterpret_cast<float(*)[8]>(&kk[i]));
+    float4 r = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      r.x = fmaf(kk[i], S[i].x, r.x);
+      r.y = fmaf(kk[i], S[i].y, r.y);
+      r.z = fmaf(kk[i], S[i].z, r.z);
+      r.w = fmaf(kk[i], S[i].w, r.w);
+    }
+    r = sum_rows(r);
+    const float4 u = make_float4(bt * (to_f(vp[0]) - a * r.x), bt * (to_f(vp[1]) - a * r.y),
+                                 bt * (to_f(vp[2]) - a * r.z), bt * (to_f(vp[3]) - a * r.w));
+    float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+    for (int i = 0; i < R; i += 8) {
+      float qq[8];
+      load8(qp + i, qq);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        float4& s = S[i + j];
+        s.x = fmaf(kk[i + j], u.x, a * s.x);
+        s.y = fmaf(kk[i + j], u.y, a * s.y);
+        s.z = fmaf(kk[i + j], u.z, a * s.z);
+        s.w = fmaf(kk[i + j], u.w, a * s.w);
+        y.x = fmaf(qq[j], s.x, y.x);
+        y.y = fmaf(qq[j], s.y, y.y);
+        y.z = fmaf(qq[j], s.z, y.z);
+        y.w = fmaf(qq[j], s.w, y.w);
+      }
+    }
+    if (o != nullptr) {
+      y = sum_rows(y);
+      if (rg == 0) store4(o + at * Hv * Dv + (int64_t)h * Dv + col,
+                          make_float4(scale * y.x, scale * y.y, scale * y.z, scale * y.w));
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < R; ++i) store4(s_out + base + (int64_t)i * Dv, S[i]);
+}
+
+template <typename T, typename TS, int DK>
+blr_status launch(const blr::GdrSizes& s, float scale, const void* s_prev, const void* q, const void* k,
+                  const void* v, const void* g, const void* beta, void* s_out, void* o,
+                  cudaStream_t stream) {
+  const int64_t blocks = s.B * s.Hv * (s.Dv / (16 * kWarps));
+  if (blocks > 0x7fffffff) return fail(BLR_ERR_UNSUPPORTED, "too many states");
+  gdr_steps_kernel<T, TS, DK><<<(unsigned)blocks, kWarps * 32, 0, stream>>>(
+      s.L, (int)s.Hk, (int)s.Hv, (int)s.Dv, s.ldq, s.ldk, s.ldv, scale, static_cast<const TS*>(s_prev),
+      static_cast<const T*>(q), static_cast<const T*>(k), static_cast<const T*>(v),
+      static_cast<const T*>(g), static_cast<const T*>(beta), static_cast<TS*>(s_out), static_cast<T*>(o));
+  return blr::cuda_check(cudaGetLastError(), "blr_gdr_steps");
+}
+
+template <typename T, typename TS, typename... A>
+blr_status by_dk(const blr::GdrSizes& s, A... a) {
+  return s.Dk == 64 ? launch<T, TS, 64>(s, a...) : launch<T, TS, 128>(s, a...);
+}
+
+}  // namespace
+
+blr_status blr_gdr_steps(const blr_gdr_desc* desc, blr_dtype state, const void* s_prev, const void* q,
+                         const void* k, const void* v, const void* g, const void* beta, void* s_out,
+                         void* o, blr_stream_t stream) {
+  blr::GdrSizes s;
+  BLR_TRY(blr::gdr_check(desc, &s));
+  if (state != BLR_F32 && state != BLR_BF16)
+    return fail(BLR_ERR_INVALID_ARG, "unknown state dtype %d", (int)state);
+  if (s.empty) return BLR_OK;
+  BLR_TRY(blr::need(s_out, "s_out", 16));
+  BLR_TRY(blr::optional(s_prev, "s_prev", 16));
+  if (s.L > 0) {
+    BLR_TRY(blr::need(q, "q", 16));
+    BLR_TRY(blr::need(k, "k", 16));
+    BLR_TRY(blr::need(v, "v", 16));
+    BLR_TRY(blr::need(g, "g", desc->io == BLR_F32 ? 4 : 2));
+    BLR_TRY(blr::need(beta, "beta", desc->io == BLR_F32 ? 4 : 2));
+    BLR_TRY(blr::optional(o, "o", 16));
+  }
+  const float c = desc->scale;
+  if (desc->io == BLR_F32)
+    return state == BLR_F32 ? by_dk<float, float>(s, c, s_prev, q, k, v, g, beta, s_out, o, stream)
+                            : by_dk<float, __nv_bfloat16>(s, c, s_prev, q, k, v, g, beta, s_out, o, stream);
+  return state == BLR_F32
+             ? by_dk<__nv_bfloat16, float>(s, c, s_prev, q, k, v, g, beta, s_out, o, stream)
+             : by_dk<__nv_bfloat16, __nv_bfloat16>(s, c, s_prev, q, k, v, g, beta, s_out, o, stream);
+}

@@ -1,0 +1,307 @@
+// Tiles, fragments and matrix products of the gated delta rule's kernels.
+//
+// A chunk is 64 steps. Every matrix tile has 64 rows and is kept, in shared
+// memory and in the workspace, as 8 x 8 blocks of bfloat16 of 128 contiguous
+// bytes, block rows one after the other: a fragment load reads whole blocks
+// (no bank conflicts, no padding, no swizzle), a register of an accumulator
+// tile is one block (a 128-byte store), and a tile of the workspace is copied
+// linearly. A matrix in float32 precision is carried as two planes of such
+// tiles, x = hi + lo with 16 significant bits together; a product of two such
+// operands is hi hi + lo hi + hi lo.
+//
+// The products use the warp-level m16n8k16 instruction: the recurrence over
+// chunks then stays in a warp's registers (an accumulator tile is, unchanged,
+// the next product's left operand), with no trip through shared or tensor
+// memory between its dependent products.
+#pragma once
+
+#include <stdint.h>
+
+#include <type_traits>
+
+#include <cuda_bf16.h>
+
+namespace blr {
+namespace gdr {
+
+constexpr int kC = 64;               // steps of a chunk
+constexpr float kMinDecay = -120.0f;  // exp(-120) is 0 in float32
+
+__device__ __forceinline__ uint32_t smem_u32(const void* p) {
+  return (uint32_t)__cvta_generic_to_shared(p);
+}
+
+__device__ __forceinline__ uint32_t pack2(float a, float b) {  // a in the low half
+  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ float lo_f(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float hi_f(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+
+// Two values as P planes of packed pairs.
+template <int P>
+__device__ __forceinline__ void split2(float a, float b, uint32_t (&w)[P]) {
+  w[0] = pack2(a, b);
+  if constexpr (P == 2) w[1] = pack2(a - lo_f(w[0]), b - hi_f(w[0]));
+}
+template <int P>
+__device__ __forceinline__ float2 join2(const uint32_t (&w)[P]) {
+  float2 r = make_float2(lo_f(w[0]), hi_f(w[0]));
+  if constexpr (P == 2) {
+    r.x += lo_f(w[1]);
+    r.y += hi_f(w[1]);
+  }
+  return r;
+}
+
+// exp of a value <= 0: to the last bits where operands have two planes.
+template <int P>
+__device__ __forceinline__ float exp_p(float x) {
+  if constexpr (P == 2) return expf(x);
+  return __expf(x);
+}
+
+// A chunk's gates: its cumulative log decay (64), beta (64), and with two planes what the decay's
+// floats leave out (64).
+constexpr int kGates = 192;
+template <int P>
+constexpr int kGateFloats = P == 2 ? 192 : 128;
+
+// e^{G_i - G_j}, j <= i
+template <int P>
+__device__ __forceinline__ float decay_between(const float* G, int i, int j) {
+  float d = G[i] - G[j];
+  if constexpr (P == 2) d += G[128 + i] - G[128 + j];
+  return exp_p<P>(d);
+}
+
+__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
+      "{%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+template <int PA, int PB>
+__device__ __forceinline__ void mma_p(float (&d)[4], const uint32_t (&a)[PA][4], const uint32_t (&b)[PB][2]) {
+  mma(d, a[0], b[0][0], b[0][1]);
+  if constexpr (PA == 2) mma(d, a[1], b[0][0], b[0][1]);
+  if constexpr (PB == 2) mma(d, a[0], b[1][0], b[1][1]);
+}
+
+__device__ __forceinline__ void ldsm(uint32_t addr, uint32_t& r0, uint32_t& r1, uint32_t& r2, uint32_t& r3) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r0), "=r"(r1), "=r"(r2), "=r"(r3) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm_t(uint32_t addr, uint32_t& r0, uint32_t& r1, uint32_t& r2, uint32_t& r3) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r0), "=r"(r1), "=r"(r2), "=r"(r3) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+
+// A tile of 64 rows x C8 * 8 columns in shared memory, P planes.
+template <int C8, int P>
+struct Tile {
+  static constexpr int kPlane = 8 * C8 * 128;  // bytes
+  static constexpr int kBytes = P * kPlane;
+  uint32_t base;
+  __device__ __forceinline__ uint32_t at(int p, int r8, int c8) const {
+    return base + p * kPlane + (r8 * C8 + c8) * 128;
+  }
+  // Left operand, rows 8 m8 .. + 16, columns 8 k8 .. + 16, of the tile.
+  __device__ __forceinline__ void a(int m8, int k8, uint32_t (&f)[P][4]) const {
+    const int l = threadIdx.x & 31, i = l >> 3;
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+      ldsm(at(p, m8 + (i & 1), k8 + (i >> 1)) + (l & 7) * 16, f[p][0], f[p][1], f[p][2], f[p][3]);
+  }
+  // Left operand of the transposed tile: rows 8 m8 .. are the tile's columns.
+  __device__ __forceinline__ void a_t(int m8, int k8, uint32_t (&f)[P][4]) const {
+    const int l = threadIdx.x & 31, i = l >> 3;
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+      ldsm_t(at(p, k8 + (i >> 1), m8 + (i & 1)) + (l & 7) * 16, f[p][0], f[p][1], f[p][2], f[p][3]);
+  }
+  // Right operands of two 8-column blocks n8, n8 + 1 of X^T, X this tile (its rows are the columns).
+  __device__ __forceinline__ void b_t(int n8, int k8, uint32_t (&f)[2][P][2]) const {
+    const int l = threadIdx.x & 31, i = l >> 3;
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+      ldsm(at(p, n8 + (i >> 1), k8 + (i & 1)) + (l & 7) * 16, f[0][p][0], f[0][p][1], f[1][p][0], f[1][p][1]);
+  }
+  // Right operands of two 8-column blocks of X, X this tile.
+  __device__ __forceinline__ void b(int n8, int k8, uint32_t (&f)[2][P][2]) const {
+    const int l = threadIdx.x & 31, i = l >> 3;
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+      ldsm_t(at(p, k8 + (i & 1), n8 + (i >> 1)) + (l & 7) * 16, f[0][p][0], f[0][p][1], f[1][p][0], f[1][p][1]);
+  }
+  // The pair of values (row 8 r8 + lane / 4, columns 8 c8 + 2 (lane % 4) + {0, 1}).
+  __device__ __forceinline__ float2 pair(int r8, int c8) const {
+    uint32_t w[P];
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+      asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[p]) : "r"(at(p, r8, c8) + (threadIdx.x & 31) * 4) : "memory");
+    return join2<P>(w);
+  }
+  __device__ __forceinline__ void put(int r8, int c8, float x, float y) const {
+    uint32_t w[P];
+    split2<P>(x, y, w);
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+      asm volatile("st.shared.b32 [%0], %1;" ::"r"(at(p, r8, c8) + (threadIdx.x & 31) * 4), "r"(w[p]) : "memory");
+  }
+};
+
+// An accumulator tile (16 rows x 8 columns in d[0], d[1]: row lane / 4; d[2], d[3]: row + 8) as half
+// of a left operand: blocks (x, y) give its columns 0..7 and 8..15.
+template <int P>
+__device__ __forceinline__ void to_a(const float (&x)[4], const float (&y)[4], uint32_t (&f)[P][4]) {
+  uint32_t w[P];
+  split2<P>(x[0], x[1], w);
+#pragma unroll
+  for (int p = 0; p < P; ++p) f[p][0] = w[p];
+  split2<P>(x[2], x[3], w);
+#pragma unroll
+  for (int p = 0; p < P; ++p) f[p][1] = w[p];
+  split2<P>(y[0], y[1], w);
+#pragma unroll
+  for (int p = 0; p < P; ++p) f[p][2] = w[p];
+  split2<P>(y[2], y[3], w);
+#pragma unroll
+  for (int p = 0; p < P; ++p) f[p][3] = w[p];
+}
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool real) {
+  const int n = real ? 16 : 0;  // the rest of the 16 bytes becomes zero
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// A linear copy of `bytes` (a multiple of 16) from the workspace.
+__device__ __forceinline__ void copy_ws(uint32_t dst, const void* src, int bytes, int tid, int threads) {
+  for (int i = tid * 16; i < bytes; i += threads * 16)
+    cp_async16(dst + i, static_cast<const char*>(src) + i, true);
+}
+
+// 64 rows of a caller's tensor (row r at p + r ld; rows from `rows` on are zero and not read) as a
+// tile. bfloat16 arrives asynchronously; float32 is split into its planes on the way. 16-byte piece i
+// of the tile is row 8 (i / (8 C8)) + i % 8, column block (i / 8) % C8: a warp reads 64 bytes of 8 rows.
+template <int C8>
+__device__ __forceinline__ void load_rows(const Tile<C8, 1>& t, const __nv_bfloat16* p, int64_t ld, int rows,
+                                          int tid, int threads) {
+  for (int i = tid; i < 64 * C8; i += threads) {
+    const int r = (i / (8 * C8)) * 8 + (i & 7), c8 = (i >> 3) % C8;
+    const bool real = r < rows;
+    cp_async16(t.base + i * 16, p + (real ? r * ld + c8 * 8 : 0), real);
+  }
+}
+template <int C8>
+__device__ __forceinline__ void load_rows(const Tile<C8, 2>& t, const float* p, int64_t ld, int rows, int tid,
+                                          int threads) {
+  for (int i = tid; i < 64 * C8; i += threads) {
+    const int r = (i / (8 * C8)) * 8 + (i & 7), c8 = (i >> 3) % C8;
+    float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f), y = x;
+    if (r < rows) {
+      const float4* s = reinterpret_cast<const float4*>(p + r * ld + c8 * 8);
+      x = __ldg(s);
+      y = __ldg(s + 1);
+    }
+    uint32_t w[4][2];
+    split2<2>(x.x, x.y, w[0]);
+    split2<2>(x.z, x.w, w[1]);
+    split2<2>(y.x, y.y, w[2]);
+    split2<2>(y.z, y.w, w[3]);
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+      asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(t.base + q * Tile<C8, 2>::kPlane + i * 16),
+                   "r"(w[0][q]), "r"(w[1][q]), "r"(w[2][q]), "r"(w[3][q]) : "memory");
+  }
+}
+
+// One accumulator pair into a tile of the workspace: block (r8, c8), 128 bytes a warp.
+template <int C8, int P>
+__device__ __forceinline__ void store_block(char* tile, int r8, int c8, float x, float y) {
+  uint32_t w[P];
+  split2<P>(x, y, w);
+#pragma unroll
+  for (int p = 0; p < P; ++p)
+    *reinterpret_cast<uint32_t*>(tile + p * (8 * C8 * 128) + (r8 * C8 + c8) * 128 + (threadIdx.x & 31) * 4) = w[p];
+}
+// The same, transposed: the accumulator's rows become the tile's columns.
+template <int C8, int P>
+__device__ __forceinline__ void store_block_t(char* tile, int r8, int c8, float x, float y) {
+  uint32_t w[P];
+  split2<P>(x, y, w);
+#pragma unroll
+  for (int p = 0; p < P; ++p)
+    *reinterpret_cast<uint32_t*>(tile + p * (8 * C8 * 128) + (r8 * C8 + c8) * 128 + (threadIdx.x & 31) * 4) =
+        transpose8(w[p]);
+}
+
+__device__ __forceinline__ void store_pair(__nv_bfloat16* p, float x, float y) {
+  *reinterpret_cast<uint32_t*>(p) = pack2(x, y);
+}
+__device__ __forceinline__ void store_pair(float* p, float x, float y) {
+  *reinterpret_cast<float2*>(p) = make_float2(x, y);
+}
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ void store_one(float* p, float x) { *p = x; }
+__device__ __forceinline__ void store_one(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
+
+// The problem as the kernels see it. Chunks of a row are counted from its first
+// real step. Slot s = 64 c + i of a row with `len` real steps is step
+// L - len + s when s < len, else the padding step s - len (when s < L).
+struct Problem {
+  int64_t B, L, n;  // n: chunks of a full row
+  int Hk, Hv, Dv;
+  int64_t ldq, ldk, ldv;
+  float scale;
+  const int32_t* lengths;
+  // workspace
+  float* gates;  // per chunk: kGates
+  char *W, *U, *S, *T, *dU, *dS;
+  float *pq, *pk;  // per value head gradients of q and k, when heads are shared
+};
+
+// One chunk of one head.
+struct Where {
+  int64_t b, nc;  // batch row; chunk number over everything
+  int h, hk;
+  int64_t c, len, first;  // chunk of the row, the row's real steps, the step of the chunk's first slot
+  int rows;               // real steps in the chunk (may be <= 0)
+};
+__device__ __forceinline__ int64_t row_length(const Problem& P, int64_t b) {
+  if (P.lengths == nullptr) return P.L;
+  const int64_t n = P.lengths[b];
+  return n < 0 ? 0 : n > P.L ? P.L : n;
+}
+__device__ __forceinline__ Where locate(const Problem& P, int64_t bh, int64_t c) {
+  Where w;
+  w.b = bh / P.Hv;
+  w.h = (int)(bh % P.Hv);
+  w.hk = w.h / (P.Hv / P.Hk);
+  w.c = c;
+  w.nc = bh * P.n + c;
+  w.len = row_length(P, w.b);
+  w.first = P.L - w.len + c * kC;
+  const int64_t left = w.len - c * kC;
+  w.rows = (int)(left < kC ? left : kC);
+  return w;
+}
+// The padding step that slot i of the chunk stands for, or -1.
+__device__ __forceinline__ int64_t padding_step(const Problem& P, const Where& w, int i) {
+  const int64_t s = w.c * kC + i;
+  return s >= w.len && s < P.L ? s - w.len : -1;
+}
+
+}  // namespace gdr
+}  // namespace blr

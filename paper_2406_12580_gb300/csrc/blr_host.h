@@ -1,0 +1,37 @@
+// Host-side checks and error text shared by the library's C entry points.
+#pragma once
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include <cuda_runtime.h>
+
+#include "blr.h"
+
+namespace blr {
+
+// Records the text of blr_last_error_string() and returns `s`.
+blr_status fail(blr_status s, const char* fmt, ...);
+blr_status cuda_check(cudaError_t e, const char* what);
+
+inline bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
+
+inline blr_status need(const void* p, const char* name, size_t align) {
+  if (p == nullptr) return fail(BLR_ERR_INVALID_ARG, "%s is NULL", name);
+  if (!aligned(p, align)) return fail(BLR_ERR_INVALID_ARG, "%s is not %zu-byte aligned", name, align);
+  return BLR_OK;
+}
+
+inline blr_status optional(const void* p, const char* name, size_t align) {
+  if (p != nullptr && !aligned(p, align))
+    return fail(BLR_ERR_INVALID_ARG, "%s is not %zu-byte aligned", name, align);
+  return BLR_OK;
+}
+
+#define BLR_TRY(expr)                  \
+  do {                                 \
+    blr_status s_ = (expr);            \
+    if (s_ != BLR_OK) return s_;       \
+  } while (0)
+
+}  // namespace blr

@@ -1,0 +1,78 @@
+"""AdamW for a whole model in few launches (``blr_adamw_step``), moments in float32 or in 8 bits."""
+from __future__ import annotations
+
+import torch
+
+from . import blr_adamw_step
+
+
+class AdamW(torch.optim.Optimizer):
+    """torch.optim.AdamW's update on the library's kernel.
+
+    bits=8 keeps the moments in 8 bits: float8 e4m3 codes with a float32 scale per 256 values
+    (the second moment as its root), a quarter of the float32 states' memory. Parameters are
+    float32 or bfloat16; master=True keeps float32 weights beside bfloat16 parameters. grad_scale
+    of step(): a float32 CUDA tensor of one value that every gradient is multiplied by (a clipping
+    or unscaling factor, read on the device)."""
+
+    def __init__(self, params, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8,
+                 weight_decay: float = 1e-2, bits: int = 32, master: bool = False):
+        if bits not in (8, 32):
+            raise ValueError("bits is 8 or 32")
+        super().__init__(params, dict(lr=lr, betas=betas, eps=eps, weight_decay=weight_decay, bits=bits,
+                                      master=master))
+
+    def _init(self, p, group):
+        state = self.state[p]
+        state["step"] = 0
+        moment = torch.float32 if group["bits"] == 32 else torch.float8_e4m3fn
+        for name in ("m", "v"):
+            state[name] = torch.zeros(p.shape, dtype=torch.float32, device=p.device).to(moment)
+            if group["bits"] == 8:
+                state[name + "_scale"] = torch.zeros(-(-p.numel() // 256), device=p.device)
+        if group["master"] and p.dtype == torch.bfloat16:
+            state["w"] = p.detach().float().contiguous()
+
+    def load_state_dict(self, state_dict):
+        """torch's, but the states keep their own dtypes (torch casts them to the parameter's)."""
+        super().load_state_dict(state_dict)
+        saved = state_dict["state"]
+        order = [p for group in self.param_groups for p in group["params"]]
+        numbers = [i for group in state_dict["param_groups"] for i in group["params"]]
+        for number, p in zip(numbers, order):
+            for name, value in saved.get(number, {}).items():
+                if torch.is_tensor(value):
+                    self.state[p][name] = value.to(device=p.device).clone()
+
+    @torch.no_grad()
+    def step(self, closure=None, grad_scale=None):
+        loss = None
+        if closure is not None:
+            with torch.enable_grad():
+                loss = closure()
+        for group in self.param_groups:
+            calls = {}
+            for p in group["params"]:
+                if p.grad is None:
+                    continue
+                if p.grad.is_sparse:
+                    raise ValueError("sparse gradients are not supported")
+                if not self.state[p]:
+                    self._init(p, group)
+                self.state[p]["step"] += 1
+                calls.setdefault((p.device, p.dtype, self.state[p]["step"]), []).append(p)
+            for (device, _, step), ps in calls.items():
+                states = [self.state[p] for p in ps]
+
+                def column(name):
+                    return [s[name] for s in states] if name in states[0] else None
+
+                with torch.cuda.device(device):
+                    blr_adamw_step(ps, [p.grad.contiguous() for p in ps], column("m"), column("v"), lr=group["lr"],
+                                   step=step, beta1=group["betas"][0], beta2=group["betas"][1], eps=group["eps"],
+                                   weight_decay=group["weight_decay"], masters=column("w"),
+                                   m_scales=column("m_scale"), v_scales=column("v_scale"), grad_scale=grad_scale)
+        return loss
+
+
+__all__ = ["AdamW"]

@@ -1,0 +1,145 @@
+"""CPU: the gated delta rule's and the AdamW step's entry points size their workspace and refuse bad
+arguments on the host, before anything reaches a GPU; and the float64 statement that the GPU tests
+compare with has the gradients of its own differences."""
+import ctypes
+
+import pytest
+
+from paper_2406_12580_gb300 import _lib
+from paper_2406_12580_gb300 import build as blr_build
+
+FAKE = 0x7f0000000000  # 256-byte aligned address, never dereferenced
+INVALID, UNSUPPORTED = _lib.BLR_ERR_INVALID_ARG, _lib.BLR_ERR_UNSUPPORTED
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if blr_build.stale():
+        blr_build.build()
+    return _lib.load()
+
+
+def desc(B=2, L=100, Hk=1, Hv=2, Dk=64, Dv=128, ldq=0, ldk=0, ldv=0, io=0, scale=1.0):
+    return _lib.blr_gdr_desc(B, L, Hk, Hv, Dk, Dv, ldq, ldk, ldv, io, scale)
+
+
+def fwd(lib, d, flags=2, ws_bytes=None, **kw):
+    a = dict(lengths=None, q=FAKE, k=FAKE, v=FAKE, g=FAKE, beta=FAKE, s0=None, o=FAKE, s_last=None, ws=FAKE)
+    a.update(kw)
+    size = lib.blr_gdr_workspace_bytes(ctypes.byref(d), flags) if ws_bytes is None else ws_bytes
+    return lib.blr_gdr_fwd(ctypes.byref(d), flags, *a.values(), size, None)
+
+
+def bwd(lib, d, flags=3, **kw):
+    a = dict(lengths=None, d_o=FAKE, ds_last=None, q=FAKE, k=FAKE, v=FAKE, g=FAKE, beta=FAKE, s0=None, dq=FAKE,
+             dk=FAKE, dv=FAKE, dg=FAKE, dbeta=FAKE, ds0=None, ws=FAKE)
+    a.update(kw)
+    size = lib.blr_gdr_workspace_bytes(ctypes.byref(d), flags)
+    return lib.blr_gdr_bwd(ctypes.byref(d), flags, *a.values(), size, None)
+
+
+def steps(lib, d, state=0, **kw):
+    a = dict(s_prev=FAKE, q=FAKE, k=FAKE, v=FAKE, g=FAKE, beta=FAKE, s_out=FAKE, o=FAKE)
+    a.update(kw)
+    return lib.blr_gdr_steps(ctypes.byref(d), state, *a.values(), None)
+
+
+BAD = [(dict(B=-1), INVALID), (dict(Hv=3, Hk=2), INVALID), (dict(Hk=0), INVALID), (dict(io=7), INVALID),
+       (dict(scale=float("nan")), INVALID), (dict(ldq=56), INVALID), (dict(ldv=260), INVALID),
+       (dict(Dk=32), UNSUPPORTED), (dict(Dv=96), UNSUPPORTED), (dict(Dv=320), UNSUPPORTED),
+       (dict(L=1 << 31), UNSUPPORTED)]
+
+
+@pytest.mark.parametrize("bad,status", BAD, ids=[str(b[0]) for b in BAD])
+def test_refused_descriptions(lib, bad, status):
+    d = desc(**bad)
+    assert fwd(lib, d, ws_bytes=1 << 60) == status and bwd(lib, d) == status and steps(lib, d) == status
+    assert lib.blr_last_error_string()
+    assert lib.blr_gdr_workspace_bytes(ctypes.byref(d), 0) == 0
+
+
+@pytest.mark.parametrize("name", ["q", "k", "v", "g", "beta", "o", "ws"])
+def test_refused_pointers(lib, name):
+    assert fwd(lib, desc(), **{name: None}) == INVALID
+    assert fwd(lib, desc(), **{name: FAKE + 2}) == INVALID
+
+
+def test_refused_calls(lib):
+    d = desc()
+    assert fwd(lib, d, flags=8) == INVALID
+    assert fwd(lib, d, flags=0, s0=FAKE) == INVALID and fwd(lib, d, flags=1, s_last=FAKE) == INVALID
+    assert fwd(lib, d, ws_bytes=lib.blr_gdr_workspace_bytes(ctypes.byref(d), 2) - 1) == INVALID
+    assert bwd(lib, d, flags=2) == INVALID and bwd(lib, d, flags=1, ds0=FAKE) == INVALID
+    for name in ("d_o", "dq", "dk", "dv", "dg", "dbeta"):
+        assert bwd(lib, d, **{name: None}) == INVALID
+    assert steps(lib, d, state=3) == INVALID and steps(lib, d, s_out=None) == INVALID
+    assert steps(lib, d, q=None) == INVALID
+
+
+def test_workspace_sizes(lib):
+    size = lambda d, f: lib.blr_gdr_workspace_bytes(ctypes.byref(d), f)  # noqa: E731
+    assert size(desc(L=0), 0) == 0 and size(desc(B=0), 0) == 0
+    plain, train = size(desc(io=1), 0), size(desc(io=1), 1)
+    assert 0 < plain < train < size(desc(io=1), 3)
+    assert size(desc(L=128, io=1), 0) == size(desc(L=65, io=1), 0) < size(desc(L=129, io=1), 0)
+
+
+class Tensor(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("p", "g", "m", "v", "w", "m_scale", "v_scale")] + [("n", ctypes.c_int64)]
+
+
+def adamw(lib, records, io=0, bits=32, lr=1e-3, beta1=0.9, beta2=0.99, eps=1e-8, wd=0.0, step=1, count=None):
+    table = (Tensor * max(1, len(records)))(*[Tensor(*r) for r in records])
+    return lib.blr_adamw_step(len(records) if count is None else count, ctypes.cast(table, ctypes.c_void_p), io, bits,
+                              lr, beta1, beta2, eps, wd, step, None, None)
+
+
+def test_adamw_refusals(lib):
+    one = (FAKE, FAKE, FAKE, FAKE, None, None, None, 10)
+    assert adamw(lib, []) == _lib.BLR_OK
+    assert adamw(lib, [(None,) * 7 + (0,)]) == _lib.BLR_OK
+    for bad in (dict(io=5), dict(bits=16), dict(lr=float("inf")), dict(beta1=1.0), dict(beta2=-0.1), dict(eps=0.0),
+                dict(step=0), dict(count=-1), dict(bits=8)):
+        assert adamw(lib, [one], **bad) == INVALID, bad
+    assert adamw(lib, [one[:7] + (-1,)]) == INVALID
+    assert adamw(lib, [(FAKE + 2,) + one[1:]]) == INVALID
+    for i in range(4):
+        assert adamw(lib, [one[:i] + (None,) + one[i + 1:]]) == INVALID
+    with_master = one[:4] + (FAKE,) + one[5:]
+    assert adamw(lib, [with_master]) == INVALID  # float32 parameters have none
+    assert adamw(lib, [with_master, one], io=1) == INVALID
+
+
+def test_the_statement_against_differences():
+    torch = pytest.importorskip("torch")
+    from delta_common import make, reference
+    d = make(2, 5, 1, 2, 4, 3, torch.float64, seed=1, state=True, lengths=[5, 3])
+    want = reference(d)
+
+    def loss(c):
+        r = reference(c, backward=False)
+        return float((r["o"] * d["do"]).sum() + (r["s"] * d["ds"].double()).sum())
+
+    for name in ("q", "k", "v", "g", "beta"):
+        e = torch.randn(d[name].shape, generator=torch.Generator().manual_seed(2), dtype=torch.float64)
+        h = 1e-5
+        slope = (loss({**d, name: d[name] + h * e}) - loss({**d, name: d[name] - h * e})) / (2 * h)
+        assert abs(slope - float((want["d" + name] * e).sum())) <= 1e-7 * (1 + abs(slope)), name
+
+
+def test_the_chunked_form_equals_the_recurrence():
+    """The chunk's formulas (the triangular inverse, the state's recursion) in float64, against the steps."""
+    torch = pytest.importorskip("torch")
+    from delta_common import make, off, reference
+    d = make(1, 12, 1, 1, 6, 5, torch.float64, seed=3, state=True)
+    want = reference(d, backward=False)
+    S, outs = d["s0"][0, 0].double(), []
+    for a in range(0, 12, 4):
+        q, k, v = (d[n][0, a:a + 4, 0] for n in ("q", "k", "v"))
+        G, beta = d["g"][0, a:a + 4, 0].cumsum(0), d["beta"][0, a:a + 4, 0]
+        D = torch.exp(G[:, None] - G[None, :]).tril()
+        T = torch.linalg.inv(torch.eye(4, dtype=torch.float64) + (beta[:, None] * D * (k @ k.T)).tril(-1))
+        U = T @ (beta[:, None] * v) - T @ ((beta * G.exp())[:, None] * k) @ S
+        outs.append(d["scale"] * (G.exp()[:, None] * (q @ S) + (D * (q @ k.T)) @ U))
+        S = G[-1].exp() * S + (k * (G[-1] - G).exp()[:, None]).T @ U
+    assert off(torch.cat(outs)[None, :, None], want["o"]) <= 1e-6 and off(S[None, None], want["s"]) <= 1e-6

@@ -1,0 +1,153 @@
+"""GPU: the AdamW step over many tensors against float64, with float32 and 8-bit moments."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+if not torch.cuda.is_available():  # collected on CPU machines, but never run there
+    pytest.skip("no CUDA device", allow_module_level=True)
+
+from paper_2406_12580_gb300 import blr_adamw_step  # noqa: E402
+
+SIZES = [1, 7, 8, 255, 256, 257, 4095, 4096, 4097, 20000, 3, 0, 64 * 33]
+HYPER = dict(lr=3e-3, beta1=0.9, beta2=0.99, eps=1e-7, weight_decay=0.1)
+
+
+def tensors(sizes, io, bits, master, seed=0, offset=0):
+    gen = torch.Generator().manual_seed(seed)
+
+    def place(x, dtype):  # a view `offset` values into a buffer of its own
+        flat = torch.zeros(x.numel() + offset, dtype=dtype, device="cuda")
+        flat[offset:].copy_(x.to(dtype))
+        return flat[offset:]
+
+    t = {n: [] for n in ("p", "g", "m", "v", "w", "ms", "vs")}
+    for n in sizes:
+        x = torch.randn(4, n, generator=gen)
+        size = 10.0 ** (4 * torch.rand(n, generator=gen) - 5)
+        w, g, m, r = x[0] * 0.1, x[1] * size, 0.3 * x[2] * size, (0.5 + x[3].abs()) * size
+        w, g, m, r = (y.float() for y in (w, g, m, r))
+        t["w"].append(place(w, torch.float32))
+        t["p"].append(place(w, io))
+        t["g"].append(place(g, io))
+        if bits == 32:
+            t["m"].append(place(m, torch.float32))
+            t["v"].append(place(r * r, torch.float32))
+        else:
+            for name, y in (("m", m), ("v", r)):
+                pad = torch.nn.functional.pad(y, (0, -n % 256)).view(-1, 256)
+                scale = pad.abs().amax(1) / 448.0
+                codes = (pad / scale.clamp(min=1e-30)[:, None]).view(-1)[:n].to(torch.float8_e4m3fn)
+                t[name].append(place(codes.view(torch.uint8), torch.uint8).view(torch.float8_e4m3fn))
+                t[name + "s"].append(scale.cuda())
+    return t
+
+
+def call(t, bits, master, step, grad_scale=None):
+    blr_adamw_step(t["p"], t["g"], t["m"], t["v"], masters=t["w"] if master else None,
+                   m_scales=t["ms"] if bits == 8 else None, v_scales=t["vs"] if bits == 8 else None, step=step,
+                   grad_scale=grad_scale, **HYPER)
+
+
+def wanted(t, i, bits, master, step, grad_scale=1.0):
+    """w, m, v (the root with 8 bits) of tensor i after the step, float64."""
+    h = HYPER
+    w = (t["w"] if master else t["p"])[i].double().cpu()
+    g, n = t["g"][i].double().cpu() * grad_scale, t["g"][i].numel()
+    if bits == 32:
+        m, v = t["m"][i].double().cpu(), t["v"][i].double().cpu()
+    else:
+        at = torch.arange(n) // 256
+        m = t["m"][i].float().double().cpu() * t["ms"][i].double().cpu()[at]
+        v = (t["v"][i].float().double().cpu() * t["vs"][i].double().cpu()[at]) ** 2
+    m, v = h["beta1"] * m + (1 - h["beta1"]) * g, h["beta2"] * v + (1 - h["beta2"]) * g * g
+    update = (m / (1 - h["beta1"] ** step)) / ((v / (1 - h["beta2"] ** step)).sqrt() + h["eps"])
+    return w * (1 - h["lr"] * h["weight_decay"]) - h["lr"] * update, m, v if bits == 32 else v.sqrt()
+
+
+@pytest.mark.parametrize("offset", [0, 1, 8])
+@pytest.mark.parametrize("io,master", [(torch.float32, False), (torch.bfloat16, False), (torch.bfloat16, True)],
+                         ids=["f32", "bf16", "master"])
+@pytest.mark.parametrize("bits", [32, 8])
+def test_step(bits, io, master, offset):
+    t = tensors(SIZES, io, bits, master, offset=offset)
+    step, scale = 3, 0.5
+    want = [wanted(t, i, bits, master, step, scale) for i in range(len(SIZES))]
+    call(t, bits, master, step, torch.tensor([scale], device="cuda"))
+    for i, n in enumerate(SIZES):
+        if n == 0:
+            continue
+        w, m, v = want[i]
+        got = t["w" if master else "p"][i].double().cpu()
+        # a handful of float32 roundings of values no larger than w + lr update: 8 of 2^-24
+        size = w.abs() + HYPER["lr"] * 10.0
+        assert ((got - w).abs() <= (2.0 ** -21 if io == torch.float32 or master else 2.0 ** -8) * size).all()
+        if master:
+            assert torch.equal(t["p"][i], t["w"][i].bfloat16())
+        if bits == 32:
+            assert torch.allclose(t["m"][i].double().cpu(), m, rtol=2.0 ** -21, atol=2.0 ** -22 * float(m.abs().max()))
+            assert torch.allclose(t["v"][i].double().cpu(), v, rtol=2.0 ** -21, atol=0)
+            continue
+        at = torch.arange(n) // 256
+        for name, x in (("m", m), ("v", v)):
+            top = torch.zeros(-(-n // 256), dtype=torch.float64).scatter_reduce(0, at, x.abs(), "amax")
+            scales = t[name + "s"][i].double().cpu()
+            assert torch.allclose(scales, top / 448.0, rtol=2.0 ** -20, atol=1e-40)
+            back = t[name][i].float().double().cpu() * scales[at]
+            # e4m3: half a unit of 3 mantissa bits, or of the smallest code; a root is lifted to that code
+            tiny = 2.0 ** -9 * top[at] / 448.0
+            assert ((back - x).abs() <= 2.0 ** -4 * x.abs() * 1.001 + (0.501 if name == "m" else 1.001) * tiny).all()
+            assert name == "m" or (back[x > 0] > 0).all()
+
+
+@pytest.mark.parametrize("count", [1, 32, 33, 449, 1000])
+def test_many_tensors(count):
+    sizes = [1 + (37 * i) % 700 for i in range(count)]
+    t = tensors(sizes, torch.float32, 32, False, seed=5)
+    want = [wanted(t, i, 32, False, 1)[0] for i in range(count)]
+    call(t, 32, False, 1)
+    got = torch.cat([x.double().cpu() for x in t["p"]])
+    assert torch.allclose(got, torch.cat(want), rtol=2.0 ** -21, atol=2.0 ** -21 * HYPER["lr"] * 10)
+
+
+def test_nothing_beside_the_tensors_is_written():
+    buffers = {n: torch.full((1000,), 7.0, device="cuda") for n in "pgmv"}
+    views = {n: b[300:701] for n, b in buffers.items()}
+    blr_adamw_step([views["p"]], [views["g"]], [views["m"]], [views["v"]], lr=1e-2, step=1)
+    for n in "pmv":
+        assert (buffers[n][:300] == 7.0).all() and (buffers[n][701:] == 7.0).all() and (views[n] != 7.0).all()
+
+
+def test_follows_torch_over_steps():
+    """Twenty steps beside torch's own optimizer in float64."""
+    torch.manual_seed(3)
+    p = [torch.randn(50, 7, device="cuda"), torch.randn(11, device="cuda")]
+    ref = [x.double().clone().requires_grad_(True) for x in p]
+    opt = torch.optim.AdamW(ref, lr=HYPER["lr"], betas=(HYPER["beta1"], HYPER["beta2"]), eps=HYPER["eps"],
+                            weight_decay=HYPER["weight_decay"])
+    m, v = [torch.zeros_like(x) for x in p], [torch.zeros_like(x) for x in p]
+    for step in range(1, 21):
+        g = [torch.randn_like(x) for x in p]
+        for r, x in zip(ref, g):
+            r.grad = x.double()
+        opt.step()
+        blr_adamw_step(p, g, m, v, step=step, **HYPER)
+    for x, r in zip(p, ref):
+        assert float((x.double() - r.detach()).norm() / r.detach().norm()) <= 20 * 2.0 ** -22
+
+
+def test_refusals():
+    x = [torch.zeros(10, device="cuda")]
+    with pytest.raises(ValueError):
+        blr_adamw_step(x, [torch.zeros(9, device="cuda")], x, x, lr=1e-3, step=1)
+    with pytest.raises(ValueError):
+        blr_adamw_step(x, [torch.zeros(10)], x, x, lr=1e-3, step=1)
+    with pytest.raises(ValueError):
+        blr_adamw_step(x, [torch.zeros(20, device="cuda")[::2]], x, x, lr=1e-3, step=1)
+    with pytest.raises(ValueError):
+        blr_adamw_step(x, x, [y.to(torch.float8_e4m3fn) for y in x], [y.to(torch.float8_e4m3fn) for y in x], lr=1e-3, step=1)
+    for bad in (dict(lr=math.nan, step=1), dict(lr=1e-3, step=0), dict(lr=1e-3, step=1, beta1=1.0), dict(lr=1e-3, step=1, eps=0.0)):
+        with pytest.raises(RuntimeError):
+            blr_adamw_step(x, x, x, x, **bad)
