@@ -375,11 +375,12 @@ BLR_API blr_status blr_selftest_wait_timeout(const blr_desc* desc, void* ws, siz
  *          (values outside [0, L] are clamped). The padding before them is never
  *          read; o and the gradients are zero there. s_last of an empty row is
  *          its s0.
- * Precision  Sums, decays and states are float32. With io == BLR_F32, or with
- *          BLR_GDR_STATE (a float32 state goes in or out), or with fewer than 16
- *          steps, every operand of a matrix product is carried as two bfloat16 terms (16 significant
- *          bits). Without, products round their operands to bfloat16, as the
- *          bfloat16 inputs are.
+ * Precision  Sums, decays and states are float32. With io == BLR_F32 every operand
+ *          of a matrix product is carried in float32 (two tf32 terms). With
+ *          bfloat16 and BLR_GDR_STATE (a float32 state goes in or out), or with
+ *          fewer than 16 steps, what is computed is carried as two bfloat16
+ *          terms (16 significant bits); else products round their operands to
+ *          bfloat16, as the inputs are.
  * Checks, streams, errors: as above; q, k, v, o, states and gradients 16-byte
  *          aligned (ldq, ldk, ldv multiples of 8), the others to their element.
  */

@@ -27,7 +27,7 @@ blr_status make_layout(const blr_gdr_desc* d, int flags, const GdrSizes& s, Layo
   l->n = (s.L + kC - 1) / kC;
   l->nc = s.B * s.Hv * l->n;
   // One block a chunk; a state's columns and a tensor's offsets are counted in 64 bits.
-  if (l->nc >= 0x7fffffff || s.B * s.Hv * (s.Dv / 64) >= 0x7fffffff)
+  if (l->nc >= 0x7fffffff || s.B * s.Hv * (s.Dv / 32) >= 0x7fffffff)
     return fail(BLR_ERR_UNSUPPORTED, "too many chunks (%lld)", (long long)l->nc);
   l->np = d->io == BLR_F32 || (flags & BLR_GDR_STATE) || s.L < kFewSteps ? 2 : 1;
   const size_t tile = (size_t)l->nc * l->np * 64 * 2;  // bytes per column of a tile
@@ -60,10 +60,11 @@ Problem make_problem(const blr_gdr_desc* d, const GdrSizes& s, const Layout& l, 
   Problem p;
   p.B = s.B;
   p.L = s.L;
-  p.n = l.n;
+  p.n = (int)l.n;
   p.Hk = (int)s.Hk;
   p.Hv = (int)s.Hv;
   p.Dv = (int)s.Dv;
+  p.group = (int)(s.Hv / s.Hk);
   p.ldq = s.ldq;
   p.ldk = s.ldk;
   p.ldv = s.ldv;

@@ -27,14 +27,14 @@ __global__ void __launch_bounds__(128)
 du_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k, const TI* __restrict__ d_o) {
   extern __shared__ __align__(128) unsigned char smem[];
   using L = DuSmem<DK, NI>;
-  const Where w = locate(P, blockIdx.x / P.n, blockIdx.x % P.n);
+  const Where w = locate(P);
   if (w.rows <= 0) return;
   const uint32_t base = smem_u32(smem);
   const Tile<DK / 8, NI> tq{base}, tk{base + L::kQ};
   const Tile<8, NI> to{base + 2 * L::kQ};
   float* G = reinterpret_cast<float*>(smem + 2 * L::kQ + L::kO);
   const int tid = threadIdx.x, warp = tid >> 5, l = tid & 31;
-  const int64_t row0 = w.b * P.L + w.first, ldo = (int64_t)P.Hv * P.Dv;
+  const int64_t row0 = w.step, ldo = (int64_t)P.Hv * P.Dv;
   const TI* src = d_o + row0 * ldo + (int64_t)w.h * P.Dv;
   load_rows(tq, q + row0 * P.ldq + w.hk * DK, P.ldq, w.rows, tid, 128);
   load_rows(tk, k + row0 * P.ldk + w.hk * DK, P.ldk, w.rows, tid, 128);
@@ -44,17 +44,17 @@ du_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k, c
   cp_async_wait<0>();
   __syncthreads();
   const int r0 = 16 * warp + (l >> 2), c0 = 2 * (l & 3);
-  uint32_t p[4][NM][4];  // scale P^T: rows j (this warp's), columns i >= j
+  uint32_t p[4][kPl<NM>][4];  // scale P^T: rows j (this warp's), columns i >= j
   {
     float acc[8][4] = {};
 #pragma unroll
     for (int kk = 0; kk < DK / 16; ++kk) {
-      uint32_t a[NI][4];
+      uint32_t a[kPl<NI>][4];
       tk.a(2 * warp, 2 * kk, a);
 #pragma unroll
       for (int nn = 0; nn < 4; ++nn)
         if (nn >= warp) {
-          uint32_t b[2][NI][2];
+          uint32_t b[2][kPl<NI>][2];
           tq.b_t(2 * nn, 2 * kk, b);
           mma_p<NI, NI>(acc[2 * nn], a, b[0]);
           mma_p<NI, NI>(acc[2 * nn + 1], a, b[1]);
@@ -85,7 +85,7 @@ du_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k, c
       if (kk >= warp) {
 #pragma unroll
         for (int nn = 0; nn < 4; ++nn) {
-          uint32_t b[2][NI][2];
+          uint32_t b[2][kPl<NI>][2];
           to.b(2 * nn, 2 * kk, b);
           mma_p<NM, NI>(acc[2 * nn], p[kk], b[0]);
           mma_p<NM, NI>(acc[2 * nn + 1], p[kk], b[1]);
@@ -100,147 +100,184 @@ du_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k, c
   }
 }
 
-template <int DK, int NI, int NM>
+template <int DK, int NI, int NM, int WARPS>
 struct BackSmem {
-  static constexpr int kW = Tile<DK / 8, NM>::kBytes, kK = Tile<DK / 8, NI>::kBytes, kO = Tile<8, NI>::kBytes,
-                       kU = Tile<8, NM>::kBytes;
+  static constexpr int kW = Tile<DK / 8, NM>::kBytes, kK = Tile<DK / 8, NI>::kBytes, kO = Tile<2 * WARPS, NI>::kBytes,
+                       kU = Tile<2 * WARPS, NM>::kBytes;
   static constexpr int kStage = kW + 2 * kK + kO + kU + kGates * 4;
-  static constexpr int kStages = 2 * kStage <= 227 * 1024 ? 2 : 1;
+  static constexpr int kStages = WARPS == 2 && 3 * kStage <= 227 * 1024 ? 3 : 2;
   static constexpr int kBytes = kStages * kStage;
 };
 
 // The states' gradients from chunk to chunk, last to first: as chain_kernel, a warp holds dS^T of 16
-// columns in accumulators.
-template <typename TI, int DK, int NI, int NM>
-__global__ void __launch_bounds__(128)
+// columns in accumulators, and two more warps load.
+template <typename TI, int DK, int NI, int NM, int WARPS>
+__global__ void __launch_bounds__(32 * (WARPS + kLoadWarps))
 back_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k, const TI* __restrict__ d_o,
             const float* __restrict__ ds_last, float* __restrict__ ds0) {
   extern __shared__ __align__(128) unsigned char smem[];
-  using L = BackSmem<DK, NI, NM>;
-  const int dvb = P.Dv / 64;
-  const int64_t bh = blockIdx.x / dvb;
-  const int part = blockIdx.x % dvb;
-  const int tid = threadIdx.x, warp = tid >> 5, l = tid & 31;
-  const int64_t chunks = (locate(P, bh, 0).len + kC - 1) / kC;
-  const int col = 64 * part + 16 * warp + (l >> 2), row = 2 * (l & 3);
-  const int64_t ldo = (int64_t)P.Hv * P.Dv;
+  using L = BackSmem<DK, NI, NM, WARPS>;
+  const int parts = P.Dv / (16 * WARPS), dvb = P.Dv / 64;
+  const uint32_t bh = blockIdx.x / parts;
+  const int part = blockIdx.x - bh * parts;
+  const int warp = threadIdx.x >> 5, l = threadIdx.x & 31;
+  const Where w0 = locate(P, bh, 0);
+  const int chunks = (int)((w0.len + kC - 1) / kC);
+  const int block = part * WARPS / 4, c8 = 2 * ((part * WARPS) & 3);
+  if (warp >= WARPS) {  // loads
+    const int tid = threadIdx.x - 32 * WARPS;
+    const int64_t ldo = (int64_t)P.Hv * P.Dv;
+    const auto load = [&](int c) {
+      if (c >= 0) {
+        const uint32_t st = smem_u32(smem) + (uint32_t)(c % L::kStages) * L::kStage;
+        const int64_t nc = w0.nc + c, left = w0.len - (int64_t)c * kC, row0 = w0.step + (int64_t)c * kC;
+        const int rows = (int)(left < kC ? left : kC);
+        copy_ws(st, P.W + nc * L::kW, L::kW, tid, 32 * kLoadWarps);
+        load_rows(Tile<DK / 8, NI>{st + L::kW}, k + row0 * P.ldk + w0.hk * DK, P.ldk, rows, tid, 32 * kLoadWarps);
+        load_rows(Tile<DK / 8, NI>{st + L::kW + L::kK}, q + row0 * P.ldq + w0.hk * DK, P.ldq, rows, tid, 32 * kLoadWarps);
+        load_rows(Tile<2 * WARPS, NI>{st + L::kW + 2 * L::kK},
+                  d_o + row0 * ldo + (int64_t)w0.h * P.Dv + 16 * WARPS * part, ldo, rows, tid, 32 * kLoadWarps);
+        copy_columns(Tile<2 * WARPS, NM>{st + L::kW + 2 * L::kK + L::kO},
+                     P.dU + (nc * dvb + block) * Tile<8, NM>::kBytes, c8, tid, 32 * kLoadWarps);
+        copy_ws(st + L::kW + 2 * L::kK + L::kO + L::kU, P.gates + nc * kGates, 1024, tid, 32 * kLoadWarps);
+      }
+      cp_async_commit();
+    };
+#pragma unroll
+    for (int i = 0; i < L::kStages - 1; ++i) load(chunks - 1 - i);
+    for (int c = chunks - 1; c >= 0; --c) {
+      cp_async_wait<L::kStages - 2>();
+      __syncthreads();
+      load(c - (L::kStages - 1));
+    }
+    return;
+  }
+  const int col = 16 * (part * WARPS + warp) + (l >> 2), row = 2 * (l & 3);
   float S[DK / 8][4];
 #pragma unroll
   for (int nb = 0; nb < DK / 8; ++nb)
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      S[nb][e] = ds_last == nullptr ? 0.0f : ds_last[(bh * DK + 8 * nb + row + (e & 1)) * P.Dv + col + 8 * (e >> 1)];
-  const auto load = [&](int64_t c) {
-    if (c >= 0) {
-      const Where w = locate(P, bh, c);
-      const uint32_t st = smem_u32(smem) + (uint32_t)(c % L::kStages) * L::kStage;
-      const int64_t row0 = w.b * P.L + w.first;
-      copy_ws(st, P.W + w.nc * L::kW, L::kW, tid, 128);
-      load_rows(Tile<DK / 8, NI>{st + L::kW}, k + row0 * P.ldk + w.hk * DK, P.ldk, w.rows, tid, 128);
-      load_rows(Tile<DK / 8, NI>{st + L::kW + L::kK}, q + row0 * P.ldq + w.hk * DK, P.ldq, w.rows, tid, 128);
-      load_rows(Tile<8, NI>{st + L::kW + 2 * L::kK}, d_o + row0 * ldo + (int64_t)w.h * P.Dv + 64 * part, ldo, w.rows,
-                tid, 128);
-      copy_ws(st + L::kW + 2 * L::kK + L::kO, P.dU + (w.nc * dvb + part) * L::kU, L::kU, tid, 128);
-      copy_ws(st + L::kW + 2 * L::kK + L::kO + L::kU, P.gates + w.nc * kGates, 4 * kGateFloats<NM>, tid, 128);
-    }
-    cp_async_commit();
-  };
-  for (int i = 0; i < L::kStages - 1; ++i) load(chunks - 1 - i);
-  for (int64_t c = chunks - 1; c >= 0; --c) {
-    load(c - (L::kStages - 1));
-    cp_async_wait<L::kStages - 1>();
+      S[nb][e] = ds_last == nullptr
+                     ? 0.0f
+                     : ds_last[((int64_t)bh * DK + 8 * nb + row + (e & 1)) * P.Dv + col + 8 * (e >> 1)];
+  for (int c = chunks - 1; c >= 0; --c) {
     __syncthreads();
-    const int s = (int)(c % L::kStages);
+    const int s = c % L::kStages;
     const uint32_t st = smem_u32(smem) + s * L::kStage;
     const Tile<DK / 8, NM> tw{st};
     const Tile<DK / 8, NI> tk{st + L::kW}, tq{st + L::kW + L::kK};
-    const Tile<8, NI> to{st + L::kW + 2 * L::kK};
-    const Tile<8, NM> tu{st + L::kW + 2 * L::kK + L::kO};
+    const Tile<2 * WARPS, NI> to{st + L::kW + 2 * L::kK};
+    const Tile<2 * WARPS, NM> tu{st + L::kW + 2 * L::kK + L::kO};
     const float* G = reinterpret_cast<const float*>(smem + s * L::kStage + L::kW + 2 * L::kK + L::kO + L::kU);
-    const int64_t nc = bh * P.n + c;
+    const int64_t tile = (w0.nc + c) * dvb + block;
     // K dS': columns are the chunk's steps
     float u[8][4] = {};
-    char* so = P.dS + (nc * dvb + part) * Tile<DK / 8, NM>::kBytes;
+    char* so = P.dS + tile * Tile<DK / 8, NM>::kBytes + (c8 + 2 * warp) * (DK / 8) * 128 + l * 4;
+    pipelined<DK / 16, 4, NI>(
+        [&](int kk, auto& b) {
 #pragma unroll
-    for (int kk = 0; kk < DK / 16; ++kk) {
-      uint32_t a[NM][4];
-      to_a<NM>(S[2 * kk], S[2 * kk + 1], a);
+          for (int nn = 0; nn < 4; ++nn) tk.b_t(2 * nn, 2 * kk, b[nn]);
+        },
+        [&](int kk, auto& b) {
+          uint32_t a[kPl<NM>][4];
+          to_a<NM>(S[2 * kk], S[2 * kk + 1], a);
 #pragma unroll
-      for (int p = 0; p < NM; ++p)
+          for (int p = 0; p < kPl<NM>; ++p)
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          *reinterpret_cast<uint32_t*>(so + p * Tile<DK / 8, NM>::kPlane +
-                                       ((2 * warp + (e & 1)) * (DK / 8) + 2 * kk + (e >> 1)) * 128 + l * 4) = a[p][e];
+            for (int e = 0; e < 4; ++e)
+              *reinterpret_cast<uint32_t*>(so + p * Tile<DK / 8, NM>::kPlane +
+                                           ((e & 1) * (DK / 8) + 2 * kk + (e >> 1)) * 128) = a[p][e];
 #pragma unroll
-      for (int nn = 0; nn < 4; ++nn) {
-        uint32_t b[2][NI][2];
-        tk.b_t(2 * nn, 2 * kk, b);
-        mma_p<NM, NI>(u[2 * nn], a, b[0]);
-        mma_p<NM, NI>(u[2 * nn + 1], a, b[1]);
-      }
-    }
-    const float decay = exp_p<NM>(G[63]);
+          for (int nn = 0; nn < 4; ++nn) {
+            mma_p<NM, NI>(u[2 * nn], a, b[nn][0]);
+            mma_p<NM, NI>(u[2 * nn + 1], a, b[nn][1]);
+          }
+        });
+    const float decay = G[kUp + 63];
 #pragma unroll
     for (int nb = 0; nb < DK / 8; ++nb)
 #pragma unroll
       for (int e = 0; e < 4; ++e) S[nb][e] *= decay;
-    char* uo = P.dU + (nc * dvb + part) * L::kU;
+    // scale (diag(gamma) Q)^T dO: dO^T as left operands, scaled by their steps
+    pipelined<4 * (DK / 64), 4, NI>(
+        [&](int s, auto& b) {
+          const int kk = s / (DK / 64), n0 = 8 * (s % (DK / 64));
 #pragma unroll
-    for (int kk = 0; kk < 4; ++kk) {
-      // this chunk's dU^T, 16 steps of it: the decayed sum and the part computed before
-      uint32_t f[2][NM][2];
-      const int i = l >> 3;
+          for (int nn = 0; nn < 4; ++nn) tq.b(n0 + 2 * nn, 2 * kk, b[nn]);
+        },
+        [&](int s, auto& b) {
+          const int kk = s / (DK / 64), n0 = 8 * (s % (DK / 64));
+          uint32_t fo[kPl<NI>][4], a[kPl<NM>][4];
+          to.a_t(2 * warp, 2 * kk, fo);
 #pragma unroll
-      for (int p = 0; p < NM; ++p)
-        ldsm_t(tu.at(p, 2 * kk + (i >> 1), 2 * warp + (i & 1)) + (l & 7) * 16, f[0][p][0], f[0][p][1], f[1][p][0],
-               f[1][p][1]);
-      // dO^T of these steps, scaled by scale gamma
-      uint32_t fo[NI][4], ao[NM][4];
-      to.a_t(2 * warp, 2 * kk, fo);
+          for (int h = 0; h < 2; ++h) {
+            const float2 up = *reinterpret_cast<const float2*>(&G[kUp + 16 * kk + 8 * h + row]);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const float2 gg = *reinterpret_cast<const float2*>(&G[16 * kk + 8 * h + row]);
-        const float e0 = decay_between<NM>(G, 63, 16 * kk + 8 * h + row);
-        const float e1 = decay_between<NM>(G, 63, 16 * kk + 8 * h + row + 1);
-        const float y0 = P.scale * exp_p<NM>(gg.x), y1 = P.scale * exp_p<NM>(gg.y);
+            for (int e = 0; e < 2; ++e) {
+              uint32_t x[kPl<NI>], y[kPl<NM>];
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          uint32_t x[NM], xo[NI], yo[NM];
+              for (int p = 0; p < kPl<NI>; ++p) x[p] = fo[p][2 * h + e];
+              const float2 v = join2<NI>(x);
+              split2<NM>(P.scale * up.x * v.x, P.scale * up.y * v.y, y);
 #pragma unroll
-          for (int p = 0; p < NM; ++p) x[p] = f[h][p][e];
-          const float2 v = join2<NM>(x);
-          u[2 * kk + h][2 * e] = fmaf(u[2 * kk + h][2 * e], e0, v.x);
-          u[2 * kk + h][2 * e + 1] = fmaf(u[2 * kk + h][2 * e + 1], e1, v.y);
-          store_block_t<8, NM>(uo, 2 * kk + h, 2 * warp + e, u[2 * kk + h][2 * e], u[2 * kk + h][2 * e + 1]);
+              for (int p = 0; p < kPl<NM>; ++p) a[p][2 * h + e] = y[p];
+            }
+          }
 #pragma unroll
-          for (int p = 0; p < NI; ++p) xo[p] = fo[p][2 * h + e];
-          const float2 ov = join2<NI>(xo);
-          split2<NM>(ov.x * y0, ov.y * y1, yo);
+          for (int nn = 0; nn < 4; ++nn) {
+            mma_p<NM, NI>(S[n0 + 2 * nn], a, b[nn][0]);
+            mma_p<NM, NI>(S[n0 + 2 * nn + 1], a, b[nn][1]);
+          }
+        });
+    // this chunk's dU^T: the decayed sum and the part computed before; then -W^T dU
+    char* uo = P.dU + tile * Tile<8, NM>::kBytes;
+    uint32_t a[kPl<NM>][4];
+    pipelined<4 * (DK / 64), 4, NM>(
+        [&](int s, auto& b) {
+          const int kk = s / (DK / 64), n0 = 8 * (s % (DK / 64));
 #pragma unroll
-          for (int p = 0; p < NM; ++p) ao[p][2 * h + e] = yo[p];
-        }
-      }
-      uint32_t a[NM][4];
-      to_a<NM>(u[2 * kk], u[2 * kk + 1], a);
+          for (int nn = 0; nn < 4; ++nn) tw.b(n0 + 2 * nn, 2 * kk, b[nn]);  // holds -W
+        },
+        [&](int s, auto& b) {
+          const int kk = s / (DK / 64), n0 = 8 * (s % (DK / 64));
+          if (n0 == 0) {
+            uint32_t f[2][kPl<NM>][2];
+            const int i = l >> 3;
 #pragma unroll
-      for (int nn = 0; nn < DK / 16; ++nn) {
-        uint32_t b[2][NM][2], bq[2][NI][2];
-        tw.b(2 * nn, 2 * kk, b);  // holds -W
-        tq.b(2 * nn, 2 * kk, bq);
-        mma_p<NM, NM>(S[2 * nn], a, b[0]);
-        mma_p<NM, NM>(S[2 * nn + 1], a, b[1]);
-        mma_p<NM, NI>(S[2 * nn], ao, bq[0]);
-        mma_p<NM, NI>(S[2 * nn + 1], ao, bq[1]);
-      }
-    }
-    __syncthreads();
+            for (int p = 0; p < kPl<NM>; ++p)
+              ldsm_t(tu.at(p, 2 * kk + (i >> 1), 2 * warp + (i & 1)) + (l & 7) * 16, f[0][p][0], f[0][p][1],
+                     f[1][p][0], f[1][p][1]);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const float2 down = *reinterpret_cast<const float2*>(&G[kDown + 16 * kk + 8 * h + row]);
+              float(&y)[4] = u[2 * kk + h];
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                uint32_t x[kPl<NM>];
+#pragma unroll
+                for (int p = 0; p < kPl<NM>; ++p) x[p] = f[h][p][e];
+                const float2 v = join2<NM>(x);
+                y[2 * e] = fmaf(y[2 * e], down.x, v.x);
+                y[2 * e + 1] = fmaf(y[2 * e + 1], down.y, v.y);
+                store_block_t<8, NM>(uo, 2 * kk + h, c8 + 2 * warp + e, y[2 * e], y[2 * e + 1]);
+              }
+            }
+            to_a<NM>(u[2 * kk], u[2 * kk + 1], a);
+          }
+#pragma unroll
+          for (int nn = 0; nn < 4; ++nn) {
+            mma_p<NM, NM>(S[n0 + 2 * nn], a, b[nn][0]);
+            mma_p<NM, NM>(S[n0 + 2 * nn + 1], a, b[nn][1]);
+          }
+        });
   }
   if (ds0 != nullptr) {
 #pragma unroll
     for (int nb = 0; nb < DK / 8; ++nb)
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        ds0[(bh * DK + 8 * nb + row + (e & 1)) * P.Dv + col + 8 * (e >> 1)] = S[nb][e];
+        ds0[((int64_t)bh * DK + 8 * nb + row + (e & 1)) * P.Dv + col + 8 * (e >> 1)] = S[nb][e];
   }
 }
 
@@ -269,7 +306,7 @@ grad_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k,
   extern __shared__ __align__(128) unsigned char smem[];
   using L = GradSmem<DK, NI, NM>;
   constexpr int NB = DK / 16;  // 8-column blocks in a warp's half of Dk
-  const Where w = locate(P, blockIdx.x / P.n, blockIdx.x % P.n);
+  const Where w = locate(P);
   const int tid = threadIdx.x, warp = tid >> 5, l = tid & 31, rg = warp & 3, hf = warp >> 2;
   const int64_t hq = heads == P.Hk ? w.hk : w.h;
   if (w.rows < kC && w.len < P.L) {
@@ -300,7 +337,7 @@ grad_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k,
   float* rows = G + kGates;         // [half][5][64]: dbeta without S, x1.q, x2.k, x3.k, row sums less none
   float* cols = rows + 2 * 5 * 64;  // [rg][64]
   float* dots = cols + 4 * 64;   // per warp: part of <S, dS'>
-  const int64_t row0 = w.b * P.L + w.first, ldo = (int64_t)P.Hv * P.Dv;
+  const int64_t row0 = w.step, ldo = (int64_t)P.Hv * P.Dv;
   const int dvb = P.Dv / 64;
   load_rows(tq, q + row0 * P.ldq + w.hk * DK, P.ldq, w.rows, tid, 256);
   load_rows(tk, k + row0 * P.ldk + w.hk * DK, P.ldk, w.rows, tid, 256);
@@ -326,11 +363,11 @@ grad_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k,
 #pragma unroll
       for (int kk = 0; kk < 4; ++kk)
         if (kk >= rg) {
-          uint32_t a[NM][4];
+          uint32_t a[kPl<NM>][4];
           tt.a_t(2 * rg, 2 * kk, a);
 #pragma unroll
           for (int nn = 0; nn < 2; ++nn) {
-            uint32_t b[2][NM][2];
+            uint32_t b[2][kPl<NM>][2];
             tdu.b(4 * hf + 2 * nn, 2 * kk, b);
             mma_p<NM, NM>(r[2 * nn], a, b[0]);
             mma_p<NM, NM>(r[2 * nn + 1], a, b[1]);
@@ -354,9 +391,9 @@ grad_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k,
       }
     }
     for (int i = tid; i < Tile<DK / 8, NM>::kPlane / 4; i += 256) {
-      uint32_t a[NM], b[NM];
+      uint32_t a[kPl<NM>], b[kPl<NM>];
 #pragma unroll
-      for (int p = 0; p < NM; ++p) {
+      for (int p = 0; p < kPl<NM>; ++p) {
         asm volatile("ld.shared.b32 %0, [%1];" : "=r"(a[p]) : "r"(ts.base + p * Tile<DK / 8, NM>::kPlane + 4 * i));
         asm volatile("ld.shared.b32 %0, [%1];" : "=r"(b[p]) : "r"(tds.base + p * Tile<DK / 8, NM>::kPlane + 4 * i));
       }
@@ -366,13 +403,13 @@ grad_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k,
     __syncthreads();
 #pragma unroll
     for (int kk = 0; kk < 4; ++kk) {
-      uint32_t ao[NI][4], au[NM][4], ar[NM][4];
+      uint32_t ao[kPl<NI>][4], au[kPl<NM>][4], ar[kPl<NM>][4];
       to.a(2 * rg, 2 * kk, ao);
       tu.a(2 * rg, 2 * kk, au);
       tdu.a(2 * rg, 2 * kk, ar);
 #pragma unroll
       for (int nn = 0; nn < NB / 2; ++nn) {
-        uint32_t b[2][NM][2];
+        uint32_t b[2][kPl<NM>][2];
         ts.b(NB * hf + 2 * nn, 2 * kk, b);
         mma_p<NI, NM>(x1[2 * nn], ao, b[0]);
         mma_p<NI, NM>(x1[2 * nn + 1], ao, b[1]);
@@ -384,7 +421,7 @@ grad_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k,
       }
 #pragma unroll
       for (int nn = 0; nn < 2; ++nn) {
-        uint32_t b[2][NM][2];
+        uint32_t b[2][kPl<NM>][2];
         tu.b_t(4 * hf + 2 * nn, 2 * kk, b);
         mma_p<NI, NM>(dp[2 * nn], ao, b[0]);
         mma_p<NI, NM>(dp[2 * nn + 1], ao, b[1]);
@@ -398,12 +435,12 @@ grad_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k,
     float qk[4][4] = {}, kk_[4][4] = {};
 #pragma unroll
     for (int kk = 0; kk < DK / 16; ++kk) {
-      uint32_t aq[NI][4], ak[NI][4];
+      uint32_t aq[kPl<NI>][4], ak[kPl<NI>][4];
       tq.a(2 * rg, 2 * kk, aq);
       tk.a(2 * rg, 2 * kk, ak);
 #pragma unroll
       for (int nn = 0; nn < 2; ++nn) {
-        uint32_t b[2][NI][2];
+        uint32_t b[2][kPl<NI>][2];
         tk.b_t(4 * hf + 2 * nn, 2 * kk, b);
         mma_p<NI, NI>(qk[2 * nn], aq, b[0]);
         mma_p<NI, NI>(qk[2 * nn + 1], aq, b[1]);
@@ -470,7 +507,7 @@ grad_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k,
       float a[5];
 #pragma unroll
       for (int x = 0; x < 5; ++x) a[x] = rows[x * 64 + i] + rows[(5 + x) * 64 + i];
-      const float up = exp_p<NM>(G[i]), down = decay_between<NM>(G, 63, i);
+      const float up = G[kUp + i], down = G[kDown + i];
       const float col = (cols[i] + cols[64 + i]) + (cols[128 + i] + cols[192 + i]);
       dG[e] = P.scale * up * a[1] - bt[i] * up * a[3] - down * a[2] + a[4] - col;
       add += down * a[2];
@@ -479,7 +516,7 @@ grad_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k,
     const float all = ((dots[0] + dots[1]) + (dots[2] + dots[3])) + ((dots[4] + dots[5]) + (dots[6] + dots[7]));
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) add += __shfl_xor_sync(0xffffffffu, add, d);
-    if (l == 31) dG[1] += add + exp_p<NM>(G[63]) * all;
+    if (l == 31) dG[1] += add + G[kUp + 63] * all;
     float s = dG[0] + dG[1];
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -489,8 +526,7 @@ grad_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k,
     if (2 * l < w.rows) store_one(dg + (row0 + 2 * l) * P.Hv + w.h, s);
     if (2 * l + 1 < w.rows) store_one(dg + (row0 + 2 * l + 1) * P.Hv + w.h, s - dG[0]);
   }
-  const float up0 = exp_p<NM>(G[r0]), up1 = exp_p<NM>(G[r0 + 8]);
-  const float dn0 = decay_between<NM>(G, 63, r0), dn1 = decay_between<NM>(G, 63, r0 + 8);
+  const float up0 = G[kUp + r0], up1 = G[kUp + r0 + 8], dn0 = G[kDown + r0], dn1 = G[kDown + r0 + 8];
   const float b0 = bt[r0] * up0, b1 = bt[r0 + 8] * up1;
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb)
@@ -502,12 +538,12 @@ grad_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k,
 #pragma unroll
   for (int kk = 0; kk < 4; ++kk) {
     if (kk <= rg) {  // rows of scale dP o D and of M against K
-      uint32_t ap[NM][4], am[NM][4];
+      uint32_t ap[kPl<NM>][4], am[kPl<NM>][4];
       tu.a(2 * rg, 2 * kk, ap);
       tdu.a(2 * rg, 2 * kk, am);
 #pragma unroll
       for (int nn = 0; nn < NB / 2; ++nn) {
-        uint32_t b[2][NI][2];
+        uint32_t b[2][kPl<NI>][2];
         tk.b(NB * hf + 2 * nn, 2 * kk, b);
         mma_p<NM, NI>(x1[2 * nn], ap, b[0]);
         mma_p<NM, NI>(x1[2 * nn + 1], ap, b[1]);
@@ -516,12 +552,12 @@ grad_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k,
       }
     }
     if (kk >= rg) {  // their columns against Q and K
-      uint32_t ap[NM][4], am[NM][4];
+      uint32_t ap[kPl<NM>][4], am[kPl<NM>][4];
       tu.a_t(2 * rg, 2 * kk, ap);
       tdu.a_t(2 * rg, 2 * kk, am);
 #pragma unroll
       for (int nn = 0; nn < NB / 2; ++nn) {
-        uint32_t b[2][NI][2];
+        uint32_t b[2][kPl<NI>][2];
         tq.b(NB * hf + 2 * nn, 2 * kk, b);
         mma_p<NM, NI>(x2[2 * nn], ap, b[0]);
         mma_p<NM, NI>(x2[2 * nn + 1], ap, b[1]);

@@ -4,8 +4,8 @@
 namespace blr {
 namespace gdr {
 
-blr_status fwd_f32(const Problem& p, const FwdCall& c) { return fwd<float, 2, 2>(p, c); }
-blr_status bwd_f32(const Problem& p, const BwdCall& c) { return bwd<float, 2, 2>(p, c); }
+blr_status fwd_f32(const Problem& p, const FwdCall& c) { return fwd<float, 3, 3>(p, c); }
+blr_status bwd_f32(const Problem& p, const BwdCall& c) { return bwd<float, 3, 3>(p, c); }
 
 }  // namespace gdr
 }  // namespace blr

@@ -18,7 +18,7 @@ namespace gdr {
 template <int P, typename T>
 __device__ __forceinline__ void load_gates(const T* g, const T* beta, int64_t stride, int rows,
                                            float* out) {  // by one warp; `out`: kGates floats
-  using Sum = typename std::conditional<P == 2, double, float>::type;
+  using Sum = typename std::conditional<(P > 1), double, float>::type;
   const int l = threadIdx.x & 31;
   const Sum x = 2 * l < rows ? fmaxf(to_float(g[2 * l * stride]), kMinDecay) : 0.0f;
   const Sum y = 2 * l + 1 < rows ? fmaxf(to_float(g[(2 * l + 1) * stride]), kMinDecay) : 0.0f;
@@ -28,14 +28,15 @@ __device__ __forceinline__ void load_gates(const T* g, const T* beta, int64_t st
     const Sum o = __shfl_up_sync(0xffffffffu, s, d);
     if (l >= d) s += o;
   }
-  const Sum first = s - y;
-  out[2 * l] = (float)first;
-  out[2 * l + 1] = (float)s;
-  out[64 + 2 * l] = 2 * l < rows ? to_float(beta[2 * l * stride]) : 0.0f;
-  out[64 + 2 * l + 1] = 2 * l + 1 < rows ? to_float(beta[(2 * l + 1) * stride]) : 0.0f;
-  if constexpr (P == 2) {
-    out[128 + 2 * l] = (float)(first - (Sum)(float)first);
-    out[128 + 2 * l + 1] = (float)(s - (Sum)(float)s);
+  const Sum G[2] = {s - y, s}, last = __shfl_sync(0xffffffffu, s, 31);
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const int i = 2 * l + e;
+    out[i] = (float)G[e];
+    out[kBeta + i] = i < rows ? to_float(beta[i * stride]) : 0.0f;
+    out[kUp + i] = exp_p<P>((float)G[e]);
+    out[kDown + i] = exp_p<P>((float)(last - G[e]));
+    if constexpr (P > 1) out[kRest + i] = (float)(G[e] - (Sum)(float)G[e]);
   }
 }
 
@@ -43,7 +44,7 @@ constexpr int kLd = 68;  // row stride of float32 squares in shared memory: frag
 
 // Block column J of T^-1's lower triangle from the inverses of the diagonal blocks (already in `inv`):
 // T_iJ = -T_ii sum_{J <= m < i} A_im T_mJ, kept transposed so that an accumulator is the next left operand.
-template <int J>
+template <int J, int P>
 __device__ __forceinline__ void inverse_column(const float* A, float* inv) {
   const int l = threadIdx.x & 31, r = l >> 2, c = 2 * (l & 3);
   float t[4][2][4];  // T_mJ^T, m = J..3: 16 x 16 as two column blocks
@@ -52,16 +53,16 @@ __device__ __forceinline__ void inverse_column(const float* A, float* inv) {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       t[J][nb][e] = inv[(16 * J + 8 * nb + c + (e & 1)) * kLd + 16 * J + r + 8 * (e >> 1)];
-  auto right = [&](const float* m, int row0, int col0, uint32_t (&b)[2][2][2]) {  // of m^T's block
+  auto right = [&](const float* m, int row0, int col0, uint32_t (&b)[2][kPl<P>][2]) {  // of m^T's block
 #pragma unroll
     for (int nb = 0; nb < 2; ++nb)
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) {
         const float2 v = *reinterpret_cast<const float2*>(&m[(row0 + 8 * nb + r) * kLd + col0 + 8 * kb + c]);
-        uint32_t w[2];
-        split2<2>(v.x, v.y, w);
-        b[nb][0][kb] = w[0];
-        b[nb][1][kb] = w[1];
+        uint32_t w[kPl<P>];
+        split2<P>(v.x, v.y, w);
+#pragma unroll
+        for (int p = 0; p < kPl<P>; ++p) b[nb][p][kb] = w[p];
       }
   };
 #pragma unroll
@@ -69,13 +70,13 @@ __device__ __forceinline__ void inverse_column(const float* A, float* inv) {
     float s[2][4] = {};
 #pragma unroll
     for (int m = J; m < i; ++m) {
-      uint32_t a[2][4], b[2][2][2];
-      to_a<2>(t[m][0], t[m][1], a);
+      uint32_t a[kPl<P>][4], b[2][kPl<P>][2];
+      to_a<P>(t[m][0], t[m][1], a);
       right(A, 16 * i, 16 * m, b);
-      mma_p<2, 2>(s[0], a, b[0]);
-      mma_p<2, 2>(s[1], a, b[1]);
+      mma_p<P, P>(s[0], a, b[0]);
+      mma_p<P, P>(s[1], a, b[1]);
     }
-    uint32_t a[2][4], b[2][2][2];
+    uint32_t a[kPl<P>][4], b[2][kPl<P>][2];
 #pragma unroll
     for (int nb = 0; nb < 2; ++nb)
 #pragma unroll
@@ -83,10 +84,10 @@ __device__ __forceinline__ void inverse_column(const float* A, float* inv) {
         s[nb][e] = -s[nb][e];
         t[i][nb][e] = 0.0f;
       }
-    to_a<2>(s[0], s[1], a);
+    to_a<P>(s[0], s[1], a);
     right(inv, 16 * i, 16 * i, b);
-    mma_p<2, 2>(t[i][0], a, b[0]);
-    mma_p<2, 2>(t[i][1], a, b[1]);
+    mma_p<P, P>(t[i][0], a, b[0]);
+    mma_p<P, P>(t[i][1], a, b[1]);
 #pragma unroll
     for (int nb = 0; nb < 2; ++nb)
 #pragma unroll
@@ -104,7 +105,7 @@ struct PrepareSmem {
 
 // T, W = T diag(beta gamma) K (stored negated), U0 = T diag(beta) V of one chunk of one head. A warp
 // holds 16 rows of the chunk. The diagonal 16 x 16 blocks of T by substitution in float32, the rest by
-// two-plane products, so that T is exact to float32's last bits but two whatever K.
+// products of two planes at least, whatever the operands of the rest.
 template <typename TI, int DK, int NI, int NM, bool TRAIN>
 __global__ void __launch_bounds__(128)
 prepare_kernel(const Problem P, const TI* __restrict__ k, const TI* __restrict__ v, const TI* __restrict__ g,
@@ -117,10 +118,10 @@ prepare_kernel(const Problem P, const TI* __restrict__ k, const TI* __restrict__
   float* inv = A + 64 * kLd;
   float* sg = inv + 64 * kLd;  // the gates
   float* sb = sg + 64;
-  const Where w = locate(P, blockIdx.x / P.n, blockIdx.x % P.n);
+  const Where w = locate(P);
   if (w.rows <= 0) return;
   const int tid = threadIdx.x, warp = tid >> 5, l = tid & 31;
-  const int64_t row0 = w.b * P.L + w.first;
+  const int64_t row0 = w.step;
   load_rows(tk, k + row0 * P.ldk + w.hk * DK, P.ldk, w.rows, tid, 128);
   load_rows(tv, v + row0 * P.ldv + (int64_t)w.h * P.Dv, P.ldv, w.rows, tid, 128);
   cp_async_commit();
@@ -139,12 +140,12 @@ prepare_kernel(const Problem P, const TI* __restrict__ k, const TI* __restrict__
     float acc[8][4] = {};
 #pragma unroll
     for (int kk = 0; kk < DK / 16; ++kk) {
-      uint32_t a[NI][4];
+      uint32_t a[kPl<NI>][4];
       tk.a(2 * warp, 2 * kk, a);
 #pragma unroll
       for (int nn = 0; nn < 4; ++nn) {
         if (nn <= warp) {
-          uint32_t b[2][NI][2];
+          uint32_t b[2][kPl<NI>][2];
           tk.b_t(2 * nn, 2 * kk, b);
           mma_p<NI, NI>(acc[2 * nn], a, b[0]);
           mma_p<NI, NI>(acc[2 * nn + 1], a, b[1]);
@@ -180,12 +181,13 @@ prepare_kernel(const Problem P, const TI* __restrict__ k, const TI* __restrict__
     }
   }
   __syncthreads();
-  if (warp == 0) inverse_column<0>(A, inv);
-  else if (warp == 1) inverse_column<1>(A, inv);
-  else if (warp == 2) inverse_column<2>(A, inv);
+  constexpr int kInv = NM == 3 ? 3 : 2;
+  if (warp == 0) inverse_column<0, kInv>(A, inv);
+  else if (warp == 1) inverse_column<1, kInv>(A, inv);
+  else if (warp == 2) inverse_column<2, kInv>(A, inv);
   __syncthreads();
   // rows of T, scaled by column, as left operands
-  const auto rows_of_t = [&](int kk, const float* scale, uint32_t (&a)[NM][4]) {
+  const auto rows_of_t = [&](int kk, const float* scale, uint32_t (&a)[kPl<NM>][4]) {
     float x[2][4];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -223,11 +225,11 @@ prepare_kernel(const Problem P, const TI* __restrict__ k, const TI* __restrict__
 #pragma unroll
     for (int kk = 0; kk < 4; ++kk)
       if (kk <= warp) {
-        uint32_t a[NM][4];
+        uint32_t a[kPl<NM>][4];
         rows_of_t(kk, sb, a);
 #pragma unroll
         for (int nn = 0; nn < 4; ++nn) {
-          uint32_t b[2][NI][2];
+          uint32_t b[2][kPl<NI>][2];
           tv.b(2 * nn, 2 * kk, b);
           mma_p<NM, NI>(acc[2 * nn], a, b[0]);
           mma_p<NM, NI>(acc[2 * nn + 1], a, b[1]);
@@ -242,7 +244,7 @@ prepare_kernel(const Problem P, const TI* __restrict__ k, const TI* __restrict__
   }
   // -W: the column scale becomes -beta gamma
   __syncthreads();
-  if (tid < 64) sb[tid] *= -exp_p<NM>(sg[tid]);
+  if (tid < 64) sb[tid] *= -sg[kUp + tid];
   __syncthreads();
   char* wt = P.W + w.nc * Tile<DK / 8, NM>::kBytes;
 #pragma unroll
@@ -251,11 +253,11 @@ prepare_kernel(const Problem P, const TI* __restrict__ k, const TI* __restrict__
 #pragma unroll
     for (int kk = 0; kk < 4; ++kk)
       if (kk <= warp) {
-        uint32_t a[NM][4];
+        uint32_t a[kPl<NM>][4];
         rows_of_t(kk, sb, a);
 #pragma unroll
         for (int nn = 0; nn < 4; ++nn) {
-          uint32_t b[2][NI][2];
+          uint32_t b[2][kPl<NI>][2];
           tk.b(8 * half + 2 * nn, 2 * kk, b);
           mma_p<NM, NI>(acc[2 * nn], a, b[0]);
           mma_p<NM, NI>(acc[2 * nn + 1], a, b[1]);
@@ -269,139 +271,157 @@ prepare_kernel(const Problem P, const TI* __restrict__ k, const TI* __restrict__
   }
 }
 
-template <int DK, int NI, int NM>
+template <int DK, int NI, int NM, int WARPS>
 struct ChainSmem {
-  static constexpr int kW = Tile<DK / 8, NM>::kBytes, kK = Tile<DK / 8, NI>::kBytes, kU = Tile<8, NM>::kBytes;
+  static constexpr int kW = Tile<DK / 8, NM>::kBytes, kK = Tile<DK / 8, NI>::kBytes, kU = Tile<2 * WARPS, NM>::kBytes;
   static constexpr int kStage = kW + kK + kU + kGates * 4;
-  static constexpr int kStages = 2;
+  static constexpr int kStages = WARPS == 2 && 3 * kStage <= 227 * 1024 ? 3 : 2;
   static constexpr int kBytes = kStages * kStage;
 };
 
-// The states from chunk to chunk. A block takes 64 columns of a head's state, a warp 16 of them, as
+// The states from chunk to chunk. A block takes 16 WARPS columns of a head's state, a warp 16 of them, as
 // S^T (16 x Dk) in accumulators: U^T = U0^T + S^T (-W)^T and S'^T = gamma_C S^T + (U^T diag(e^{G_C - G})) K
 // take their left operands from registers, so the warps of a head never exchange anything; the block
-// shares only the tiles that it streams.
-template <typename TI, int DK, int NI, int NM>
-__global__ void __launch_bounds__(128)
+// shares only the tiles that it streams. Two more warps only load, kStages - 1 chunks ahead: one barrier a
+// chunk says both that a stage has arrived and that the one before it may be filled again.
+template <typename TI, int DK, int NI, int NM, int WARPS>
+__global__ void __launch_bounds__(32 * (WARPS + kLoadWarps))
 chain_kernel(const Problem P, const TI* __restrict__ k, const float* __restrict__ s0,
              float* __restrict__ s_last) {
   extern __shared__ __align__(128) unsigned char smem[];
-  using L = ChainSmem<DK, NI, NM>;
-  const int dvb = P.Dv / 64;
-  const int64_t bh = blockIdx.x / dvb;
-  const int part = blockIdx.x % dvb;
-  const int tid = threadIdx.x, warp = tid >> 5, l = tid & 31;
+  using L = ChainSmem<DK, NI, NM, WARPS>;
+  const int parts = P.Dv / (16 * WARPS), dvb = P.Dv / 64;
+  const uint32_t bh = blockIdx.x / parts;
+  const int part = blockIdx.x - bh * parts;
+  const int warp = threadIdx.x >> 5, l = threadIdx.x & 31;
   const Where w0 = locate(P, bh, 0);
-  const int64_t chunks = (w0.len + kC - 1) / kC;
-  const int col = 64 * part + 16 * warp + (l >> 2), row = 2 * (l & 3);  // of S (row + 8 nb, col (+ 8))
+  const int chunks = (int)((w0.len + kC - 1) / kC);
+  const int block = part * WARPS / 4, c8 = 2 * ((part * WARPS) & 3);  // this part's 64 columns, and where in them
+  if (warp >= WARPS) {  // loads
+    const int tid = threadIdx.x - 32 * WARPS;
+    const auto load = [&](int c) {
+      if (c < chunks) {
+        const uint32_t st = smem_u32(smem) + (uint32_t)(c % L::kStages) * L::kStage;
+        const int64_t nc = w0.nc + c, left = w0.len - (int64_t)c * kC;
+        copy_ws(st, P.W + nc * L::kW, L::kW, tid, 32 * kLoadWarps);
+        load_rows(Tile<DK / 8, NI>{st + L::kW}, k + (w0.step + (int64_t)c * kC) * P.ldk + w0.hk * DK, P.ldk,
+                  (int)(left < kC ? left : kC), tid, 32 * kLoadWarps);
+        copy_columns(Tile<2 * WARPS, NM>{st + L::kW + L::kK}, P.U + (nc * dvb + block) * Tile<8, NM>::kBytes, c8, tid,
+                     32 * kLoadWarps);
+        copy_ws(st + L::kW + L::kK + L::kU, P.gates + nc * kGates, 1024, tid, 32 * kLoadWarps);
+      }
+      cp_async_commit();
+    };
+#pragma unroll
+    for (int i = 0; i < L::kStages - 1; ++i) load(i);
+    for (int c = 0; c < chunks; ++c) {
+      cp_async_wait<L::kStages - 2>();
+      __syncthreads();
+      load(c + L::kStages - 1);
+    }
+    return;
+  }
+  const int col = 16 * (part * WARPS + warp) + (l >> 2), row = 2 * (l & 3);  // of S (row + 8 nb, col (+ 8))
   float S[DK / 8][4];
 #pragma unroll
   for (int nb = 0; nb < DK / 8; ++nb)
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      S[nb][e] = s0 == nullptr ? 0.0f : s0[(bh * DK + 8 * nb + row + (e & 1)) * P.Dv + col + 8 * (e >> 1)];
-  const auto load = [&](int64_t c) {
-    if (c < chunks) {
-      const Where w = locate(P, bh, c);
-      const uint32_t st = smem_u32(smem) + (uint32_t)(c % L::kStages) * L::kStage;
-      copy_ws(st, P.W + w.nc * L::kW, L::kW, tid, 128);
-      load_rows(Tile<DK / 8, NI>{st + L::kW}, k + (w.b * P.L + w.first) * P.ldk + w.hk * DK, P.ldk, w.rows, tid, 128);
-      copy_ws(st + L::kW + L::kK, P.U + (w.nc * dvb + part) * L::kU, L::kU, tid, 128);
-      copy_ws(st + L::kW + L::kK + L::kU, P.gates + w.nc * kGates, 4 * kGateFloats<NM>, tid, 128);
-    }
-    cp_async_commit();
-  };
-  for (int i = 0; i < L::kStages - 1; ++i) load(i);
-  for (int64_t c = 0; c < chunks; ++c) {
-    load(c + L::kStages - 1);
-    cp_async_wait<L::kStages - 1>();
+      S[nb][e] = s0 == nullptr ? 0.0f : s0[((int64_t)bh * DK + 8 * nb + row + (e & 1)) * P.Dv + col + 8 * (e >> 1)];
+  for (int c = 0; c < chunks; ++c) {
     __syncthreads();
-    const int s = (int)(c % L::kStages);
+    const int s = c % L::kStages;
     const uint32_t st = smem_u32(smem) + s * L::kStage;
     const Tile<DK / 8, NM> tw{st};
     const Tile<DK / 8, NI> tk{st + L::kW};
-    const Tile<8, NM> tu{st + L::kW + L::kK};
+    const Tile<2 * WARPS, NM> tu{st + L::kW + L::kK};
     const float* G = reinterpret_cast<const float*>(smem + s * L::kStage + L::kW + L::kK + L::kU);
-    const int64_t nc = bh * P.n + c;
+    const int64_t tile = (w0.nc + c) * dvb + block;
     float u[8][4];
 #pragma unroll
     for (int nb = 0; nb < 8; nb += 2) {  // U0^T: blocks (tokens 8 nb, columns 16 warp), transposed
-      uint32_t f[2][NM][2];
+      uint32_t f[2][kPl<NM>][2];
       const int i = l >> 3;
 #pragma unroll
-      for (int p = 0; p < NM; ++p)
+      for (int p = 0; p < kPl<NM>; ++p)
         ldsm_t(tu.at(p, nb + (i >> 1), 2 * warp + (i & 1)) + (l & 7) * 16, f[0][p][0], f[0][p][1], f[1][p][0],
                f[1][p][1]);
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          uint32_t x[NM];
+          uint32_t x[kPl<NM>];
 #pragma unroll
-          for (int p = 0; p < NM; ++p) x[p] = f[h][p][e];
+          for (int p = 0; p < kPl<NM>; ++p) x[p] = f[h][p][e];
           const float2 v = join2<NM>(x);
           u[nb + h][2 * e] = v.x;
           u[nb + h][2 * e + 1] = v.y;
         }
     }
-    char* so = P.S + (nc * dvb + part) * Tile<DK / 8, NM>::kBytes;
+    // the state before the chunk goes out as it becomes an operand: blocks (columns 16 warp.., rows 16 kk..)
+    char* so = P.S + tile * Tile<DK / 8, NM>::kBytes + (c8 + 2 * warp) * (DK / 8) * 128 + l * 4;
+    pipelined<DK / 16, 4, NM>(
+        [&](int kk, auto& b) {
 #pragma unroll
-    for (int kk = 0; kk < DK / 16; ++kk) {
-      uint32_t a[NM][4];
-      to_a<NM>(S[2 * kk], S[2 * kk + 1], a);
-      // the state before the chunk: blocks (columns 16 warp.., rows 16 kk..) of S^T
+          for (int nn = 0; nn < 4; ++nn) tw.b_t(2 * nn, 2 * kk, b[nn]);
+        },
+        [&](int kk, auto& b) {
+          uint32_t a[kPl<NM>][4];
+          to_a<NM>(S[2 * kk], S[2 * kk + 1], a);
 #pragma unroll
-      for (int p = 0; p < NM; ++p)
+          for (int p = 0; p < kPl<NM>; ++p)
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          *reinterpret_cast<uint32_t*>(so + p * Tile<DK / 8, NM>::kPlane +
-                                       ((2 * warp + (e & 1)) * (DK / 8) + 2 * kk + (e >> 1)) * 128 + l * 4) = a[p][e];
+            for (int e = 0; e < 4; ++e)
+              *reinterpret_cast<uint32_t*>(so + p * Tile<DK / 8, NM>::kPlane +
+                                           ((e & 1) * (DK / 8) + 2 * kk + (e >> 1)) * 128) = a[p][e];
 #pragma unroll
-      for (int nn = 0; nn < 4; ++nn) {
-        uint32_t b[2][NM][2];
-        tw.b_t(2 * nn, 2 * kk, b);
-        mma_p<NM, NM>(u[2 * nn], a, b[0]);
-        mma_p<NM, NM>(u[2 * nn + 1], a, b[1]);
-      }
-    }
-    const float decay = exp_p<NM>(G[63]);
+          for (int nn = 0; nn < 4; ++nn) {
+            mma_p<NM, NM>(u[2 * nn], a, b[nn][0]);
+            mma_p<NM, NM>(u[2 * nn + 1], a, b[nn][1]);
+          }
+        });
+    const float decay = G[kUp + 63];
 #pragma unroll
     for (int nb = 0; nb < DK / 8; ++nb)
 #pragma unroll
       for (int e = 0; e < 4; ++e) S[nb][e] *= decay;
-    char* uo = P.U + (nc * dvb + part) * L::kU;
+    char* uo = P.U + tile * Tile<8, NM>::kBytes;
+    uint32_t a[kPl<NM>][4];
+    pipelined<4 * (DK / 64), 4, NI>(
+        [&](int s, auto& b) {
+          const int kk = s / (DK / 64), n0 = 8 * (s % (DK / 64));
 #pragma unroll
-    for (int kk = 0; kk < 4; ++kk) {
+          for (int nn = 0; nn < 4; ++nn) tk.b(n0 + 2 * nn, 2 * kk, b[nn]);
+        },
+        [&](int s, auto& b) {
+          const int kk = s / (DK / 64), n0 = 8 * (s % (DK / 64));
+          if (n0 == 0) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        float(&x)[4] = u[2 * kk + h];
-        store_block_t<8, NM>(uo, 2 * kk + h, 2 * warp, x[0], x[1]);
-        store_block_t<8, NM>(uo, 2 * kk + h, 2 * warp + 1, x[2], x[3]);
-        const int i = 16 * kk + 8 * h + row;
-        const float e0 = decay_between<NM>(G, 63, i), e1 = decay_between<NM>(G, 63, i + 1);
-        x[0] *= e0;
-        x[1] *= e1;
-        x[2] *= e0;
-        x[3] *= e1;
-      }
-      uint32_t a[NM][4];
-      to_a<NM>(u[2 * kk], u[2 * kk + 1], a);
+            for (int h = 0; h < 2; ++h) {
+              float(&x)[4] = u[2 * kk + h];
+              store_block_t<8, NM>(uo, 2 * kk + h, c8 + 2 * warp, x[0], x[1]);
+              store_block_t<8, NM>(uo, 2 * kk + h, c8 + 2 * warp + 1, x[2], x[3]);
+              const float2 down = *reinterpret_cast<const float2*>(&G[kDown + 16 * kk + 8 * h + row]);
+              x[0] *= down.x;
+              x[1] *= down.y;
+              x[2] *= down.x;
+              x[3] *= down.y;
+            }
+            to_a<NM>(u[2 * kk], u[2 * kk + 1], a);
+          }
 #pragma unroll
-      for (int nn = 0; nn < DK / 16; ++nn) {
-        uint32_t b[2][NI][2];
-        tk.b(2 * nn, 2 * kk, b);
-        mma_p<NM, NI>(S[2 * nn], a, b[0]);
-        mma_p<NM, NI>(S[2 * nn + 1], a, b[1]);
-      }
-    }
-    __syncthreads();
+          for (int nn = 0; nn < 4; ++nn) {
+            mma_p<NM, NI>(S[n0 + 2 * nn], a, b[nn][0]);
+            mma_p<NM, NI>(S[n0 + 2 * nn + 1], a, b[nn][1]);
+          }
+        });
   }
   if (s_last != nullptr) {
 #pragma unroll
     for (int nb = 0; nb < DK / 8; ++nb)
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        s_last[(bh * DK + 8 * nb + row + (e & 1)) * P.Dv + col + 8 * (e >> 1)] = S[nb][e];
+        s_last[((int64_t)bh * DK + 8 * nb + row + (e & 1)) * P.Dv + col + 8 * (e >> 1)] = S[nb][e];
   }
 }
 
@@ -417,7 +437,7 @@ __global__ void __launch_bounds__(128)
 output_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k, TI* __restrict__ o) {
   extern __shared__ __align__(128) unsigned char smem[];
   using L = OutputSmem<DK, NI, NM>;
-  const Where w = locate(P, blockIdx.x / P.n, blockIdx.x % P.n);
+  const Where w = locate(P);
   const int tid = threadIdx.x, warp = tid >> 5, l = tid & 31;
   if (w.rows < kC && w.len < P.L) {
     for (int i = tid; i < kC * (P.Dv / 2); i += 128) {
@@ -431,7 +451,7 @@ output_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ 
   const Tile<8, NM> tu{base + 2 * L::kQ};
   const Tile<DK / 8, NM> ts{base + 2 * L::kQ + L::kU};
   float* G = reinterpret_cast<float*>(smem + 2 * L::kQ + L::kU + L::kS);
-  const int64_t row0 = w.b * P.L + w.first;
+  const int64_t row0 = w.step;
   const int dvb = P.Dv / 64;
   load_rows(tq, q + row0 * P.ldq + w.hk * DK, P.ldq, w.rows, tid, 128);
   load_rows(tk, k + row0 * P.ldk + w.hk * DK, P.ldk, w.rows, tid, 128);
@@ -446,17 +466,17 @@ output_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ 
   cp_async_wait<1>();
   __syncthreads();
   const int r = l >> 2, c0 = 2 * (l & 3), r0 = 16 * warp + r;
-  uint32_t p[4][NM][4];  // P, as left operands
+  uint32_t p[4][kPl<NM>][4];  // P, as left operands
   {
     float acc[8][4] = {};
 #pragma unroll
     for (int kk = 0; kk < DK / 16; ++kk) {
-      uint32_t a[NI][4];
+      uint32_t a[kPl<NI>][4];
       tq.a(2 * warp, 2 * kk, a);
 #pragma unroll
       for (int nn = 0; nn < 4; ++nn)
         if (nn <= warp) {
-          uint32_t b[2][NI][2];
+          uint32_t b[2][kPl<NI>][2];
           tk.b_t(2 * nn, 2 * kk, b);
           mma_p<NI, NI>(acc[2 * nn], a, b[0]);
           mma_p<NI, NI>(acc[2 * nn + 1], a, b[1]);
@@ -472,7 +492,7 @@ output_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ 
 #pragma unroll
     for (int kk = 0; kk < 4; ++kk) to_a<NM>(acc[2 * kk], acc[2 * kk + 1], p[kk]);
   }
-  const float up0 = exp_p<NM>(G[r0]), up1 = exp_p<NM>(G[r0 + 8]);
+  const float up0 = G[kUp + r0], up1 = G[kUp + r0 + 8];
   for (int part = 0; part < dvb; ++part) {
     if (part > 0) {
       __syncthreads();
@@ -483,11 +503,11 @@ output_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ 
     float acc[8][4] = {};
 #pragma unroll
     for (int kk = 0; kk < DK / 16; ++kk) {
-      uint32_t a[NI][4];
+      uint32_t a[kPl<NI>][4];
       tq.a(2 * warp, 2 * kk, a);
 #pragma unroll
       for (int nn = 0; nn < 4; ++nn) {
-        uint32_t b[2][NM][2];
+        uint32_t b[2][kPl<NM>][2];
         ts.b_t(2 * nn, 2 * kk, b);
         mma_p<NI, NM>(acc[2 * nn], a, b[0]);
         mma_p<NI, NM>(acc[2 * nn + 1], a, b[1]);
@@ -505,7 +525,7 @@ output_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ 
       if (kk <= warp) {
 #pragma unroll
         for (int nn = 0; nn < 4; ++nn) {
-          uint32_t b[2][NM][2];
+          uint32_t b[2][kPl<NM>][2];
           tu.b(2 * nn, 2 * kk, b);
           mma_p<NM, NM>(acc[2 * nn], p[kk], b[0]);
           mma_p<NM, NM>(acc[2 * nn + 1], p[kk], b[1]);

@@ -18,6 +18,10 @@ blr_status start(const char* name, K kernel, int64_t blocks, int threads, int by
   return cuda_check(cudaGetLastError(), name);
 }
 
+// Whether the chains of states go 64 columns to a block: with fewer such blocks than SMs, 32 to a block
+// put each chain's warps on more of them (twice the loads of W and K, half the shared-memory reads of an SM).
+inline bool wide_chains(const Problem& p) { return p.B * p.Hv * (p.Dv / 64) > 152; }
+
 template <typename TI, int DK, int NI, int NM>
 blr_status fwd_dk(const Problem& p, const FwdCall& c) {
   const int64_t chunks = p.B * p.Hv * p.n;
@@ -25,8 +29,12 @@ blr_status fwd_dk(const Problem& p, const FwdCall& c) {
            *g = static_cast<const TI*>(c.g), *beta = static_cast<const TI*>(c.beta);
   BLR_TRY(start("prepare", c.train ? prepare_kernel<TI, DK, NI, NM, true> : prepare_kernel<TI, DK, NI, NM, false>,
                 chunks, 128, PrepareSmem<DK, NI, NM>::kBytes, c.stream, p, k, v, g, beta));
-  BLR_TRY(start("chain", chain_kernel<TI, DK, NI, NM>, p.B * p.Hv * (p.Dv / 64), 128, ChainSmem<DK, NI, NM>::kBytes,
-                c.stream, p, k, c.s0, c.s_last));
+  if (wide_chains(p))
+    BLR_TRY(start("chain", chain_kernel<TI, DK, NI, NM, 4>, p.B * p.Hv * (p.Dv / 64), 32 * (4 + kLoadWarps),
+                  ChainSmem<DK, NI, NM, 4>::kBytes, c.stream, p, k, c.s0, c.s_last));
+  else
+    BLR_TRY(start("chain", chain_kernel<TI, DK, NI, NM, 2>, p.B * p.Hv * (p.Dv / 32), 32 * (2 + kLoadWarps),
+                  ChainSmem<DK, NI, NM, 2>::kBytes, c.stream, p, k, c.s0, c.s_last));
   return start("output", output_kernel<TI, DK, NI, NM>, chunks, 128, OutputSmem<DK, NI, NM>::kBytes, c.stream, p, q, k,
                static_cast<TI*>(c.o));
 }
@@ -39,8 +47,14 @@ blr_status bwd_dk(const Problem& p, const BwdCall& c) {
   TI *dq = static_cast<TI*>(c.dq), *dk = static_cast<TI*>(c.dk_out), *dv = static_cast<TI*>(c.dv),
      *dg = static_cast<TI*>(c.dg), *dbeta = static_cast<TI*>(c.dbeta);
   BLR_TRY(start("du", du_kernel<TI, DK, NI, NM>, chunks, 128, DuSmem<DK, NI>::kBytes, c.stream, p, q, k, d_o));
-  BLR_TRY(start("back", back_kernel<TI, DK, NI, NM>, p.B * p.Hv * (p.Dv / 64), 128, BackSmem<DK, NI, NM>::kBytes,
-                c.stream, p, q, k, d_o, c.ds_last, c.ds0));
+  // two stages of float32 tiles and 64 columns do not fit beside each other
+  constexpr int kWide = 2 * BackSmem<DK, NI, NM, 4>::kStage <= 227 * 1024 ? 4 : 2;
+  if (wide_chains(p))
+    BLR_TRY(start("back", back_kernel<TI, DK, NI, NM, kWide>, p.B * p.Hv * (p.Dv / (16 * kWide)), 32 * (kWide + kLoadWarps),
+                  BackSmem<DK, NI, NM, kWide>::kBytes, c.stream, p, q, k, d_o, c.ds_last, c.ds0));
+  else
+    BLR_TRY(start("back", back_kernel<TI, DK, NI, NM, 2>, p.B * p.Hv * (p.Dv / 32), 32 * (2 + kLoadWarps),
+                  BackSmem<DK, NI, NM, 2>::kBytes, c.stream, p, q, k, d_o, c.ds_last, c.ds0));
   constexpr int bytes = GradSmem<DK, NI, NM>::kBytes;
   if (p.Hk == p.Hv)
     return start("grad", grad_kernel<TI, TI, DK, NI, NM>, chunks, 256, bytes, c.stream, p, q, k, v, d_o, dq, dk,

@@ -5,9 +5,13 @@
 // bytes, block rows one after the other: a fragment load reads whole blocks
 // (no bank conflicts, no padding, no swizzle), a register of an accumulator
 // tile is one block (a 128-byte store), and a tile of the workspace is copied
-// linearly. A matrix in float32 precision is carried as two planes of such
-// tiles, x = hi + lo with 16 significant bits together; a product of two such
-// operands is hi hi + lo hi + hi lo.
+// linearly. A matrix comes in one of three forms P:
+//   1  bfloat16;
+//   2  two bfloat16 planes, x = hi + lo with 16 significant bits together; a
+//      product of two such operands is hi hi + lo hi + hi lo;
+//   3  float32, its upper and its lower 16 bits in two planes (so that the same
+//      fragment loads, transposed ones too, move it); a product takes each
+//      operand apart into two tf32 terms of 11 bits, hi hi + lo hi + hi lo.
 //
 // The products use the warp-level m16n8k16 instruction: the recurrence over
 // chunks then stays in a warp's registers (an accumulator tile is, unchanged,
@@ -25,6 +29,7 @@ namespace blr {
 namespace gdr {
 
 constexpr int kC = 64;               // steps of a chunk
+constexpr int kLoadWarps = 2;        // warps of a chain kernel's block that only load
 constexpr float kMinDecay = -120.0f;  // exp(-120) is 0 in float32
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) {
@@ -38,14 +43,25 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {  // a in the low h
 __device__ __forceinline__ float lo_f(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float hi_f(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
-// Two values as P planes of packed pairs.
 template <int P>
-__device__ __forceinline__ void split2(float a, float b, uint32_t (&w)[P]) {
+constexpr int kPl = P == 1 ? 1 : 2;  // planes
+
+// Two values as packed pairs, one for each plane.
+template <int P>
+__device__ __forceinline__ void split2(float a, float b, uint32_t (&w)[kPl<P>]) {
+  if constexpr (P == 3) {
+    w[0] = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
+    w[1] = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x5410);
+    return;
+  }
   w[0] = pack2(a, b);
   if constexpr (P == 2) w[1] = pack2(a - lo_f(w[0]), b - hi_f(w[0]));
 }
 template <int P>
-__device__ __forceinline__ float2 join2(const uint32_t (&w)[P]) {
+__device__ __forceinline__ float2 join2(const uint32_t (&w)[kPl<P>]) {
+  if constexpr (P == 3)
+    return make_float2(__uint_as_float(__byte_perm(w[1], w[0], 0x5410)),
+                       __uint_as_float(__byte_perm(w[1], w[0], 0x7632)));
   float2 r = make_float2(lo_f(w[0]), hi_f(w[0]));
   if constexpr (P == 2) {
     r.x += lo_f(w[1]);
@@ -57,37 +73,74 @@ __device__ __forceinline__ float2 join2(const uint32_t (&w)[P]) {
 // exp of a value <= 0: to the last bits where operands have two planes.
 template <int P>
 __device__ __forceinline__ float exp_p(float x) {
-  if constexpr (P == 2) return expf(x);
+  if constexpr (P > 1) return expf(x);
   return __expf(x);
 }
 
-// A chunk's gates: its cumulative log decay (64), beta (64), and with two planes what the decay's
-// floats leave out (64).
-constexpr int kGates = 192;
+// A chunk's gates, 64 floats each: its cumulative log decay G, beta, e^G, e^{G_C - G}, and with two
+// planes what G's floats leave out.
+constexpr int kBeta = 64, kUp = 128, kDown = 192, kRest = 256;
+constexpr int kGates = 320;
 template <int P>
-constexpr int kGateFloats = P == 2 ? 192 : 128;
+constexpr int kGateFloats = P > 1 ? 320 : 256;
 
 // e^{G_i - G_j}, j <= i
 template <int P>
 __device__ __forceinline__ float decay_between(const float* G, int i, int j) {
   float d = G[i] - G[j];
-  if constexpr (P == 2) d += G[128 + i] - G[128 + j];
+  if constexpr (P > 1) d += G[kRest + i] - G[kRest + j];
   return exp_p<P>(d);
 }
 
 __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
       "{%0,%1,%2,%3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+__device__ __forceinline__ void mma_tf32(float (&d)[4], const uint32_t (&a)[4], const uint32_t (&b)[2]) {
+  asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
+}
+// x = hi + lo, hi rounded to tf32's bits (cut off instead, all products would err to one side), lo exact
+// before the product rounds it too.
+__device__ __forceinline__ void tf32_terms(float x, uint32_t& hi, uint32_t& lo) {
+  hi = (__float_as_uint(x) + 0x1000u) & 0xffffe000u;
+  lo = __float_as_uint(x - __uint_as_float(hi));
+}
+
 template <int PA, int PB>
-__device__ __forceinline__ void mma_p(float (&d)[4], const uint32_t (&a)[PA][4], const uint32_t (&b)[PB][2]) {
-  mma(d, a[0], b[0][0], b[0][1]);
-  if constexpr (PA == 2) mma(d, a[1], b[0][0], b[0][1]);
-  if constexpr (PB == 2) mma(d, a[0], b[1][0], b[1][1]);
+__device__ __forceinline__ void mma_p(float (&d)[4], const uint32_t (&a)[kPl<PA>][4], const uint32_t (&b)[kPl<PB>][2]) {
+  static_assert((PA == 3) == (PB == 3), "float32 operands meet float32 operands");
+  if constexpr (PA == 3) {
+    // A fragment register holds columns 2c, 2c + 1 of 8 (c = lane % 4); the tf32 product's slots c and
+    // c + 4 take them, in both operands.
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      uint32_t ah[4], al[4], bh[2], bl[2];
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const uint32_t w[2] = {a[0][2 * h + r], a[1][2 * h + r]};
+        const float2 v = join2<3>(w);
+        tf32_terms(v.x, ah[r], al[r]);
+        tf32_terms(v.y, ah[2 + r], al[2 + r]);
+      }
+      const uint32_t w[2] = {b[0][h], b[1][h]};
+      const float2 v = join2<3>(w);
+      tf32_terms(v.x, bh[0], bl[0]);
+      tf32_terms(v.y, bh[1], bl[1]);
+      mma_tf32(d, al, bh);
+      mma_tf32(d, ah, bl);
+      mma_tf32(d, ah, bh);
+    }
+    return;
+  } else {
+    mma(d, a[0], b[0][0], b[0][1]);
+    if constexpr (PA == 2) mma(d, a[1], b[0][0], b[0][1]);
+    if constexpr (PB == 2) mma(d, a[0], b[1][0], b[1][1]);
+  }
 }
 
 __device__ __forceinline__ void ldsm(uint32_t addr, uint32_t& r0, uint32_t& r1, uint32_t& r2, uint32_t& r3) {
@@ -100,7 +153,7 @@ __device__ __forceinline__ void ldsm_t(uint32_t addr, uint32_t& r0, uint32_t& r1
 }
 __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
   uint32_t y;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
 
@@ -108,52 +161,52 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
 template <int C8, int P>
 struct Tile {
   static constexpr int kPlane = 8 * C8 * 128;  // bytes
-  static constexpr int kBytes = P * kPlane;
+  static constexpr int kBytes = kPl<P> * kPlane;
   uint32_t base;
   __device__ __forceinline__ uint32_t at(int p, int r8, int c8) const {
     return base + p * kPlane + (r8 * C8 + c8) * 128;
   }
   // Left operand, rows 8 m8 .. + 16, columns 8 k8 .. + 16, of the tile.
-  __device__ __forceinline__ void a(int m8, int k8, uint32_t (&f)[P][4]) const {
+  __device__ __forceinline__ void a(int m8, int k8, uint32_t (&f)[kPl<P>][4]) const {
     const int l = threadIdx.x & 31, i = l >> 3;
 #pragma unroll
-    for (int p = 0; p < P; ++p)
+    for (int p = 0; p < kPl<P>; ++p)
       ldsm(at(p, m8 + (i & 1), k8 + (i >> 1)) + (l & 7) * 16, f[p][0], f[p][1], f[p][2], f[p][3]);
   }
   // Left operand of the transposed tile: rows 8 m8 .. are the tile's columns.
-  __device__ __forceinline__ void a_t(int m8, int k8, uint32_t (&f)[P][4]) const {
+  __device__ __forceinline__ void a_t(int m8, int k8, uint32_t (&f)[kPl<P>][4]) const {
     const int l = threadIdx.x & 31, i = l >> 3;
 #pragma unroll
-    for (int p = 0; p < P; ++p)
+    for (int p = 0; p < kPl<P>; ++p)
       ldsm_t(at(p, k8 + (i >> 1), m8 + (i & 1)) + (l & 7) * 16, f[p][0], f[p][1], f[p][2], f[p][3]);
   }
   // Right operands of two 8-column blocks n8, n8 + 1 of X^T, X this tile (its rows are the columns).
-  __device__ __forceinline__ void b_t(int n8, int k8, uint32_t (&f)[2][P][2]) const {
+  __device__ __forceinline__ void b_t(int n8, int k8, uint32_t (&f)[2][kPl<P>][2]) const {
     const int l = threadIdx.x & 31, i = l >> 3;
 #pragma unroll
-    for (int p = 0; p < P; ++p)
+    for (int p = 0; p < kPl<P>; ++p)
       ldsm(at(p, n8 + (i >> 1), k8 + (i & 1)) + (l & 7) * 16, f[0][p][0], f[0][p][1], f[1][p][0], f[1][p][1]);
   }
   // Right operands of two 8-column blocks of X, X this tile.
-  __device__ __forceinline__ void b(int n8, int k8, uint32_t (&f)[2][P][2]) const {
+  __device__ __forceinline__ void b(int n8, int k8, uint32_t (&f)[2][kPl<P>][2]) const {
     const int l = threadIdx.x & 31, i = l >> 3;
 #pragma unroll
-    for (int p = 0; p < P; ++p)
+    for (int p = 0; p < kPl<P>; ++p)
       ldsm_t(at(p, k8 + (i & 1), n8 + (i >> 1)) + (l & 7) * 16, f[0][p][0], f[0][p][1], f[1][p][0], f[1][p][1]);
   }
   // The pair of values (row 8 r8 + lane / 4, columns 8 c8 + 2 (lane % 4) + {0, 1}).
   __device__ __forceinline__ float2 pair(int r8, int c8) const {
-    uint32_t w[P];
+    uint32_t w[kPl<P>];
 #pragma unroll
-    for (int p = 0; p < P; ++p)
+    for (int p = 0; p < kPl<P>; ++p)
       asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[p]) : "r"(at(p, r8, c8) + (threadIdx.x & 31) * 4) : "memory");
     return join2<P>(w);
   }
   __device__ __forceinline__ void put(int r8, int c8, float x, float y) const {
-    uint32_t w[P];
+    uint32_t w[kPl<P>];
     split2<P>(x, y, w);
 #pragma unroll
-    for (int p = 0; p < P; ++p)
+    for (int p = 0; p < kPl<P>; ++p)
       asm volatile("st.shared.b32 [%0], %1;" ::"r"(at(p, r8, c8) + (threadIdx.x & 31) * 4), "r"(w[p]) : "memory");
   }
 };
@@ -161,20 +214,20 @@ struct Tile {
 // An accumulator tile (16 rows x 8 columns in d[0], d[1]: row lane / 4; d[2], d[3]: row + 8) as half
 // of a left operand: blocks (x, y) give its columns 0..7 and 8..15.
 template <int P>
-__device__ __forceinline__ void to_a(const float (&x)[4], const float (&y)[4], uint32_t (&f)[P][4]) {
-  uint32_t w[P];
+__device__ __forceinline__ void to_a(const float (&x)[4], const float (&y)[4], uint32_t (&f)[kPl<P>][4]) {
+  uint32_t w[kPl<P>];
   split2<P>(x[0], x[1], w);
 #pragma unroll
-  for (int p = 0; p < P; ++p) f[p][0] = w[p];
+  for (int p = 0; p < kPl<P>; ++p) f[p][0] = w[p];
   split2<P>(x[2], x[3], w);
 #pragma unroll
-  for (int p = 0; p < P; ++p) f[p][1] = w[p];
+  for (int p = 0; p < kPl<P>; ++p) f[p][1] = w[p];
   split2<P>(y[0], y[1], w);
 #pragma unroll
-  for (int p = 0; p < P; ++p) f[p][2] = w[p];
+  for (int p = 0; p < kPl<P>; ++p) f[p][2] = w[p];
   split2<P>(y[2], y[3], w);
 #pragma unroll
-  for (int p = 0; p < P; ++p) f[p][3] = w[p];
+  for (int p = 0; p < kPl<P>; ++p) f[p][3] = w[p];
 }
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool real) {
@@ -192,7 +245,7 @@ __device__ __forceinline__ void copy_ws(uint32_t dst, const void* src, int bytes
 }
 
 // 64 rows of a caller's tensor (row r at p + r ld; rows from `rows` on are zero and not read) as a
-// tile. bfloat16 arrives asynchronously; float32 is split into its planes on the way. 16-byte piece i
+// tile. bfloat16 arrives asynchronously; float32 is taken apart into its planes on the way. 16-byte piece i
 // of the tile is row 8 (i / (8 C8)) + i % 8, column block (i / 8) % C8: a warp reads 64 bytes of 8 rows.
 template <int C8>
 __device__ __forceinline__ void load_rows(const Tile<C8, 1>& t, const __nv_bfloat16* p, int64_t ld, int rows,
@@ -204,7 +257,7 @@ __device__ __forceinline__ void load_rows(const Tile<C8, 1>& t, const __nv_bfloa
   }
 }
 template <int C8>
-__device__ __forceinline__ void load_rows(const Tile<C8, 2>& t, const float* p, int64_t ld, int rows, int tid,
+__device__ __forceinline__ void load_rows(const Tile<C8, 3>& t, const float* p, int64_t ld, int rows, int tid,
                                           int threads) {
   for (int i = tid; i < 64 * C8; i += threads) {
     const int r = (i / (8 * C8)) * 8 + (i & 7), c8 = (i >> 3) % C8;
@@ -215,33 +268,56 @@ __device__ __forceinline__ void load_rows(const Tile<C8, 2>& t, const float* p, 
       y = __ldg(s + 1);
     }
     uint32_t w[4][2];
-    split2<2>(x.x, x.y, w[0]);
-    split2<2>(x.z, x.w, w[1]);
-    split2<2>(y.x, y.y, w[2]);
-    split2<2>(y.z, y.w, w[3]);
+    split2<3>(x.x, x.y, w[0]);
+    split2<3>(x.z, x.w, w[1]);
+    split2<3>(y.x, y.y, w[2]);
+    split2<3>(y.z, y.w, w[3]);
 #pragma unroll
     for (int q = 0; q < 2; ++q)
-      asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(t.base + q * Tile<C8, 2>::kPlane + i * 16),
+      asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(t.base + q * Tile<C8, 3>::kPlane + i * 16),
                    "r"(w[0][q]), "r"(w[1][q]), "r"(w[2][q]), "r"(w[3][q]) : "memory");
+  }
+}
+
+// Columns [8 c8, 8 c8 + 8 C) of a 64 x 64 tile of the workspace.
+template <int C, int P>
+__device__ __forceinline__ void copy_columns(const Tile<C, P>& t, const char* src, int c8, int tid, int threads) {
+#pragma unroll
+  for (int p = 0; p < kPl<P>; ++p)
+    for (int i = tid; i < 64 * C; i += threads)
+      cp_async16(t.base + p * Tile<C, P>::kPlane + i * 16,
+                 src + p * Tile<8, P>::kPlane + ((i / (8 * C)) * 8 + c8) * 128 + (i % (8 * C)) * 16, true);
+}
+
+// N steps of which each loads right operands and multiplies by them: the next step's are on their way
+// while this one's are multiplied.
+template <int N, int R, int P, typename Load, typename Use>
+__device__ __forceinline__ void pipelined(Load load, Use use) {
+  uint32_t f[2][R][2][kPl<P>][2];
+  load(0, f[0]);
+#pragma unroll
+  for (int s = 0; s < N; ++s) {
+    if (s + 1 < N) load(s + 1, f[(s + 1) & 1]);
+    use(s, f[s & 1]);
   }
 }
 
 // One accumulator pair into a tile of the workspace: block (r8, c8), 128 bytes a warp.
 template <int C8, int P>
 __device__ __forceinline__ void store_block(char* tile, int r8, int c8, float x, float y) {
-  uint32_t w[P];
+  uint32_t w[kPl<P>];
   split2<P>(x, y, w);
 #pragma unroll
-  for (int p = 0; p < P; ++p)
+  for (int p = 0; p < kPl<P>; ++p)
     *reinterpret_cast<uint32_t*>(tile + p * (8 * C8 * 128) + (r8 * C8 + c8) * 128 + (threadIdx.x & 31) * 4) = w[p];
 }
 // The same, transposed: the accumulator's rows become the tile's columns.
 template <int C8, int P>
 __device__ __forceinline__ void store_block_t(char* tile, int r8, int c8, float x, float y) {
-  uint32_t w[P];
+  uint32_t w[kPl<P>];
   split2<P>(x, y, w);
 #pragma unroll
-  for (int p = 0; p < P; ++p)
+  for (int p = 0; p < kPl<P>; ++p)
     *reinterpret_cast<uint32_t*>(tile + p * (8 * C8 * 128) + (r8 * C8 + c8) * 128 + (threadIdx.x & 31) * 4) =
         transpose8(w[p]);
 }
@@ -261,8 +337,9 @@ __device__ __forceinline__ void store_one(__nv_bfloat16* p, float x) { *p = __fl
 // real step. Slot s = 64 c + i of a row with `len` real steps is step
 // L - len + s when s < len, else the padding step s - len (when s < L).
 struct Problem {
-  int64_t B, L, n;  // n: chunks of a full row
-  int Hk, Hv, Dv;
+  int64_t B, L;
+  int n;  // chunks of a full row
+  int Hk, Hv, Dv, group;  // group: value heads that share a key head
   int64_t ldq, ldk, ldv;
   float scale;
   const int32_t* lengths;
@@ -274,32 +351,36 @@ struct Problem {
 
 // One chunk of one head.
 struct Where {
-  int64_t b, nc;  // batch row; chunk number over everything
-  int h, hk;
-  int64_t c, len, first;  // chunk of the row, the row's real steps, the step of the chunk's first slot
-  int rows;               // real steps in the chunk (may be <= 0)
+  int b, h, hk, c;  // batch row, value head, key head, chunk of the row
+  int rows;         // real steps in the chunk (may be <= 0)
+  int64_t nc, len;  // chunk number over everything; the row's real steps
+  int64_t step;     // the chunk's first slot as a step of the whole batch, b L + t
 };
-__device__ __forceinline__ int64_t row_length(const Problem& P, int64_t b) {
+__device__ __forceinline__ int64_t row_length(const Problem& P, int b) {
   if (P.lengths == nullptr) return P.L;
   const int64_t n = P.lengths[b];
   return n < 0 ? 0 : n > P.L ? P.L : n;
 }
-__device__ __forceinline__ Where locate(const Problem& P, int64_t bh, int64_t c) {
+__device__ __forceinline__ Where locate(const Problem& P, uint32_t bh, int c) {
   Where w;
-  w.b = bh / P.Hv;
-  w.h = (int)(bh % P.Hv);
-  w.hk = w.h / (P.Hv / P.Hk);
+  w.b = (int)(bh / (uint32_t)P.Hv);
+  w.h = (int)(bh - (uint32_t)w.b * P.Hv);
+  w.hk = w.h / P.group;
   w.c = c;
-  w.nc = bh * P.n + c;
+  w.nc = (int64_t)bh * P.n + c;
   w.len = row_length(P, w.b);
-  w.first = P.L - w.len + c * kC;
-  const int64_t left = w.len - c * kC;
+  w.step = w.b * P.L + P.L - w.len + (int64_t)c * kC;
+  const int64_t left = w.len - (int64_t)c * kC;
   w.rows = (int)(left < kC ? left : kC);
   return w;
 }
+__device__ __forceinline__ Where locate(const Problem& P) {  // of a grid with a block for every chunk
+  const uint32_t bh = blockIdx.x / (uint32_t)P.n;
+  return locate(P, bh, (int)(blockIdx.x - bh * P.n));
+}
 // The padding step that slot i of the chunk stands for, or -1.
 __device__ __forceinline__ int64_t padding_step(const Problem& P, const Where& w, int i) {
-  const int64_t s = w.c * kC + i;
+  const int64_t s = (int64_t)w.c * kC + i;
   return s >= w.len && s < P.L ? s - w.len : -1;
 }
 
