@@ -36,10 +36,10 @@ du_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k, c
   const int tid = threadIdx.x, warp = tid >> 5, l = tid & 31;
   const int64_t row0 = w.step, ldo = (int64_t)P.Hv * P.Dv;
   const TI* src = d_o + row0 * ldo + (int64_t)w.h * P.Dv;
-  load_rows(tq, q + row0 * P.ldq + w.hk * DK, P.ldq, w.rows, tid, 128);
-  load_rows(tk, k + row0 * P.ldk + w.hk * DK, P.ldk, w.rows, tid, 128);
-  load_rows(to, src, ldo, w.rows, tid, 128);
-  copy_ws(smem_u32(G), P.gates + w.nc * kGates, 4 * kGateFloats<NM>, tid, 128);
+  load_rows<128>(tq, q + row0 * P.ldq + w.hk * DK, P.ldq, w.rows, tid);
+  load_rows<128>(tk, k + row0 * P.ldk + w.hk * DK, P.ldk, w.rows, tid);
+  load_rows<128>(to, src, ldo, w.rows, tid);
+  copy_ws<4 * kGateFloats<NM>, 128>(smem_u32(G), P.gates + w.nc * kGates, tid);
   cp_async_commit();
   cp_async_wait<0>();
   __syncthreads();
@@ -74,7 +74,7 @@ du_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k, c
   for (int part = 0; part < dvb; ++part) {
     if (part > 0) {
       __syncthreads();
-      load_rows(to, src + 64 * part, ldo, w.rows, tid, 128);
+      load_rows<128>(to, src + 64 * part, ldo, w.rows, tid);
       cp_async_commit();
       cp_async_wait<0>();
       __syncthreads();
@@ -112,7 +112,7 @@ struct BackSmem {
 // The states' gradients from chunk to chunk, last to first: as chain_kernel, a warp holds dS^T of 16
 // columns in accumulators, and two more warps load.
 template <typename TI, int DK, int NI, int NM, int WARPS>
-__global__ void __launch_bounds__(32 * (WARPS + kLoadWarps))
+__global__ void __launch_bounds__(32 * (WARPS + kLoadWarps), WARPS == 4 && NM < 3 ? 2 : 1)
 back_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k, const TI* __restrict__ d_o,
             const float* __restrict__ ds_last, float* __restrict__ ds0) {
   extern __shared__ __align__(128) unsigned char smem[];
@@ -132,14 +132,12 @@ back_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k,
         const uint32_t st = smem_u32(smem) + (uint32_t)(c % L::kStages) * L::kStage;
         const int64_t nc = w0.nc + c, left = w0.len - (int64_t)c * kC, row0 = w0.step + (int64_t)c * kC;
         const int rows = (int)(left < kC ? left : kC);
-        copy_ws(st, P.W + nc * L::kW, L::kW, tid, 32 * kLoadWarps);
-        load_rows(Tile<DK / 8, NI>{st + L::kW}, k + row0 * P.ldk + w0.hk * DK, P.ldk, rows, tid, 32 * kLoadWarps);
-        load_rows(Tile<DK / 8, NI>{st + L::kW + L::kK}, q + row0 * P.ldq + w0.hk * DK, P.ldq, rows, tid, 32 * kLoadWarps);
-        load_rows(Tile<2 * WARPS, NI>{st + L::kW + 2 * L::kK},
-                  d_o + row0 * ldo + (int64_t)w0.h * P.Dv + 16 * WARPS * part, ldo, rows, tid, 32 * kLoadWarps);
-        copy_columns(Tile<2 * WARPS, NM>{st + L::kW + 2 * L::kK + L::kO},
-                     P.dU + (nc * dvb + block) * Tile<8, NM>::kBytes, c8, tid, 32 * kLoadWarps);
-        copy_ws(st + L::kW + 2 * L::kK + L::kO + L::kU, P.gates + nc * kGates, 1024, tid, 32 * kLoadWarps);
+        copy_ws<L::kW, 32 * kLoadWarps>(st, P.W + nc * L::kW, tid);
+        load_rows<32 * kLoadWarps>(Tile<DK / 8, NI>{st + L::kW}, k + row0 * P.ldk + w0.hk * DK, P.ldk, rows, tid);
+        load_rows<32 * kLoadWarps>(Tile<DK / 8, NI>{st + L::kW + L::kK}, q + row0 * P.ldq + w0.hk * DK, P.ldq, rows, tid);
+        load_rows<32 * kLoadWarps>(Tile<2 * WARPS, NI>{st + L::kW + 2 * L::kK}, d_o + row0 * ldo + (int64_t)w0.h * P.Dv + 16 * WARPS * part, ldo, rows, tid);
+        copy_columns<32 * kLoadWarps>(Tile<2 * WARPS, NM>{st + L::kW + 2 * L::kK + L::kO}, P.dU + (nc * dvb + block) * Tile<8, NM>::kBytes, c8, tid);
+        copy_ws<1024, 32 * kLoadWarps>(st + L::kW + 2 * L::kK + L::kO + L::kU, P.gates + nc * kGates, tid);
       }
       cp_async_commit();
     };
@@ -281,12 +279,17 @@ back_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k,
   }
 }
 
-template <int DK, int NI, int NM>
+template <int DK, int NI, int NM, int PARTS>
 struct GradSmem {
   static constexpr int kQ = Tile<DK / 8, NI>::kBytes, kI = Tile<8, NI>::kBytes, kM = Tile<8, NM>::kBytes,
                        kS = Tile<DK / 8, NM>::kBytes;
-  static constexpr int kTiles = 2 * kQ + kM /*T*/ + 2 * kI /*V, dO*/ + 2 * kM /*U, dU*/ + 2 * kS;
-  static constexpr int kFloats = kGates + 2 * 5 * 64 /*row sums by half*/ + 4 * 64 /*column sums by row group*/ + 16;
+  static constexpr int kStage = 2 * kI /*V, dO*/ + 2 * kM /*U, dU*/ + 2 * kS;
+  static constexpr int kFixed = 2 * kQ + kM /*T*/;
+  // gates; row sums by column part; column sums by row group; <S, dS'> by warp
+  static constexpr int kFloats = kGates + PARTS * 5 * 64 + 4 * 64 + 4 * PARTS;
+  // Dk 64: two blocks an SM overlap each other; Dk 128: one, whose next 64 columns of Dv load meanwhile
+  static constexpr int kStages = DK == 128 && kFixed + 2 * kStage + 4 * kFloats <= 227 * 1024 ? 2 : 1;
+  static constexpr int kTiles = kFixed + kStages * kStage;
   static constexpr int kBytes = kTiles + 4 * kFloats;
 };
 
@@ -295,30 +298,58 @@ __device__ __forceinline__ float quad_sum(float x) {  // over the 4 lanes of a f
   return x + __shfl_xor_sync(0xffffffffu, x, 2);
 }
 
-// Everything else, for all chunks at once. Warp (rg, hf) of 8 holds rows 16 rg .. of the chunk and half
-// of the columns of each product.
-template <typename TI, typename TG, int DK, int NI, int NM>
-__global__ void __launch_bounds__(256, 1)
+// The dot product of 16 bytes of two tiles of one layout (PLANE bytes between their planes).
+template <int P, int PLANE>
+__device__ __forceinline__ float dot16(uint32_t a, uint32_t b) {
+  uint32_t x[kPl<P>][4], y[kPl<P>][4];
+#pragma unroll
+  for (int p = 0; p < kPl<P>; ++p) {
+    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(x[p][0]), "=r"(x[p][1]), "=r"(x[p][2]), "=r"(x[p][3])
+                 : "r"(a + p * PLANE) : "memory");
+    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(y[p][0]), "=r"(y[p][1]), "=r"(y[p][2]), "=r"(y[p][3])
+                 : "r"(b + p * PLANE) : "memory");
+  }
+  float s = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t u[kPl<P>], v[kPl<P>];
+#pragma unroll
+    for (int p = 0; p < kPl<P>; ++p) {
+      u[p] = x[p][i];
+      v[p] = y[p][i];
+    }
+    const float2 f = join2<P>(u), g = join2<P>(v);
+    s = fmaf(f.x, g.x, s);
+    s = fmaf(f.y, g.y, s);
+  }
+  return s;
+}
+
+// Everything else, for all chunks at once. Warp (rg, pt) holds rows 16 rg .. of the chunk and one of
+// PARTS parts of the columns of each product.
+template <typename TI, typename TG, int DK, int NI, int NM, int PARTS>
+__global__ void __launch_bounds__(128 * PARTS, PARTS == 4 || NM == 3 ? 1 : 2)
 grad_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k, const TI* __restrict__ v,
-            const TI* __restrict__ d_o, TG* __restrict__ dq, TG* __restrict__ dk, int64_t heads, TI* __restrict__ dv,
+            const TI* __restrict__ d_o, TG* __restrict__ dq, TG* __restrict__ dk, int heads, TI* __restrict__ dv,
             TI* __restrict__ dg, TI* __restrict__ dbeta) {
   // dq, dk: `heads` heads a step (the key heads, or the value heads where a later kernel sums them)
   extern __shared__ __align__(128) unsigned char smem[];
-  using L = GradSmem<DK, NI, NM>;
-  constexpr int NB = DK / 16;  // 8-column blocks in a warp's half of Dk
+  using L = GradSmem<DK, NI, NM, PARTS>;
+  constexpr int THREADS = 128 * PARTS;
+  constexpr int NB = DK / (8 * PARTS), VB = 8 / PARTS;  // 8-column blocks of a warp's part of Dk, of 64 columns
   const Where w = locate(P);
-  const int tid = threadIdx.x, warp = tid >> 5, l = tid & 31, rg = warp & 3, hf = warp >> 2;
-  const int64_t hq = heads == P.Hk ? w.hk : w.h;
+  const int tid = threadIdx.x, warp = tid >> 5, l = tid & 31, rg = warp & 3, pt = warp >> 2;
+  const int hq = heads == P.Hk ? w.hk : w.h;
   if (w.rows < kC && w.len < P.L) {
     for (int i = 0; i < kC; ++i) {
       const int64_t t = padding_step(P, w, i);
       if (t < 0) continue;
       const int64_t at = w.b * P.L + t;
-      for (int j = tid; j < DK / 2; j += 256) {
+      for (int j = tid; j < DK / 2; j += THREADS) {
         store_pair(dq + (at * heads + hq) * DK + 2 * j, 0.0f, 0.0f);
         store_pair(dk + (at * heads + hq) * DK + 2 * j, 0.0f, 0.0f);
       }
-      for (int j = tid; j < P.Dv / 2; j += 256) store_pair(dv + (at * P.Hv + w.h) * P.Dv + 2 * j, 0.0f, 0.0f);
+      for (int j = tid; j < P.Dv / 2; j += THREADS) store_pair(dv + (at * P.Hv + w.h) * P.Dv + 2 * j, 0.0f, 0.0f);
       if (tid == 0) {
         store_one(dg + at * P.Hv + w.h, 0.0f);
         store_one(dbeta + at * P.Hv + w.h, 0.0f);
@@ -326,58 +357,69 @@ grad_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k,
     }
   }
   if (w.rows <= 0) return;
-  uint32_t at = smem_u32(smem);
-  const Tile<DK / 8, NI> tq{at}, tk{at + L::kQ};
-  const Tile<8, NM> tt{at + 2 * L::kQ}, tu{at + 2 * L::kQ + L::kM}, tdu{at + 2 * L::kQ + 2 * L::kM};
-  at += 2 * L::kQ + 3 * L::kM;
-  const Tile<8, NI> tv{at}, to{at + L::kI};
-  const Tile<DK / 8, NM> ts{at + 2 * L::kI}, tds{at + 2 * L::kI + L::kS};
+  const uint32_t base = smem_u32(smem);
+  const Tile<DK / 8, NI> tq{base}, tk{base + L::kQ};
+  const Tile<8, NM> tt{base + 2 * L::kQ};
   float* G = reinterpret_cast<float*>(smem + L::kTiles);
-  float* bt = G + 64;
-  float* rows = G + kGates;         // [half][5][64]: dbeta without S, x1.q, x2.k, x3.k, row sums less none
-  float* cols = rows + 2 * 5 * 64;  // [rg][64]
-  float* dots = cols + 4 * 64;   // per warp: part of <S, dS'>
+  float* bt = G + kBeta;
+  float* rows = G + kGates;             // [part][5][64]: dbeta without S, x1.q, x2.k, x3.k, row sums
+  float* cols = rows + PARTS * 5 * 64;  // [rg][64]
+  float* dots = cols + 4 * 64;
   const int64_t row0 = w.step, ldo = (int64_t)P.Hv * P.Dv;
   const int dvb = P.Dv / 64;
-  load_rows(tq, q + row0 * P.ldq + w.hk * DK, P.ldq, w.rows, tid, 256);
-  load_rows(tk, k + row0 * P.ldk + w.hk * DK, P.ldk, w.rows, tid, 256);
-  copy_ws(tt.base, P.T + w.nc * L::kM, L::kM, tid, 256);
-  copy_ws(smem_u32(G), P.gates + w.nc * kGates, 4 * kGateFloats<NM>, tid, 256);
+  const TI *vsrc = v + row0 * P.ldv + w.h * P.Dv, *osrc = d_o + row0 * ldo + w.h * P.Dv;
+  const auto load = [&](int part) {
+    if (part < dvb) {
+      const uint32_t st = base + L::kFixed + (part % L::kStages) * L::kStage;
+      const int64_t tile = w.nc * dvb + part;
+      copy_ws<L::kM, THREADS>(st + 2 * L::kI + L::kM, P.dU + tile * L::kM, tid);
+      load_rows<THREADS>(Tile<8, NI>{st}, vsrc + 64 * part, P.ldv, w.rows, tid);
+      load_rows<THREADS>(Tile<8, NI>{st + L::kI}, osrc + 64 * part, ldo, w.rows, tid);
+      copy_ws<L::kM, THREADS>(st + 2 * L::kI, P.U + tile * L::kM, tid);
+      copy_ws<L::kS, THREADS>(st + 2 * L::kI + 2 * L::kM, P.S + tile * L::kS, tid);
+      copy_ws<L::kS, THREADS>(st + 2 * L::kI + 2 * L::kM + L::kS, P.dS + tile * L::kS, tid);
+    }
+  };
+  copy_ws<4 * kGateFloats<NM>, THREADS>(smem_u32(G), P.gates + w.nc * kGates, tid);
+  copy_ws<L::kM, THREADS>(tt.base, P.T + w.nc * L::kM, tid);
+  load(0);
+  if (L::kStages == 2) {
+    cp_async_commit();
+    load(1);
+  }
+  load_rows<THREADS>(tq, q + row0 * P.ldq + w.hk * DK, P.ldq, w.rows, tid);
+  load_rows<THREADS>(tk, k + row0 * P.ldk + w.hk * DK, P.ldk, w.rows, tid);
+  cp_async_commit();
   const int rr = l >> 2, c0 = 2 * (l & 3), r0 = 16 * rg + rr;
-  float x1[NB][4] = {}, x2[NB][4] = {}, x3[NB][4] = {}, dp[4][4] = {}, da[4][4] = {};
+  float x1[NB][4] = {}, x2[NB][4] = {}, x3[NB][4] = {}, dp[VB][4] = {}, da[VB][4] = {};
   float vdot[2] = {0.0f, 0.0f}, sdot = 0.0f;
   for (int part = 0; part < dvb; ++part) {
-    if (part > 0) __syncthreads();
-    load_rows(tv, v + row0 * P.ldv + (int64_t)w.h * P.Dv + 64 * part, P.ldv, w.rows, tid, 256);
-    load_rows(to, d_o + row0 * ldo + (int64_t)w.h * P.Dv + 64 * part, ldo, w.rows, tid, 256);
-    const int64_t at8 = w.nc * dvb + part;
-    copy_ws(tu.base, P.U + at8 * L::kM, L::kM, tid, 256);
-    copy_ws(tdu.base, P.dU + at8 * L::kM, L::kM, tid, 256);
-    copy_ws(ts.base, P.S + at8 * L::kS, L::kS, tid, 256);
-    copy_ws(tds.base, P.dS + at8 * L::kS, L::kS, tid, 256);
-    cp_async_commit();
-    cp_async_wait<0>();
+    cp_async_wait<L::kStages - 1>();
     __syncthreads();
+    const uint32_t st = base + L::kFixed + (part % L::kStages) * L::kStage;
+    const Tile<8, NI> tv{st}, to{st + L::kI};
+    const Tile<8, NM> tu{st + 2 * L::kI}, tdu{st + 2 * L::kI + L::kM};
+    const Tile<DK / 8, NM> ts{st + 2 * L::kI + 2 * L::kM}, tds{st + 2 * L::kI + 2 * L::kM + L::kS};
     {  // dR, dV
-      float r[4][4] = {};
+      float r[VB][4] = {};
 #pragma unroll
       for (int kk = 0; kk < 4; ++kk)
         if (kk >= rg) {
           uint32_t a[kPl<NM>][4];
           tt.a_t(2 * rg, 2 * kk, a);
 #pragma unroll
-          for (int nn = 0; nn < 2; ++nn) {
+          for (int nn = 0; nn < VB / 2; ++nn) {
             uint32_t b[2][kPl<NM>][2];
-            tdu.b(4 * hf + 2 * nn, 2 * kk, b);
+            tdu.b(VB * pt + 2 * nn, 2 * kk, b);
             mma_p<NM, NM>(r[2 * nn], a, b[0]);
             mma_p<NM, NM>(r[2 * nn + 1], a, b[1]);
           }
         }
       const float b0 = bt[r0], b1 = bt[r0 + 8];
-      TI* out = dv + ((row0 + r0) * P.Hv + w.h) * P.Dv + 64 * part + 32 * hf + c0;
+      TI* out = dv + ((row0 + r0) * P.Hv + w.h) * P.Dv + 64 * part + 8 * VB * pt + c0;
 #pragma unroll
-      for (int nb = 0; nb < 4; ++nb) {
-        const float2 va = tv.pair(2 * rg, 4 * hf + nb), vb = tv.pair(2 * rg + 1, 4 * hf + nb);
+      for (int nb = 0; nb < VB; ++nb) {
+        const float2 va = tv.pair(2 * rg, VB * pt + nb), vb = tv.pair(2 * rg + 1, VB * pt + nb);
         vdot[0] += r[nb][0] * va.x + r[nb][1] * va.y;
         vdot[1] += r[nb][2] * vb.x + r[nb][3] * vb.y;
         if (r0 < w.rows) store_pair(out + 8 * nb, b0 * r[nb][0], b0 * r[nb][1]);
@@ -385,21 +427,14 @@ grad_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k,
       }
       __syncthreads();  // dU has been read: dR takes its place
 #pragma unroll
-      for (int nb = 0; nb < 4; ++nb) {
-        tdu.put(2 * rg, 4 * hf + nb, r[nb][0], r[nb][1]);
-        tdu.put(2 * rg + 1, 4 * hf + nb, r[nb][2], r[nb][3]);
+      for (int nb = 0; nb < VB; ++nb) {
+        tdu.put(2 * rg, VB * pt + nb, r[nb][0], r[nb][1]);
+        tdu.put(2 * rg + 1, VB * pt + nb, r[nb][2], r[nb][3]);
       }
     }
-    for (int i = tid; i < Tile<DK / 8, NM>::kPlane / 4; i += 256) {
-      uint32_t a[kPl<NM>], b[kPl<NM>];
-#pragma unroll
-      for (int p = 0; p < kPl<NM>; ++p) {
-        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(a[p]) : "r"(ts.base + p * Tile<DK / 8, NM>::kPlane + 4 * i));
-        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(b[p]) : "r"(tds.base + p * Tile<DK / 8, NM>::kPlane + 4 * i));
-      }
-      const float2 x = join2<NM>(a), y = join2<NM>(b);
-      sdot += x.x * y.x + x.y * y.y;
-    }
+#pragma unroll 2
+    for (int i = tid * 16; i < Tile<DK / 8, NM>::kPlane; i += THREADS * 16)
+      sdot += dot16<NM, Tile<DK / 8, NM>::kPlane>(ts.base + i, tds.base + i);
     __syncthreads();
 #pragma unroll
     for (int kk = 0; kk < 4; ++kk) {
@@ -409,39 +444,45 @@ grad_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k,
       tdu.a(2 * rg, 2 * kk, ar);
 #pragma unroll
       for (int nn = 0; nn < NB / 2; ++nn) {
-        uint32_t b[2][kPl<NM>][2];
-        ts.b(NB * hf + 2 * nn, 2 * kk, b);
+        uint32_t b[2][kPl<NM>][2], c[2][kPl<NM>][2];
+        ts.b(NB * pt + 2 * nn, 2 * kk, b);
+        tds.b(NB * pt + 2 * nn, 2 * kk, c);
         mma_p<NI, NM>(x1[2 * nn], ao, b[0]);
         mma_p<NI, NM>(x1[2 * nn + 1], ao, b[1]);
         mma_p<NM, NM>(x3[2 * nn], ar, b[0]);
         mma_p<NM, NM>(x3[2 * nn + 1], ar, b[1]);
-        tds.b(NB * hf + 2 * nn, 2 * kk, b);
-        mma_p<NM, NM>(x2[2 * nn], au, b[0]);
-        mma_p<NM, NM>(x2[2 * nn + 1], au, b[1]);
+        mma_p<NM, NM>(x2[2 * nn], au, c[0]);
+        mma_p<NM, NM>(x2[2 * nn + 1], au, c[1]);
       }
 #pragma unroll
-      for (int nn = 0; nn < 2; ++nn) {
+      for (int nn = 0; nn < VB / 2; ++nn) {
         uint32_t b[2][kPl<NM>][2];
-        tu.b_t(4 * hf + 2 * nn, 2 * kk, b);
+        tu.b_t(VB * pt + 2 * nn, 2 * kk, b);
         mma_p<NI, NM>(dp[2 * nn], ao, b[0]);
         mma_p<NI, NM>(dp[2 * nn + 1], ao, b[1]);
         mma_p<NM, NM>(da[2 * nn], ar, b[0]);
         mma_p<NM, NM>(da[2 * nn + 1], ar, b[1]);
       }
     }
+    __syncthreads();
+    load(part + L::kStages);
+    cp_async_commit();
   }
-  __syncthreads();  // U and dR have been read: scale dP o D and M take their places
+  cp_async_wait<0>();
+  __syncthreads();
+  // the stages have been read: scale dP o D and M take their place
+  const Tile<8, NM> tp{base + L::kFixed}, tm{base + L::kFixed + L::kM};
   {
-    float qk[4][4] = {}, kk_[4][4] = {};
+    float qk[VB][4] = {}, kk_[VB][4] = {};
 #pragma unroll
     for (int kk = 0; kk < DK / 16; ++kk) {
       uint32_t aq[kPl<NI>][4], ak[kPl<NI>][4];
       tq.a(2 * rg, 2 * kk, aq);
       tk.a(2 * rg, 2 * kk, ak);
 #pragma unroll
-      for (int nn = 0; nn < 2; ++nn) {
+      for (int nn = 0; nn < VB / 2; ++nn) {
         uint32_t b[2][kPl<NI>][2];
-        tk.b_t(4 * hf + 2 * nn, 2 * kk, b);
+        tk.b_t(VB * pt + 2 * nn, 2 * kk, b);
         mma_p<NI, NI>(qk[2 * nn], aq, b[0]);
         mma_p<NI, NI>(qk[2 * nn + 1], aq, b[1]);
         mma_p<NI, NI>(kk_[2 * nn], ak, b[0]);
@@ -450,11 +491,11 @@ grad_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k,
     }
     float rs[2] = {0.0f, 0.0f}, bs[2] = {0.0f, 0.0f};
 #pragma unroll
-    for (int nb = 0; nb < 4; ++nb) {
+    for (int nb = 0; nb < VB; ++nb) {
       float cs[2] = {0.0f, 0.0f};
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int i = r0 + 8 * (e >> 1), j = 32 * hf + 8 * nb + c0 + (e & 1);
+        const int i = r0 + 8 * (e >> 1), j = 8 * (VB * pt + nb) + c0 + (e & 1);
         const float d = j <= i ? decay_between<NM>(G, i, j) : 0.0f;
         const float p = P.scale * dp[nb][e] * d;
         const float m0 = j < i ? -da[nb][e] * d : 0.0f, mk = m0 * kk_[nb][e], b = bt[i];
@@ -467,11 +508,11 @@ grad_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k,
       }
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        tu.put(2 * rg + e, 4 * hf + nb, dp[nb][2 * e], dp[nb][2 * e + 1]);
-        tdu.put(2 * rg + e, 4 * hf + nb, da[nb][2 * e], da[nb][2 * e + 1]);
+        tp.put(2 * rg + e, VB * pt + nb, dp[nb][2 * e], dp[nb][2 * e + 1]);
+        tm.put(2 * rg + e, VB * pt + nb, da[nb][2 * e], da[nb][2 * e + 1]);
 #pragma unroll
         for (int d = 4; d < 32; d <<= 1) cs[e] += __shfl_xor_sync(0xffffffffu, cs[e], d);
-        if (l < 4) cols[rg * 64 + 32 * hf + 8 * nb + c0 + e] = cs[e];
+        if (l < 4) cols[rg * 64 + 8 * (VB * pt + nb) + c0 + e] = cs[e];
       }
     }
     // row products, on this warp's columns
@@ -480,7 +521,7 @@ grad_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k,
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const float2 qv = tq.pair(2 * rg + e, NB * hf + nb), kv = tk.pair(2 * rg + e, NB * hf + nb);
+        const float2 qv = tq.pair(2 * rg + e, NB * pt + nb), kv = tk.pair(2 * rg + e, NB * pt + nb);
         y1[e] += x1[nb][2 * e] * qv.x + x1[nb][2 * e + 1] * qv.y;
         y2[e] += x2[nb][2 * e] * kv.x + x2[nb][2 * e + 1] * kv.y;
         y3[e] += x3[nb][2 * e] * kv.x + x3[nb][2 * e + 1] * kv.y;
@@ -491,7 +532,7 @@ grad_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k,
                           quad_sum(rs[e])};
       if ((l & 3) == 0) {
 #pragma unroll
-        for (int i = 0; i < 5; ++i) rows[(hf * 5 + i) * 64 + r0 + 8 * e] = a[i];
+        for (int i = 0; i < 5; ++i) rows[(pt * 5 + i) * 64 + r0 + 8 * e] = a[i];
       }
     }
 #pragma unroll
@@ -499,21 +540,28 @@ grad_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k,
     if (l == 0) dots[warp] = sdot;
   }
   __syncthreads();
-  if (warp == 0) {  // dbeta, and dg: the cumulative decay's gradient summed from the end
+  if (warp == 4 * PARTS - 4) {  // dbeta, and dg: the cumulative decay's gradient summed from the end
+    // (by a warp of row group 0, whose last products are the fewest)
     float dG[2], add = 0.0f;
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       const int i = 2 * l + e;
       float a[5];
 #pragma unroll
-      for (int x = 0; x < 5; ++x) a[x] = rows[x * 64 + i] + rows[(5 + x) * 64 + i];
+      for (int x = 0; x < 5; ++x) {
+        a[x] = 0.0f;
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) a[x] += rows[(p * 5 + x) * 64 + i];
+      }
       const float up = G[kUp + i], down = G[kDown + i];
       const float col = (cols[i] + cols[64 + i]) + (cols[128 + i] + cols[192 + i]);
       dG[e] = P.scale * up * a[1] - bt[i] * up * a[3] - down * a[2] + a[4] - col;
       add += down * a[2];
       if (i < w.rows) store_one(dbeta + (row0 + i) * P.Hv + w.h, a[0] - up * a[3]);
     }
-    const float all = ((dots[0] + dots[1]) + (dots[2] + dots[3])) + ((dots[4] + dots[5]) + (dots[6] + dots[7]));
+    float all = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4 * PARTS; ++i) all += dots[i];
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) add += __shfl_xor_sync(0xffffffffu, add, d);
     if (l == 31) dG[1] += add + G[kUp + 63] * all;
@@ -539,12 +587,12 @@ grad_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k,
   for (int kk = 0; kk < 4; ++kk) {
     if (kk <= rg) {  // rows of scale dP o D and of M against K
       uint32_t ap[kPl<NM>][4], am[kPl<NM>][4];
-      tu.a(2 * rg, 2 * kk, ap);
-      tdu.a(2 * rg, 2 * kk, am);
+      tp.a(2 * rg, 2 * kk, ap);
+      tm.a(2 * rg, 2 * kk, am);
 #pragma unroll
       for (int nn = 0; nn < NB / 2; ++nn) {
         uint32_t b[2][kPl<NI>][2];
-        tk.b(NB * hf + 2 * nn, 2 * kk, b);
+        tk.b(NB * pt + 2 * nn, 2 * kk, b);
         mma_p<NM, NI>(x1[2 * nn], ap, b[0]);
         mma_p<NM, NI>(x1[2 * nn + 1], ap, b[1]);
         mma_p<NM, NI>(x2[2 * nn], am, b[0]);
@@ -553,30 +601,32 @@ grad_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k,
     }
     if (kk >= rg) {  // their columns against Q and K
       uint32_t ap[kPl<NM>][4], am[kPl<NM>][4];
-      tu.a_t(2 * rg, 2 * kk, ap);
-      tdu.a_t(2 * rg, 2 * kk, am);
+      tp.a_t(2 * rg, 2 * kk, ap);
+      tm.a_t(2 * rg, 2 * kk, am);
 #pragma unroll
       for (int nn = 0; nn < NB / 2; ++nn) {
-        uint32_t b[2][kPl<NI>][2];
-        tq.b(NB * hf + 2 * nn, 2 * kk, b);
+        uint32_t b[2][kPl<NI>][2], c[2][kPl<NI>][2];
+        tq.b(NB * pt + 2 * nn, 2 * kk, b);
+        tk.b(NB * pt + 2 * nn, 2 * kk, c);
         mma_p<NM, NI>(x2[2 * nn], ap, b[0]);
         mma_p<NM, NI>(x2[2 * nn + 1], ap, b[1]);
-        tk.b(NB * hf + 2 * nn, 2 * kk, b);
-        mma_p<NM, NI>(x2[2 * nn], am, b[0]);
-        mma_p<NM, NI>(x2[2 * nn + 1], am, b[1]);
+        mma_p<NM, NI>(x2[2 * nn], am, c[0]);
+        mma_p<NM, NI>(x2[2 * nn + 1], am, c[1]);
       }
     }
   }
-  TG* oq = dq + ((row0 + r0) * heads + hq) * DK + 8 * NB * hf + c0;
-  TG* ok = dk + ((row0 + r0) * heads + hq) * DK + 8 * NB * hf + c0;
+  TG* oq = dq + ((row0 + r0) * heads + hq) * DK + 8 * NB * pt + c0;
+  TG* ok = dk + ((row0 + r0) * heads + hq) * DK + 8 * NB * pt + c0;
 #pragma unroll
   for (int e = 0; e < 2; ++e)
     if (r0 + 8 * e < w.rows) {
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
-        store_pair(oq + 8 * e * heads * DK + 8 * nb, x1[nb][2 * e], x1[nb][2 * e + 1]);
-        store_pair(ok + 8 * e * heads * DK + 8 * nb, x2[nb][2 * e], x2[nb][2 * e + 1]);
+        store_pair(oq + 8 * nb, x1[nb][2 * e], x1[nb][2 * e + 1]);
+        store_pair(ok + 8 * nb, x2[nb][2 * e], x2[nb][2 * e + 1]);
       }
+      oq += 8 * heads * DK;
+      ok += 8 * heads * DK;
     }
 }
 

@@ -122,8 +122,8 @@ prepare_kernel(const Problem P, const TI* __restrict__ k, const TI* __restrict__
   if (w.rows <= 0) return;
   const int tid = threadIdx.x, warp = tid >> 5, l = tid & 31;
   const int64_t row0 = w.step;
-  load_rows(tk, k + row0 * P.ldk + w.hk * DK, P.ldk, w.rows, tid, 128);
-  load_rows(tv, v + row0 * P.ldv + (int64_t)w.h * P.Dv, P.ldv, w.rows, tid, 128);
+  load_rows<128>(tk, k + row0 * P.ldk + w.hk * DK, P.ldk, w.rows, tid);
+  load_rows<128>(tv, v + row0 * P.ldv + (int64_t)w.h * P.Dv, P.ldv, w.rows, tid);
   cp_async_commit();
   if (warp == 0) {
     load_gates<NM>(g + row0 * P.Hv + w.h, beta + row0 * P.Hv + w.h, P.Hv, w.rows, sg);
@@ -216,7 +216,7 @@ prepare_kernel(const Problem P, const TI* __restrict__ k, const TI* __restrict__
   for (int part = 0; part < dvb; ++part) {
     if (part > 0) {
       __syncthreads();
-      load_rows(tv, v + row0 * P.ldv + (int64_t)w.h * P.Dv + 64 * part, P.ldv, w.rows, tid, 128);
+      load_rows<128>(tv, v + row0 * P.ldv + (int64_t)w.h * P.Dv + 64 * part, P.ldv, w.rows, tid);
       cp_async_commit();
       cp_async_wait<0>();
       __syncthreads();
@@ -285,7 +285,7 @@ struct ChainSmem {
 // shares only the tiles that it streams. Two more warps only load, kStages - 1 chunks ahead: one barrier a
 // chunk says both that a stage has arrived and that the one before it may be filled again.
 template <typename TI, int DK, int NI, int NM, int WARPS>
-__global__ void __launch_bounds__(32 * (WARPS + kLoadWarps))
+__global__ void __launch_bounds__(32 * (WARPS + kLoadWarps), WARPS == 4 && NM < 3 ? 2 : 1)
 chain_kernel(const Problem P, const TI* __restrict__ k, const float* __restrict__ s0,
              float* __restrict__ s_last) {
   extern __shared__ __align__(128) unsigned char smem[];
@@ -303,12 +303,11 @@ chain_kernel(const Problem P, const TI* __restrict__ k, const float* __restrict_
       if (c < chunks) {
         const uint32_t st = smem_u32(smem) + (uint32_t)(c % L::kStages) * L::kStage;
         const int64_t nc = w0.nc + c, left = w0.len - (int64_t)c * kC;
-        copy_ws(st, P.W + nc * L::kW, L::kW, tid, 32 * kLoadWarps);
-        load_rows(Tile<DK / 8, NI>{st + L::kW}, k + (w0.step + (int64_t)c * kC) * P.ldk + w0.hk * DK, P.ldk,
-                  (int)(left < kC ? left : kC), tid, 32 * kLoadWarps);
-        copy_columns(Tile<2 * WARPS, NM>{st + L::kW + L::kK}, P.U + (nc * dvb + block) * Tile<8, NM>::kBytes, c8, tid,
-                     32 * kLoadWarps);
-        copy_ws(st + L::kW + L::kK + L::kU, P.gates + nc * kGates, 1024, tid, 32 * kLoadWarps);
+        copy_ws<L::kW, 32 * kLoadWarps>(st, P.W + nc * L::kW, tid);
+        load_rows<32 * kLoadWarps>(Tile<DK / 8, NI>{st + L::kW}, k + (w0.step + (int64_t)c * kC) * P.ldk + w0.hk * DK,
+                                   P.ldk, (int)(left < kC ? left : kC), tid);
+        copy_columns<32 * kLoadWarps>(Tile<2 * WARPS, NM>{st + L::kW + L::kK}, P.U + (nc * dvb + block) * Tile<8, NM>::kBytes, c8, tid);
+        copy_ws<1024, 32 * kLoadWarps>(st + L::kW + L::kK + L::kU, P.gates + nc * kGates, tid);
       }
       cp_async_commit();
     };
@@ -453,13 +452,13 @@ output_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ 
   float* G = reinterpret_cast<float*>(smem + 2 * L::kQ + L::kU + L::kS);
   const int64_t row0 = w.step;
   const int dvb = P.Dv / 64;
-  load_rows(tq, q + row0 * P.ldq + w.hk * DK, P.ldq, w.rows, tid, 128);
-  load_rows(tk, k + row0 * P.ldk + w.hk * DK, P.ldk, w.rows, tid, 128);
-  copy_ws(smem_u32(G), P.gates + w.nc * kGates, 4 * kGateFloats<NM>, tid, 128);
+  load_rows<128>(tq, q + row0 * P.ldq + w.hk * DK, P.ldq, w.rows, tid);
+  load_rows<128>(tk, k + row0 * P.ldk + w.hk * DK, P.ldk, w.rows, tid);
+  copy_ws<4 * kGateFloats<NM>, 128>(smem_u32(G), P.gates + w.nc * kGates, tid);
   cp_async_commit();
   const auto load = [&](int part) {
-    copy_ws(tu.base, P.U + (w.nc * dvb + part) * L::kU, L::kU, tid, 128);
-    copy_ws(ts.base, P.S + (w.nc * dvb + part) * L::kS, L::kS, tid, 128);
+    copy_ws<L::kU, 128>(tu.base, P.U + (w.nc * dvb + part) * L::kU, tid);
+    copy_ws<L::kS, 128>(ts.base, P.S + (w.nc * dvb + part) * L::kS, tid);
     cp_async_commit();
   };
   load(0);

@@ -55,12 +55,13 @@ blr_status bwd_dk(const Problem& p, const BwdCall& c) {
   else
     BLR_TRY(start("back", back_kernel<TI, DK, NI, NM, 2>, p.B * p.Hv * (p.Dv / 32), 32 * (2 + kLoadWarps),
                   BackSmem<DK, NI, NM, 2>::kBytes, c.stream, p, q, k, d_o, c.ds_last, c.ds0));
-  constexpr int bytes = GradSmem<DK, NI, NM>::kBytes;
+  // 16 warps an SM hide each other's latencies; float32's operands take the registers of 8
+  constexpr int kParts = NM == 3 || DK == 64 ? 2 : 4, bytes = GradSmem<DK, NI, NM, kParts>::kBytes;
   if (p.Hk == p.Hv)
-    return start("grad", grad_kernel<TI, TI, DK, NI, NM>, chunks, 256, bytes, c.stream, p, q, k, v, d_o, dq, dk,
-                 (int64_t)p.Hk, dv, dg, dbeta);
-  BLR_TRY(start("grad", grad_kernel<TI, float, DK, NI, NM>, chunks, 256, bytes, c.stream, p, q, k, v, d_o, p.pq, p.pk,
-                (int64_t)p.Hv, dv, dg, dbeta));
+    return start("grad", grad_kernel<TI, TI, DK, NI, NM, kParts>, chunks, 128 * kParts, bytes, c.stream, p, q, k, v,
+                 d_o, dq, dk, p.Hk, dv, dg, dbeta);
+  BLR_TRY(start("grad", grad_kernel<TI, float, DK, NI, NM, kParts>, chunks, 128 * kParts, bytes, c.stream, p, q, k, v,
+                d_o, p.pq, p.pk, p.Hv, dv, dg, dbeta));
   const int64_t pairs = p.B * p.L * p.Hk * (DK / 2), blocks = (pairs + 255) / 256;
   return start("share", share_kernel<TI>, blocks < 152 * 16 ? blocks : 152 * 16, 256, 0, c.stream,
                (const float*)p.pq, (const float*)p.pk, dq, dk, pairs, p.Hv / p.Hk, DK / 2);

@@ -238,29 +238,46 @@ __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commi
 template <int N>
 __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// A linear copy of `bytes` (a multiple of 16) from the workspace.
-__device__ __forceinline__ void copy_ws(uint32_t dst, const void* src, int bytes, int tid, int threads) {
-  for (int i = tid * 16; i < bytes; i += threads * 16)
-    cp_async16(dst + i, static_cast<const char*>(src) + i, true);
+// A linear copy of BYTES (a multiple of 16) from the workspace by THREADS threads.
+template <int BYTES, int THREADS>
+__device__ __forceinline__ void copy_ws(uint32_t dst, const void* src, int tid) {
+  const char* p = static_cast<const char*>(src) + tid * 16;
+#pragma unroll
+  for (int i = 0; i < BYTES; i += THREADS * 16)
+    if (i + THREADS * 16 <= BYTES || i + tid * 16 < BYTES) cp_async16(dst + tid * 16 + i, p + i, true);
+}
+
+// Calls f(piece, row, column block) for a thread's 16-byte pieces of a 64 x 8 C8 tile: piece i is row
+// 8 (i / (8 C8)) + i % 8, column block (i / 8) % C8, so that a warp reads at least 64 bytes of 8 rows.
+template <int C8, int THREADS, typename F>
+__device__ __forceinline__ void each_piece(int tid, F f) {
+  static_assert(THREADS % (8 * C8) == 0 || (8 * C8) % THREADS == 0, "whole rows of blocks");
+  if constexpr (THREADS >= 8 * C8) {
+    const int r = (tid / (8 * C8)) * 8 + (tid & 7), c8 = (tid >> 3) % C8;
+#pragma unroll
+    for (int j = 0; j < 64; j += THREADS / C8)
+      if (j + THREADS / C8 <= 64 || r + j < 64) f(tid + j * C8, r + j, c8);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 64; j += 8)
+#pragma unroll
+      for (int c = 0; c < C8; c += THREADS / 8) f(j * C8 + tid + 8 * c, j + (tid & 7), c + (tid >> 3));
+  }
 }
 
 // 64 rows of a caller's tensor (row r at p + r ld; rows from `rows` on are zero and not read) as a
-// tile. bfloat16 arrives asynchronously; float32 is taken apart into its planes on the way. 16-byte piece i
-// of the tile is row 8 (i / (8 C8)) + i % 8, column block (i / 8) % C8: a warp reads 64 bytes of 8 rows.
-template <int C8>
+// tile. bfloat16 arrives asynchronously; float32 is taken apart into its planes on the way.
+template <int THREADS, int C8>
 __device__ __forceinline__ void load_rows(const Tile<C8, 1>& t, const __nv_bfloat16* p, int64_t ld, int rows,
-                                          int tid, int threads) {
-  for (int i = tid; i < 64 * C8; i += threads) {
-    const int r = (i / (8 * C8)) * 8 + (i & 7), c8 = (i >> 3) % C8;
+                                          int tid) {
+  each_piece<C8, THREADS>(tid, [&](int i, int r, int c8) {
     const bool real = r < rows;
-    cp_async16(t.base + i * 16, p + (real ? r * ld + c8 * 8 : 0), real);
-  }
+    cp_async16(t.base + i * 16, real ? p + r * ld + c8 * 8 : p, real);
+  });
 }
-template <int C8>
-__device__ __forceinline__ void load_rows(const Tile<C8, 3>& t, const float* p, int64_t ld, int rows, int tid,
-                                          int threads) {
-  for (int i = tid; i < 64 * C8; i += threads) {
-    const int r = (i / (8 * C8)) * 8 + (i & 7), c8 = (i >> 3) % C8;
+template <int THREADS, int C8>
+__device__ __forceinline__ void load_rows(const Tile<C8, 3>& t, const float* p, int64_t ld, int rows, int tid) {
+  each_piece<C8, THREADS>(tid, [&](int i, int r, int c8) {
     float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f), y = x;
     if (r < rows) {
       const float4* s = reinterpret_cast<const float4*>(p + r * ld + c8 * 8);
@@ -276,15 +293,16 @@ __device__ __forceinline__ void load_rows(const Tile<C8, 3>& t, const float* p, 
     for (int q = 0; q < 2; ++q)
       asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(t.base + q * Tile<C8, 3>::kPlane + i * 16),
                    "r"(w[0][q]), "r"(w[1][q]), "r"(w[2][q]), "r"(w[3][q]) : "memory");
-  }
+  });
 }
 
 // Columns [8 c8, 8 c8 + 8 C) of a 64 x 64 tile of the workspace.
-template <int C, int P>
-__device__ __forceinline__ void copy_columns(const Tile<C, P>& t, const char* src, int c8, int tid, int threads) {
+template <int THREADS, int C, int P>
+__device__ __forceinline__ void copy_columns(const Tile<C, P>& t, const char* src, int c8, int tid) {
 #pragma unroll
   for (int p = 0; p < kPl<P>; ++p)
-    for (int i = tid; i < 64 * C; i += threads)
+#pragma unroll
+    for (int i = tid; i < 64 * C; i += THREADS)
       cp_async16(t.base + p * Tile<C, P>::kPlane + i * 16,
                  src + p * Tile<8, P>::kPlane + ((i / (8 * C)) * 8 + c8) * 128 + (i % (8 * C)) * 16, true);
 }
