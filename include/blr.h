@@ -434,6 +434,14 @@ BLR_API blr_status blr_gdr_bwd(const blr_gdr_desc* desc, int flags, const int32_
                                void* ws, size_t ws_bytes, blr_stream_t stream);
 
 /*
+ * Synchronises `stream`, then reads the error word that the kernels of the
+ * forward and backward calls on this workspace recorded: BLR_OK, or
+ * BLR_ERR_TIMEOUT if a bounded wait for a tile's load expired (outputs
+ * undefined). The next forward clears it.
+ */
+BLR_API blr_status blr_gdr_status(const void* ws, size_t ws_bytes, blr_stream_t stream);
+
+/*
  * desc->L recurrent steps on the states of desc->B rows (serving), in float32
  * arithmetic step by step. Needs no workspace.
  * state    dtype of s_prev and s_out: BLR_F32, or BLR_BF16 to halve the states'

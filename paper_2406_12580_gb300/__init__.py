@@ -49,7 +49,7 @@ __all__ = [
     "FAMILY_NONE", "FAMILY_TILED", "FAMILY_SERIAL", "FAMILY_SEGMENTED",
     "BDLRUScan", "library_loaded",
     "GDRDesc", "BLR_GDR_TRAIN", "BLR_GDR_STATE", "blr_gdr_workspace_bytes", "blr_gdr_fwd",
-    "blr_gdr_bwd", "blr_gdr_steps", "blr_adamw_step",
+    "blr_gdr_bwd", "blr_gdr_status", "blr_gdr_steps", "blr_adamw_step",
 ]
 
 
@@ -282,6 +282,11 @@ def blr_gdr_bwd(desc, flags, lengths, d_o, ds_last, q, k, v, g, beta, s0, dq, dk
                               _ptr(dbeta, "dbeta"), _ptr(ds0, "ds0"), _ptr(ws, "ws"), _ws_bytes(ws),
                               _stream(stream)),
            "blr_gdr_bwd")
+
+
+def blr_gdr_status(ws, stream=None) -> int:
+    """Status recorded in the workspace by earlier calls on it (synchronises the stream)."""
+    return int(load().blr_gdr_status(_ptr(ws, "ws"), _ws_bytes(ws), _stream(stream)))
 
 
 def blr_gdr_steps(desc, state, s_prev, q, k, v, g, beta, s_out, o=None, stream=None):

@@ -35,6 +35,25 @@ blr_status cuda_check(cudaError_t e, const char* what) {
   return fail(BLR_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
 }
 
+// cuTensorMapEncodeTiled, through the runtime's driver entry point (the
+// library links only the CUDA runtime).
+blr_status tensor_map_encoder(PFN_cuTensorMapEncodeTiled_v12000* out) {
+  static std::mutex m;
+  static PFN_cuTensorMapEncodeTiled_v12000 fn = nullptr;
+  std::lock_guard<std::mutex> lock(m);
+  if (fn == nullptr) {
+    void* ptr = nullptr;
+    cudaDriverEntryPointQueryResult q = cudaDriverEntryPointSymbolNotFound;
+    const cudaError_t e =
+        cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &ptr, 12000, cudaEnableDefault, &q);
+    if (e != cudaSuccess || q != cudaDriverEntryPointSuccess || ptr == nullptr)
+      return fail(BLR_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
+    fn = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(ptr);
+  }
+  *out = fn;
+  return BLR_OK;
+}
+
 }  // namespace blr
 
 namespace {
@@ -45,6 +64,7 @@ using blr::g_last_error;
 using blr::need;
 using blr::optional;
 using blr::Plan;
+using blr::tensor_map_encoder;
 
 // Shared checks of the problem description; fills `plan` when B, L, D > 0.
 blr_status check_desc(const blr_desc* d, Plan* plan, bool* empty_bd) {
@@ -127,25 +147,6 @@ blr_status persistent_grid(K kernel, int threads, size_t smem, int64_t n_tiles, 
   int64_t g = blocks;
   if (g > n_tiles) g = n_tiles;
   *grid = (unsigned)(g > 0 ? g : 1);
-  return BLR_OK;
-}
-
-// cuTensorMapEncodeTiled, through the runtime's driver entry point (the
-// library links only the CUDA runtime).
-blr_status tensor_map_encoder(PFN_cuTensorMapEncodeTiled_v12000* out) {
-  static std::mutex m;
-  static PFN_cuTensorMapEncodeTiled_v12000 fn = nullptr;
-  std::lock_guard<std::mutex> lock(m);
-  if (fn == nullptr) {
-    void* ptr = nullptr;
-    cudaDriverEntryPointQueryResult q = cudaDriverEntryPointSymbolNotFound;
-    const cudaError_t e =
-        cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &ptr, 12000, cudaEnableDefault, &q);
-    if (e != cudaSuccess || q != cudaDriverEntryPointSuccess || ptr == nullptr)
-      return fail(BLR_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
-    fn = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(ptr);
-  }
-  *out = fn;
   return BLR_OK;
 }
 

@@ -378,7 +378,7 @@ __device__ __forceinline__ uint64_t global_timer_ns() {
 // false once `timeout_ns` has passed (recording kErrTimeout) or another block
 // has recorded a timeout. Every path ends: the wait is bounded both by the
 // global timer and by an iteration count.
-__device__ __noinline__ bool wait_record(const uint32_t* pre, const unsigned long long* agg,
+static __device__ __noinline__ bool wait_record(const uint32_t* pre, const unsigned long long* agg,
                                          uint32_t* err, uint64_t timeout_ns) {
   const uint64_t start = global_timer_ns();
   uint32_t sleep_ns = 16;
@@ -397,7 +397,7 @@ __device__ __noinline__ bool wait_record(const uint32_t* pre, const unsigned lon
 }
 
 // The same wait on a single flag word (the bounded-wait self-test).
-__device__ __noinline__ bool wait_word(const uint32_t* flag, uint32_t* err, uint64_t timeout_ns) {
+static __device__ __noinline__ bool wait_word(const uint32_t* flag, uint32_t* err, uint64_t timeout_ns) {
   const uint64_t start = global_timer_ns();
   uint32_t sleep_ns = 32;
   for (uint32_t iter = 0;; ++iter) {

@@ -32,7 +32,7 @@ blr_status make_layout(const blr_gdr_desc* d, int flags, const GdrSizes& s, Layo
   l->np = d->io == BLR_F32 || (flags & BLR_GDR_STATE) || s.L < kFewSteps ? 2 : 1;
   const size_t tile = (size_t)l->nc * l->np * 64 * 2;  // bytes per column of a tile
   const size_t dk = (size_t)s.Dk, dv = (size_t)s.Dv;
-  size_t o = 0;
+  size_t o = 256;  // the error word
   const auto take = [&](size_t* at, size_t bytes) {
     *at = o;
     o = up(o + bytes);
@@ -70,6 +70,7 @@ Problem make_problem(const blr_gdr_desc* d, const GdrSizes& s, const Layout& l, 
   p.ldv = s.ldv;
   p.scale = d->scale;
   p.lengths = lengths;
+  p.err = reinterpret_cast<uint32_t*>(w);
   p.gates = reinterpret_cast<float*>(w + l.gates);
   p.W = w + l.W;
   p.U = w + l.U;
@@ -80,6 +81,32 @@ Problem make_problem(const blr_gdr_desc* d, const GdrSizes& s, const Layout& l, 
   p.pq = reinterpret_cast<float*>(w + l.pq);
   p.pk = reinterpret_cast<float*>(w + l.pk);
   return p;
+}
+
+// A caller's bfloat16 tensor for TMA: (columns of a step, steps, batch rows) in boxes of 64 x 64, whose
+// rows land under the 128-byte swizzle. Steps past a row's end read as zero.
+blr_status make_map(const GdrSizes& s, const void* base, int64_t cols, int64_t ld, CUtensorMap* map) {
+  PFN_cuTensorMapEncodeTiled_v12000 encode = nullptr;
+  BLR_TRY(blr::tensor_map_encoder(&encode));
+  if ((double)s.L * (double)ld * 2.0 >= (double)((int64_t)1 << 40))
+    return fail(BLR_ERR_UNSUPPORTED, "problem too large for the tiled loads");
+  const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)s.L, (cuuint64_t)s.B};
+  const cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)ld * 2 * (cuuint64_t)s.L};
+  const cuuint32_t box[3] = {64u, 64u, 1u}, step[3] = {1u, 1u, 1u};
+  const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, step,
+                            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return fail(BLR_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
+  return BLR_OK;
+}
+
+blr_status make_maps(const blr_gdr_desc* d, const GdrSizes& s, const void* q, const void* k, const void* v,
+                     const void* d_o, blr::gdr::Maps* m) {
+  if (d->io != BLR_BF16) return BLR_OK;
+  BLR_TRY(make_map(s, q, s.Hk * s.Dk, s.ldq, &m->q));
+  BLR_TRY(make_map(s, k, s.Hk * s.Dk, s.ldk, &m->k));
+  BLR_TRY(make_map(s, v, s.Hv * s.Dv, s.ldv, &m->v));
+  return d_o == nullptr ? BLR_OK : make_map(s, d_o, s.Hv * s.Dv, s.Hv * s.Dv, &m->d_o);
 }
 
 blr_status check_inputs(const blr_gdr_desc* d, int flags, const int32_t* lengths, const void* q, const void* k,
@@ -133,7 +160,8 @@ blr_status blr_gdr_fwd(const blr_gdr_desc* desc, int flags, const int32_t* lengt
   BLR_TRY(check_inputs(desc, flags, lengths, q, k, v, g, beta, s0, ws, ws_bytes, l.bytes));
   BLR_TRY(blr::need(o, "o", 16));
   const Problem p = make_problem(desc, s, l, lengths, ws);
-  const blr::gdr::FwdCall c{(int)s.Dk, (flags & BLR_GDR_TRAIN) != 0, q, k, v, g, beta, s0, o, s_last, stream};
+  blr::gdr::FwdCall c{(int)s.Dk, (flags & BLR_GDR_TRAIN) != 0, q, k, v, g, beta, s0, o, s_last, stream, {}};
+  BLR_TRY(make_maps(desc, s, q, k, v, nullptr, &c.maps));
   if (desc->io == BLR_F32) return blr::gdr::fwd_f32(p, c);
   return l.np == 2 ? blr::gdr::fwd_bf16_state(p, c) : blr::gdr::fwd_bf16(p, c);
 }
@@ -160,7 +188,18 @@ blr_status blr_gdr_bwd(const blr_gdr_desc* desc, int flags, const int32_t* lengt
   BLR_TRY(blr::need(dg, "dg", e));
   BLR_TRY(blr::need(dbeta, "dbeta", e));
   const Problem p = make_problem(desc, s, l, lengths, ws);
-  const blr::gdr::BwdCall c{(int)s.Dk, d_o, ds_last, q, k, v, dq, dk, dv, dg, dbeta, ds0, stream};
+  blr::gdr::BwdCall c{(int)s.Dk, d_o, ds_last, q, k, v, dq, dk, dv, dg, dbeta, ds0, stream, {}};
+  BLR_TRY(make_maps(desc, s, q, k, v, d_o, &c.maps));
   if (desc->io == BLR_F32) return blr::gdr::bwd_f32(p, c);
   return l.np == 2 ? blr::gdr::bwd_bf16_state(p, c) : blr::gdr::bwd_bf16(p, c);
+}
+
+blr_status blr_gdr_status(const void* ws, size_t ws_bytes, blr_stream_t stream) {
+  BLR_TRY(blr::need(ws, "ws", 16));
+  if (ws_bytes < 4) return fail(BLR_ERR_INVALID_ARG, "ws_bytes=%zu", ws_bytes);
+  uint32_t err = 0;
+  BLR_TRY(blr::cuda_check(cudaMemcpyAsync(&err, ws, 4, cudaMemcpyDeviceToHost, stream), "cudaMemcpyAsync"));
+  BLR_TRY(blr::cuda_check(cudaStreamSynchronize(stream), "cudaStreamSynchronize"));
+  if (err & blr::kErrTimeout) return fail(BLR_ERR_TIMEOUT, "a wait for a load ran out");
+  return BLR_OK;
 }

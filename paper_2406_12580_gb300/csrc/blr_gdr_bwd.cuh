@@ -10,7 +10,7 @@
 // product of what the sums above already need.
 #pragma once
 
-#include "blr_gdr_tile.cuh"
+#include "blr_gdr_fwd.cuh"
 
 namespace blr {
 namespace gdr {
@@ -18,31 +18,36 @@ namespace gdr {
 template <int DK, int NI>
 struct DuSmem {
   static constexpr int kQ = Tile<DK / 8, NI>::kBytes, kO = Tile<8, NI>::kBytes;
-  static constexpr int kBytes = 2 * kQ + kO + kGates * 4;
+  static constexpr int kBytes = 2 * kQ + kO + kGates * 4 + 16;
 };
 
 // The part of dU that does not hang on later chunks, scale P^T dO, for all chunks at once.
 template <typename TI, int DK, int NI, int NM>
 __global__ void __launch_bounds__(128)
-du_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k, const TI* __restrict__ d_o) {
-  extern __shared__ __align__(128) unsigned char smem[];
+du_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restrict__ q, const TI* __restrict__ k,
+          const TI* __restrict__ d_o) {
+  extern __shared__ __align__(1024) unsigned char smem[];
   using L = DuSmem<DK, NI>;
   const Where w = locate(P);
   if (w.rows <= 0) return;
-  const uint32_t base = smem_u32(smem);
-  const Tile<DK / 8, NI> tq{base}, tk{base + L::kQ};
-  const Tile<8, NI> to{base + 2 * L::kQ};
+  const uint32_t base = smem_addr(smem);
+  const InTile<DK / 8, NI> tq{base}, tk{base + L::kQ};
+  const InTile<8, NI> to{base + 2 * L::kQ};
   float* G = reinterpret_cast<float*>(smem + 2 * L::kQ + L::kO);
+  uint64_t* bar = reinterpret_cast<uint64_t*>(G + kGates);
   const int tid = threadIdx.x, warp = tid >> 5, l = tid & 31;
-  const int64_t row0 = w.step, ldo = (int64_t)P.Hv * P.Dv;
-  const TI* src = d_o + row0 * ldo + (int64_t)w.h * P.Dv;
-  load_rows<128>(tq, q + row0 * P.ldq + w.hk * DK, P.ldq, w.rows, tid);
-  load_rows<128>(tk, k + row0 * P.ldk + w.hk * DK, P.ldk, w.rows, tid);
-  load_rows<128>(to, src, ldo, w.rows, tid);
-  copy_ws<4 * kGateFloats<NM>, 128>(smem_u32(G), P.gates + w.nc * kGates, tid);
-  cp_async_commit();
-  cp_async_wait<0>();
+  const int64_t ldo = (int64_t)P.Hv * P.Dv;
+  if (tid == 0) {
+    mbar_init(bar, 1);
+    fence_mbar_init();
+    mbar_arrive_expect_tx(bar, 2 * tma_bytes<NI>(L::kQ) + tma_bytes<NI>(L::kO) + 4 * kGateFloats<NM>);
+    bulk_load(smem_addr(G), P.gates + w.nc * kGates, 4 * kGateFloats<NM>, bar);
+  }
+  load_rows<128>(tq, &M.q, bar, q, P.ldq, w.hk * DK, w.t, w.b, P.L, w.rows, tid);
+  load_rows<128>(tk, &M.k, bar, k, P.ldk, w.hk * DK, w.t, w.b, P.L, w.rows, tid);
+  load_rows<128>(to, &M.d_o, bar, d_o, ldo, w.h * P.Dv, w.t, w.b, P.L, w.rows, tid);
   __syncthreads();
+  mbar_wait(bar, 0, P.err);
   const int r0 = 16 * warp + (l >> 2), c0 = 2 * (l & 3);
   uint32_t p[4][kPl<NM>][4];  // scale P^T: rows j (this warp's), columns i >= j
   {
@@ -74,10 +79,10 @@ du_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k, c
   for (int part = 0; part < dvb; ++part) {
     if (part > 0) {
       __syncthreads();
-      load_rows<128>(to, src + 64 * part, ldo, w.rows, tid);
-      cp_async_commit();
-      cp_async_wait<0>();
-      __syncthreads();
+      if (tid == 0) mbar_arrive_expect_tx(bar, tma_bytes<NI>(L::kO));
+      load_rows<128>(to, &M.d_o, bar, d_o, ldo, w.h * P.Dv + 64 * part, w.t, w.b, P.L, w.rows, tid);
+      if constexpr (NI == 3) __syncthreads();
+      mbar_wait(bar, part & 1, P.err);
     }
     float acc[8][4] = {};
 #pragma unroll
@@ -102,20 +107,22 @@ du_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k, c
 
 template <int DK, int NI, int NM, int WARPS>
 struct BackSmem {
-  static constexpr int kW = Tile<DK / 8, NM>::kBytes, kK = Tile<DK / 8, NI>::kBytes, kO = Tile<2 * WARPS, NI>::kBytes,
+  // TMA brings 64 columns of dO whichever part of them the block takes
+  static constexpr int kO8 = NI == 1 ? 8 : 2 * WARPS;
+  static constexpr int kW = Tile<DK / 8, NM>::kBytes, kK = Tile<DK / 8, NI>::kBytes, kO = Tile<kO8, NI>::kBytes,
                        kU = Tile<2 * WARPS, NM>::kBytes;
-  static constexpr int kStage = kW + 2 * kK + kO + kU + kGates * 4;
+  static constexpr int kStage = 2 * kK + kO + kW + kU + kGateBytes<NI>;
   static constexpr int kStages = WARPS == 2 && 3 * kStage <= 227 * 1024 ? 3 : 2;
-  static constexpr int kBytes = kStages * kStage;
+  static constexpr int kBytes = kStages * kStage + 16 * kStages;
 };
 
 // The states' gradients from chunk to chunk, last to first: as chain_kernel, a warp holds dS^T of 16
-// columns in accumulators, and two more warps load.
+// columns in accumulators, and further warps load.
 template <typename TI, int DK, int NI, int NM, int WARPS>
-__global__ void __launch_bounds__(32 * (WARPS + kLoadWarps), WARPS == 4 && NM < 3 ? 2 : 1)
-back_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k, const TI* __restrict__ d_o,
-            const float* __restrict__ ds_last, float* __restrict__ ds0) {
-  extern __shared__ __align__(128) unsigned char smem[];
+__global__ void __launch_bounds__(32 * (WARPS + kLoadWarps<NI>), WARPS == 4 && NM < 3 ? 2 : 1)
+back_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restrict__ q, const TI* __restrict__ k,
+            const TI* __restrict__ d_o, const float* __restrict__ ds_last, float* __restrict__ ds0) {
+  extern __shared__ __align__(1024) unsigned char smem[];
   using L = BackSmem<DK, NI, NM, WARPS>;
   const int parts = P.Dv / (16 * WARPS), dvb = P.Dv / 64;
   const uint32_t bh = blockIdx.x / parts;
@@ -124,29 +131,35 @@ back_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k,
   const Where w0 = locate(P, bh, 0);
   const int chunks = (int)((w0.len + kC - 1) / kC);
   const int block = part * WARPS / 4, c8 = 2 * ((part * WARPS) & 3);
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kStages * L::kStage);
+  uint64_t* empty = full + L::kStages;
+  init_ring(full, empty, L::kStages, NI == 1 ? 1 : 1 + 32 * kLoadWarps<NI>, WARPS);
   if (warp >= WARPS) {  // loads
     const int tid = threadIdx.x - 32 * WARPS;
+    if (NI == 1 && tid > 0) return;
     const int64_t ldo = (int64_t)P.Hv * P.Dv;
-    const auto load = [&](int c) {
-      if (c >= 0) {
-        const uint32_t st = smem_u32(smem) + (uint32_t)(c % L::kStages) * L::kStage;
-        const int64_t nc = w0.nc + c, left = w0.len - (int64_t)c * kC, row0 = w0.step + (int64_t)c * kC;
-        const int rows = (int)(left < kC ? left : kC);
-        copy_ws<L::kW, 32 * kLoadWarps>(st, P.W + nc * L::kW, tid);
-        load_rows<32 * kLoadWarps>(Tile<DK / 8, NI>{st + L::kW}, k + row0 * P.ldk + w0.hk * DK, P.ldk, rows, tid);
-        load_rows<32 * kLoadWarps>(Tile<DK / 8, NI>{st + L::kW + L::kK}, q + row0 * P.ldq + w0.hk * DK, P.ldq, rows, tid);
-        load_rows<32 * kLoadWarps>(Tile<2 * WARPS, NI>{st + L::kW + 2 * L::kK}, d_o + row0 * ldo + (int64_t)w0.h * P.Dv + 16 * WARPS * part, ldo, rows, tid);
-        copy_columns<32 * kLoadWarps>(Tile<2 * WARPS, NM>{st + L::kW + 2 * L::kK + L::kO}, P.dU + (nc * dvb + block) * Tile<8, NM>::kBytes, c8, tid);
-        copy_ws<1024, 32 * kLoadWarps>(st + L::kW + 2 * L::kK + L::kO + L::kU, P.gates + nc * kGates, tid);
+    for (int n = 0; n < chunks; ++n) {
+      const int c = chunks - 1 - n, s = n % L::kStages;
+      const uint32_t st = smem_addr(smem) + s * L::kStage;
+      const int64_t nc = w0.nc + c, left = w0.len - (int64_t)c * kC, t = w0.t + (int64_t)c * kC;
+      const int rows = (int)(left < kC ? left : kC);
+      if (n >= L::kStages) mbar_wait(&empty[s], (n / L::kStages - 1) & 1, P.err);
+      constexpr int kIn = 2 * L::kK + L::kO;
+      if (tid == 0) {
+        mbar_arrive_expect_tx(&full[s], tma_bytes<NI>(kIn) + L::kW + L::kU + 4 * kGateFloats<NM>);
+        bulk_load(st + kIn, P.W + nc * L::kW, L::kW, &full[s]);
+        bulk_columns(Tile<2 * WARPS, NM>{st + kIn + L::kW}, P.dU + (nc * dvb + block) * Tile<8, NM>::kBytes, c8,
+                     &full[s]);
+        bulk_load(st + kIn + L::kW + L::kU, P.gates + nc * kGates, 4 * kGateFloats<NM>, &full[s]);
       }
-      cp_async_commit();
-    };
-#pragma unroll
-    for (int i = 0; i < L::kStages - 1; ++i) load(chunks - 1 - i);
-    for (int c = chunks - 1; c >= 0; --c) {
-      cp_async_wait<L::kStages - 2>();
-      __syncthreads();
-      load(c - (L::kStages - 1));
+      load_rows<32 * kLoadWarps<NI>>(InTile<DK / 8, NI>{st}, &M.k, &full[s], k, P.ldk, w0.hk * DK, t, w0.b, P.L, rows,
+                                     tid);
+      load_rows<32 * kLoadWarps<NI>>(InTile<DK / 8, NI>{st + L::kK}, &M.q, &full[s], q, P.ldq, w0.hk * DK, t, w0.b,
+                                     P.L, rows, tid);
+      load_rows<32 * kLoadWarps<NI>>(InTile<L::kO8, NI>{st + 2 * L::kK}, &M.d_o, &full[s], d_o, ldo,
+                                     w0.h * P.Dv + (NI == 1 ? 64 * block : 16 * WARPS * part), t, w0.b, P.L, rows,
+                                     tid);
+      if constexpr (NI == 3) mbar_arrive(&full[s]);
     }
     return;
   }
@@ -159,15 +172,16 @@ back_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k,
       S[nb][e] = ds_last == nullptr
                      ? 0.0f
                      : ds_last[((int64_t)bh * DK + 8 * nb + row + (e & 1)) * P.Dv + col + 8 * (e >> 1)];
-  for (int c = chunks - 1; c >= 0; --c) {
-    __syncthreads();
-    const int s = c % L::kStages;
-    const uint32_t st = smem_u32(smem) + s * L::kStage;
-    const Tile<DK / 8, NM> tw{st};
-    const Tile<DK / 8, NI> tk{st + L::kW}, tq{st + L::kW + L::kK};
-    const Tile<2 * WARPS, NI> to{st + L::kW + 2 * L::kK};
-    const Tile<2 * WARPS, NM> tu{st + L::kW + 2 * L::kK + L::kO};
-    const float* G = reinterpret_cast<const float*>(smem + s * L::kStage + L::kW + 2 * L::kK + L::kO + L::kU);
+  for (int n = 0; n < chunks; ++n) {
+    const int c = chunks - 1 - n, s = n % L::kStages;
+    mbar_wait(&full[s], (n / L::kStages) & 1, P.err);
+    const uint32_t st = smem_addr(smem) + s * L::kStage;
+    const InTile<DK / 8, NI> tk{st}, tq{st + L::kK};
+    const InTile<L::kO8, NI> to{st + 2 * L::kK};
+    const Tile<DK / 8, NM> tw{st + 2 * L::kK + L::kO};
+    const Tile<2 * WARPS, NM> tu{st + 2 * L::kK + L::kO + L::kW};
+    const float* G = reinterpret_cast<const float*>(smem + s * L::kStage + 2 * L::kK + L::kO + L::kW + L::kU);
+    const int o8 = (NI == 1 ? c8 : 0) + 2 * warp;  // this warp's columns of dO
     const int64_t tile = (w0.nc + c) * dvb + block;
     // K dS': columns are the chunk's steps
     float u[8][4] = {};
@@ -207,7 +221,7 @@ back_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k,
         [&](int s, auto& b) {
           const int kk = s / (DK / 64), n0 = 8 * (s % (DK / 64));
           uint32_t fo[kPl<NI>][4], a[kPl<NM>][4];
-          to.a_t(2 * warp, 2 * kk, fo);
+          to.a_t(o8, 2 * kk, fo);
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             const float2 up = *reinterpret_cast<const float2*>(&G[kUp + 16 * kk + 8 * h + row]);
@@ -244,8 +258,8 @@ back_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k,
             const int i = l >> 3;
 #pragma unroll
             for (int p = 0; p < kPl<NM>; ++p)
-              ldsm_t(tu.at(p, 2 * kk + (i >> 1), 2 * warp + (i & 1)) + (l & 7) * 16, f[0][p][0], f[0][p][1],
-                     f[1][p][0], f[1][p][1]);
+              ldsm_t(tu.at(p, 2 * kk + (i >> 1), 2 * warp + (i & 1), l & 7), f[0][p][0], f[0][p][1], f[1][p][0],
+                     f[1][p][1]);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               const float2 down = *reinterpret_cast<const float2*>(&G[kDown + 16 * kk + 8 * h + row]);
@@ -269,6 +283,8 @@ back_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k,
             mma_p<NM, NM>(S[n0 + 2 * nn + 1], a, b[nn][1]);
           }
         });
+    __syncwarp();
+    if (l == 0) mbar_arrive(&empty[s]);
   }
   if (ds0 != nullptr) {
 #pragma unroll
@@ -288,9 +304,9 @@ struct GradSmem {
   // gates; row sums by column part; column sums by row group; <S, dS'> by warp
   static constexpr int kFloats = kGates + PARTS * 5 * 64 + 4 * 64 + 4 * PARTS;
   // Dk 64: two blocks an SM overlap each other; Dk 128: one, whose next 64 columns of Dv load meanwhile
-  static constexpr int kStages = DK == 128 && kFixed + 2 * kStage + 4 * kFloats <= 227 * 1024 ? 2 : 1;
+  static constexpr int kStages = DK == 128 && kFixed + 2 * kStage + 4 * kFloats + 24 <= 227 * 1024 ? 2 : 1;
   static constexpr int kTiles = kFixed + kStages * kStage;
-  static constexpr int kBytes = kTiles + 4 * kFloats;
+  static constexpr int kBytes = kTiles + 4 * kFloats + 24;
 };
 
 __device__ __forceinline__ float quad_sum(float x) {  // over the 4 lanes of a fragment row
@@ -329,11 +345,11 @@ __device__ __forceinline__ float dot16(uint32_t a, uint32_t b) {
 // PARTS parts of the columns of each product.
 template <typename TI, typename TG, int DK, int NI, int NM, int PARTS>
 __global__ void __launch_bounds__(128 * PARTS, PARTS == 4 || NM == 3 ? 1 : 2)
-grad_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k, const TI* __restrict__ v,
+grad_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restrict__ q, const TI* __restrict__ k, const TI* __restrict__ v,
             const TI* __restrict__ d_o, TG* __restrict__ dq, TG* __restrict__ dk, int heads, TI* __restrict__ dv,
             TI* __restrict__ dg, TI* __restrict__ dbeta) {
   // dq, dk: `heads` heads a step (the key heads, or the value heads where a later kernel sums them)
-  extern __shared__ __align__(128) unsigned char smem[];
+  extern __shared__ __align__(1024) unsigned char smem[];
   using L = GradSmem<DK, NI, NM, PARTS>;
   constexpr int THREADS = 128 * PARTS;
   constexpr int NB = DK / (8 * PARTS), VB = 8 / PARTS;  // 8-column blocks of a warp's part of Dk, of 64 columns
@@ -357,47 +373,57 @@ grad_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k,
     }
   }
   if (w.rows <= 0) return;
-  const uint32_t base = smem_u32(smem);
-  const Tile<DK / 8, NI> tq{base}, tk{base + L::kQ};
+  const uint32_t base = smem_addr(smem);
+  const InTile<DK / 8, NI> tq{base}, tk{base + L::kQ};
   const Tile<8, NM> tt{base + 2 * L::kQ};
   float* G = reinterpret_cast<float*>(smem + L::kTiles);
   float* bt = G + kBeta;
   float* rows = G + kGates;             // [part][5][64]: dbeta without S, x1.q, x2.k, x3.k, row sums
   float* cols = rows + PARTS * 5 * 64;  // [rg][64]
   float* dots = cols + 4 * 64;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(dots + 4 * PARTS);  // of the stages; of Q and K
   const int64_t row0 = w.step, ldo = (int64_t)P.Hv * P.Dv;
   const int dvb = P.Dv / 64;
-  const TI *vsrc = v + row0 * P.ldv + w.h * P.Dv, *osrc = d_o + row0 * ldo + w.h * P.Dv;
-  const auto load = [&](int part) {
-    if (part < dvb) {
-      const uint32_t st = base + L::kFixed + (part % L::kStages) * L::kStage;
-      const int64_t tile = w.nc * dvb + part;
-      copy_ws<L::kM, THREADS>(st + 2 * L::kI + L::kM, P.dU + tile * L::kM, tid);
-      load_rows<THREADS>(Tile<8, NI>{st}, vsrc + 64 * part, P.ldv, w.rows, tid);
-      load_rows<THREADS>(Tile<8, NI>{st + L::kI}, osrc + 64 * part, ldo, w.rows, tid);
-      copy_ws<L::kM, THREADS>(st + 2 * L::kI, P.U + tile * L::kM, tid);
-      copy_ws<L::kS, THREADS>(st + 2 * L::kI + 2 * L::kM, P.S + tile * L::kS, tid);
-      copy_ws<L::kS, THREADS>(st + 2 * L::kI + 2 * L::kM + L::kS, P.dS + tile * L::kS, tid);
+  const auto load = [&](int part, bool first) {
+    if (part >= dvb) return;
+    const int s = part % L::kStages;
+    const uint32_t st = base + L::kFixed + s * L::kStage;
+    const int64_t tile = w.nc * dvb + part;
+    if (tid == 0) {
+      mbar_arrive_expect_tx(&bars[s], 2 * tma_bytes<NI>(L::kI) + 2 * L::kM + 2 * L::kS +
+                                          (first ? L::kM + 4 * kGateFloats<NM> : 0));
+      if (first) {
+        bulk_load(tt.base, P.T + w.nc * L::kM, L::kM, &bars[s]);
+        bulk_load(smem_addr(G), P.gates + w.nc * kGates, 4 * kGateFloats<NM>, &bars[s]);
+      }
+      bulk_load(st + 2 * L::kI + L::kM, P.dU + tile * L::kM, L::kM, &bars[s]);
+    }
+    load_rows<THREADS>(InTile<8, NI>{st}, &M.v, &bars[s], v, P.ldv, w.h * P.Dv + 64 * part, w.t, w.b, P.L, w.rows, tid);
+    load_rows<THREADS>(InTile<8, NI>{st + L::kI}, &M.d_o, &bars[s], d_o, ldo, w.h * P.Dv + 64 * part, w.t, w.b, P.L,
+                       w.rows, tid);
+    if (tid == 0) {
+      bulk_load(st + 2 * L::kI, P.U + tile * L::kM, L::kM, &bars[s]);
+      bulk_load(st + 2 * L::kI + 2 * L::kM, P.S + tile * L::kS, L::kS, &bars[s]);
+      bulk_load(st + 2 * L::kI + 2 * L::kM + L::kS, P.dS + tile * L::kS, L::kS, &bars[s]);
     }
   };
-  copy_ws<4 * kGateFloats<NM>, THREADS>(smem_u32(G), P.gates + w.nc * kGates, tid);
-  copy_ws<L::kM, THREADS>(tt.base, P.T + w.nc * L::kM, tid);
-  load(0);
-  if (L::kStages == 2) {
-    cp_async_commit();
-    load(1);
+  if (tid == 0) {
+    for (int i = 0; i <= L::kStages; ++i) mbar_init(&bars[i], 1);
+    fence_mbar_init();
+    mbar_arrive_expect_tx(&bars[L::kStages], 2 * tma_bytes<NI>(L::kQ));
   }
-  load_rows<THREADS>(tq, q + row0 * P.ldq + w.hk * DK, P.ldq, w.rows, tid);
-  load_rows<THREADS>(tk, k + row0 * P.ldk + w.hk * DK, P.ldk, w.rows, tid);
-  cp_async_commit();
+  load(0, true);
+  if (L::kStages == 2) load(1, false);
+  load_rows<THREADS>(tq, &M.q, &bars[L::kStages], q, P.ldq, w.hk * DK, w.t, w.b, P.L, w.rows, tid);
+  load_rows<THREADS>(tk, &M.k, &bars[L::kStages], k, P.ldk, w.hk * DK, w.t, w.b, P.L, w.rows, tid);
+  __syncthreads();
   const int rr = l >> 2, c0 = 2 * (l & 3), r0 = 16 * rg + rr;
   float x1[NB][4] = {}, x2[NB][4] = {}, x3[NB][4] = {}, dp[VB][4] = {}, da[VB][4] = {};
   float vdot[2] = {0.0f, 0.0f}, sdot = 0.0f;
   for (int part = 0; part < dvb; ++part) {
-    cp_async_wait<L::kStages - 1>();
-    __syncthreads();
+    mbar_wait(&bars[part % L::kStages], (part / L::kStages) & 1, P.err);
     const uint32_t st = base + L::kFixed + (part % L::kStages) * L::kStage;
-    const Tile<8, NI> tv{st}, to{st + L::kI};
+    const InTile<8, NI> tv{st}, to{st + L::kI};
     const Tile<8, NM> tu{st + 2 * L::kI}, tdu{st + 2 * L::kI + L::kM};
     const Tile<DK / 8, NM> ts{st + 2 * L::kI + 2 * L::kM}, tds{st + 2 * L::kI + 2 * L::kM + L::kS};
     {  // dR, dV
@@ -464,12 +490,12 @@ grad_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k,
         mma_p<NM, NM>(da[2 * nn + 1], ar, b[1]);
       }
     }
+    fence_proxy_async_smem();
     __syncthreads();
-    load(part + L::kStages);
-    cp_async_commit();
+    load(part + L::kStages, false);
+    if (NI == 3 && part + L::kStages < dvb) __syncthreads();
   }
-  cp_async_wait<0>();
-  __syncthreads();
+  mbar_wait(&bars[L::kStages], 0, P.err);
   // the stages have been read: scale dP o D and M take their place
   const Tile<8, NM> tp{base + L::kFixed}, tm{base + L::kFixed + L::kM};
   {

@@ -99,8 +99,10 @@ __device__ __forceinline__ void inverse_column(const float* A, float* inv) {
 template <int DK, int NI, int NM>
 struct PrepareSmem {
   static constexpr int kK = Tile<DK / 8, NI>::kBytes, kV = Tile<8, NI>::kBytes;
-  static constexpr int kSquare = 64 * kLd * 4;
-  static constexpr int kBytes = kK + kV + 2 * kSquare + kGates * 4;
+  static constexpr int kSquare = 64 * kLd * 4;  // A, whose place V's tiles take; the inverse
+  static constexpr int kSlots = kSquare / kV;
+  static constexpr int kFloats = kGates + 64;
+  static constexpr int kBytes = kK + 2 * kSquare + 4 * kFloats + 16;
 };
 
 // T, W = T diag(beta gamma) K (stored negated), U0 = T diag(beta) V of one chunk of one head. A warp
@@ -108,33 +110,41 @@ struct PrepareSmem {
 // products of two planes at least, whatever the operands of the rest.
 template <typename TI, int DK, int NI, int NM, bool TRAIN>
 __global__ void __launch_bounds__(128)
-prepare_kernel(const Problem P, const TI* __restrict__ k, const TI* __restrict__ v, const TI* __restrict__ g,
-               const TI* __restrict__ beta) {
-  extern __shared__ __align__(128) unsigned char smem[];
+prepare_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restrict__ k, const TI* __restrict__ v,
+               const TI* __restrict__ g, const TI* __restrict__ beta) {
+  extern __shared__ __align__(1024) unsigned char smem[];
   using L = PrepareSmem<DK, NI, NM>;
-  const Tile<DK / 8, NI> tk{smem_u32(smem)};
-  const Tile<8, NI> tv{smem_u32(smem) + L::kK};
-  float* A = reinterpret_cast<float*>(smem + L::kK + L::kV);
+  const InTile<DK / 8, NI> tk{smem_addr(smem)};
+  float* A = reinterpret_cast<float*>(smem + L::kK);
   float* inv = A + 64 * kLd;
   float* sg = inv + 64 * kLd;  // the gates
-  float* sb = sg + 64;
+  float* sb = sg + kBeta;
+  float* sw = sg + kGates;     // -beta gamma
+  uint64_t* bars = reinterpret_cast<uint64_t*>(sw + 64);
   const Where w = locate(P);
+  if (blockIdx.x == 0 && threadIdx.x == 0) *P.err = 0;
   if (w.rows <= 0) return;
   const int tid = threadIdx.x, warp = tid >> 5, l = tid & 31;
-  const int64_t row0 = w.step;
-  load_rows<128>(tk, k + row0 * P.ldk + w.hk * DK, P.ldk, w.rows, tid);
-  load_rows<128>(tv, v + row0 * P.ldv + (int64_t)w.h * P.Dv, P.ldv, w.rows, tid);
-  cp_async_commit();
+  if (tid == 0) {
+    mbar_init(&bars[0], 1);
+    mbar_init(&bars[1], 1);
+    fence_mbar_init();
+    mbar_arrive_expect_tx(&bars[0], tma_bytes<NI>(L::kK));
+  }
+  load_rows<128>(tk, &M.k, &bars[0], k, P.ldk, w.hk * DK, w.t, w.b, P.L, w.rows, tid);
   if (warp == 0) {
-    load_gates<NM>(g + row0 * P.Hv + w.h, beta + row0 * P.Hv + w.h, P.Hv, w.rows, sg);
+    const int64_t at = w.step * P.Hv + w.h;
+    load_gates<NM>(g + at, beta + at, P.Hv, w.rows, sg);
     __syncwarp();
     float* out = P.gates + w.nc * kGates;
 #pragma unroll
     for (int i = 0; i < kGateFloats<NM>; i += 64)
       *reinterpret_cast<float2*>(out + i + 2 * l) = *reinterpret_cast<float2*>(sg + i + 2 * l);
+    sw[2 * l] = -sb[2 * l] * sg[kUp + 2 * l];
+    sw[2 * l + 1] = -sb[2 * l + 1] * sg[kUp + 2 * l + 1];
   }
-  cp_async_wait<0>();
   __syncthreads();
+  mbar_wait(&bars[0], 0, P.err);
   const int r0 = 16 * warp + (l >> 2), c0 = 2 * (l & 3);
   {  // A
     float acc[8][4] = {};
@@ -185,6 +195,7 @@ prepare_kernel(const Problem P, const TI* __restrict__ k, const TI* __restrict__
   if (warp == 0) inverse_column<0, kInv>(A, inv);
   else if (warp == 1) inverse_column<1, kInv>(A, inv);
   else if (warp == 2) inverse_column<2, kInv>(A, inv);
+  fence_proxy_async_smem();
   __syncthreads();
   // rows of T, scaled by column, as left operands
   const auto rows_of_t = [&](int kk, const float* scale, uint32_t (&a)[kPl<NM>][4]) {
@@ -192,7 +203,7 @@ prepare_kernel(const Problem P, const TI* __restrict__ k, const TI* __restrict__
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int j = 16 * kk + 8 * h + c0;
-      const float s0 = scale == nullptr ? 1.0f : scale[j], s1 = scale == nullptr ? 1.0f : scale[j + 1];
+      const float s0 = scale[j], s1 = scale[j + 1];
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const float2 t = *reinterpret_cast<const float2*>(&inv[(r0 + 8 * e) * kLd + j]);
@@ -211,84 +222,108 @@ prepare_kernel(const Problem P, const TI* __restrict__ k, const TI* __restrict__
         store_block<8, NM>(t, 2 * warp + e, nb, x.x, x.y);
       }
   }
-  // U0, 64 columns of V at a time
   const int dvb = P.Dv / 64;
-  for (int part = 0; part < dvb; ++part) {
-    if (part > 0) {
-      __syncthreads();
-      load_rows<128>(tv, v + row0 * P.ldv + (int64_t)w.h * P.Dv + 64 * part, P.ldv, w.rows, tid);
-      cp_async_commit();
-      cp_async_wait<0>();
+  uint32_t phase = 0;
+  for (int first = 0; first < dvb; first += L::kSlots) {
+    const int count = min(L::kSlots, dvb - first);
+    if (first > 0) {
+      fence_proxy_async_smem();
       __syncthreads();
     }
-    float acc[8][4] = {};
+    if (tid == 0) mbar_arrive_expect_tx(&bars[1], tma_bytes<NI>(count * L::kV));
+    for (int i = 0; i < count; ++i)
+      load_rows<128>(InTile<8, NI>{smem_addr(A) + i * L::kV}, &M.v, &bars[1], v, P.ldv, w.h * P.Dv + 64 * (first + i),
+                     w.t, w.b, P.L, w.rows, tid);
+    if (first == 0) {  // -W, while V is on its way
+      char* wt = P.W + w.nc * Tile<DK / 8, NM>::kBytes;
 #pragma unroll
-    for (int kk = 0; kk < 4; ++kk)
-      if (kk <= warp) {
-        uint32_t a[kPl<NM>][4];
-        rows_of_t(kk, sb, a);
+      for (int half = 0; half < DK / 64; ++half) {
+        float acc[8][4] = {};
 #pragma unroll
-        for (int nn = 0; nn < 4; ++nn) {
-          uint32_t b[2][kPl<NI>][2];
-          tv.b(2 * nn, 2 * kk, b);
-          mma_p<NM, NI>(acc[2 * nn], a, b[0]);
-          mma_p<NM, NI>(acc[2 * nn + 1], a, b[1]);
+        for (int kk = 0; kk < 4; ++kk)
+          if (kk <= warp) {
+            uint32_t a[kPl<NM>][4];
+            rows_of_t(kk, sw, a);
+#pragma unroll
+            for (int nn = 0; nn < 4; ++nn) {
+              uint32_t b[2][kPl<NI>][2];
+              tk.b(8 * half + 2 * nn, 2 * kk, b);
+              mma_p<NM, NI>(acc[2 * nn], a, b[0]);
+              mma_p<NM, NI>(acc[2 * nn + 1], a, b[1]);
+            }
+          }
+#pragma unroll
+        for (int nb = 0; nb < 8; ++nb) {
+          store_block<DK / 8, NM>(wt, 2 * warp, 8 * half + nb, acc[nb][0], acc[nb][1]);
+          store_block<DK / 8, NM>(wt, 2 * warp + 1, 8 * half + nb, acc[nb][2], acc[nb][3]);
         }
       }
-    char* u = P.U + (w.nc * dvb + part) * Tile<8, NM>::kBytes;
-#pragma unroll
-    for (int nb = 0; nb < 8; ++nb) {
-      store_block<8, NM>(u, 2 * warp, nb, acc[nb][0], acc[nb][1]);
-      store_block<8, NM>(u, 2 * warp + 1, nb, acc[nb][2], acc[nb][3]);
     }
-  }
-  // -W: the column scale becomes -beta gamma
-  __syncthreads();
-  if (tid < 64) sb[tid] *= -sg[kUp + tid];
-  __syncthreads();
-  char* wt = P.W + w.nc * Tile<DK / 8, NM>::kBytes;
+    if constexpr (NI == 3) __syncthreads();
+    mbar_wait(&bars[1], phase, P.err);
+    phase ^= 1;
+    for (int i = 0; i < count; ++i) {  // U0
+      const InTile<8, NI> tv{smem_addr(A) + i * L::kV};
+      float acc[8][4] = {};
 #pragma unroll
-  for (int half = 0; half < DK / 64; ++half) {
-    float acc[8][4] = {};
+      for (int kk = 0; kk < 4; ++kk)
+        if (kk <= warp) {
+          uint32_t a[kPl<NM>][4];
+          rows_of_t(kk, sb, a);
 #pragma unroll
-    for (int kk = 0; kk < 4; ++kk)
-      if (kk <= warp) {
-        uint32_t a[kPl<NM>][4];
-        rows_of_t(kk, sb, a);
-#pragma unroll
-        for (int nn = 0; nn < 4; ++nn) {
-          uint32_t b[2][kPl<NI>][2];
-          tk.b(8 * half + 2 * nn, 2 * kk, b);
-          mma_p<NM, NI>(acc[2 * nn], a, b[0]);
-          mma_p<NM, NI>(acc[2 * nn + 1], a, b[1]);
+          for (int nn = 0; nn < 4; ++nn) {
+            uint32_t b[2][kPl<NI>][2];
+            tv.b(2 * nn, 2 * kk, b);
+            mma_p<NM, NI>(acc[2 * nn], a, b[0]);
+            mma_p<NM, NI>(acc[2 * nn + 1], a, b[1]);
+          }
         }
-      }
+      char* u = P.U + (w.nc * dvb + first + i) * Tile<8, NM>::kBytes;
 #pragma unroll
-    for (int nb = 0; nb < 8; ++nb) {
-      store_block<DK / 8, NM>(wt, 2 * warp, 8 * half + nb, acc[nb][0], acc[nb][1]);
-      store_block<DK / 8, NM>(wt, 2 * warp + 1, 8 * half + nb, acc[nb][2], acc[nb][3]);
+      for (int nb = 0; nb < 8; ++nb) {
+        store_block<8, NM>(u, 2 * warp, nb, acc[nb][0], acc[nb][1]);
+        store_block<8, NM>(u, 2 * warp + 1, nb, acc[nb][2], acc[nb][3]);
+      }
     }
   }
+}
+
+// Stages of what a chain kernel streams, filled by warps of their own: one thread issues the copies
+// (float32 tensors, which pass through registers, take two warps).
+template <int NI>
+constexpr int kLoadWarps = NI == 1 ? 1 : 2;
+// A stage's gates, padded so that the next stage's swizzled tiles are aligned.
+template <int NI>
+constexpr int kGateBytes = NI == 1 ? 2048 : kGates * 4;
+
+__device__ __forceinline__ void init_ring(uint64_t* full, uint64_t* empty, int stages, int fillers, int readers) {
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < stages; ++i) {
+      mbar_init(&full[i], fillers);
+      mbar_init(&empty[i], readers);
+    }
+    fence_mbar_init();
+  }
+  __syncthreads();
 }
 
 template <int DK, int NI, int NM, int WARPS>
 struct ChainSmem {
   static constexpr int kW = Tile<DK / 8, NM>::kBytes, kK = Tile<DK / 8, NI>::kBytes, kU = Tile<2 * WARPS, NM>::kBytes;
-  static constexpr int kStage = kW + kK + kU + kGates * 4;
+  static constexpr int kStage = kK + kW + kU + kGateBytes<NI>;
   static constexpr int kStages = WARPS == 2 && 3 * kStage <= 227 * 1024 ? 3 : 2;
-  static constexpr int kBytes = kStages * kStage;
+  static constexpr int kBytes = kStages * kStage + 16 * kStages;
 };
 
 // The states from chunk to chunk. A block takes 16 WARPS columns of a head's state, a warp 16 of them, as
 // S^T (16 x Dk) in accumulators: U^T = U0^T + S^T (-W)^T and S'^T = gamma_C S^T + (U^T diag(e^{G_C - G})) K
 // take their left operands from registers, so the warps of a head never exchange anything; the block
-// shares only the tiles that it streams. Two more warps only load, kStages - 1 chunks ahead: one barrier a
-// chunk says both that a stage has arrived and that the one before it may be filled again.
+// shares only the tiles that it streams.
 template <typename TI, int DK, int NI, int NM, int WARPS>
-__global__ void __launch_bounds__(32 * (WARPS + kLoadWarps), WARPS == 4 && NM < 3 ? 2 : 1)
-chain_kernel(const Problem P, const TI* __restrict__ k, const float* __restrict__ s0,
+__global__ void __launch_bounds__(32 * (WARPS + kLoadWarps<NI>), WARPS == 4 && NM < 3 ? 2 : 1)
+chain_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restrict__ k, const float* __restrict__ s0,
              float* __restrict__ s_last) {
-  extern __shared__ __align__(128) unsigned char smem[];
+  extern __shared__ __align__(1024) unsigned char smem[];
   using L = ChainSmem<DK, NI, NM, WARPS>;
   const int parts = P.Dv / (16 * WARPS), dvb = P.Dv / 64;
   const uint32_t bh = blockIdx.x / parts;
@@ -297,26 +332,27 @@ chain_kernel(const Problem P, const TI* __restrict__ k, const float* __restrict_
   const Where w0 = locate(P, bh, 0);
   const int chunks = (int)((w0.len + kC - 1) / kC);
   const int block = part * WARPS / 4, c8 = 2 * ((part * WARPS) & 3);  // this part's 64 columns, and where in them
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kStages * L::kStage);
+  uint64_t* empty = full + L::kStages;
+  init_ring(full, empty, L::kStages, NI == 1 ? 1 : 1 + 32 * kLoadWarps<NI>, WARPS);
   if (warp >= WARPS) {  // loads
     const int tid = threadIdx.x - 32 * WARPS;
-    const auto load = [&](int c) {
-      if (c < chunks) {
-        const uint32_t st = smem_u32(smem) + (uint32_t)(c % L::kStages) * L::kStage;
-        const int64_t nc = w0.nc + c, left = w0.len - (int64_t)c * kC;
-        copy_ws<L::kW, 32 * kLoadWarps>(st, P.W + nc * L::kW, tid);
-        load_rows<32 * kLoadWarps>(Tile<DK / 8, NI>{st + L::kW}, k + (w0.step + (int64_t)c * kC) * P.ldk + w0.hk * DK,
-                                   P.ldk, (int)(left < kC ? left : kC), tid);
-        copy_columns<32 * kLoadWarps>(Tile<2 * WARPS, NM>{st + L::kW + L::kK}, P.U + (nc * dvb + block) * Tile<8, NM>::kBytes, c8, tid);
-        copy_ws<1024, 32 * kLoadWarps>(st + L::kW + L::kK + L::kU, P.gates + nc * kGates, tid);
-      }
-      cp_async_commit();
-    };
-#pragma unroll
-    for (int i = 0; i < L::kStages - 1; ++i) load(i);
+    if (NI == 1 && tid > 0) return;
     for (int c = 0; c < chunks; ++c) {
-      cp_async_wait<L::kStages - 2>();
-      __syncthreads();
-      load(c + L::kStages - 1);
+      const int s = c % L::kStages;
+      const uint32_t st = smem_addr(smem) + s * L::kStage;
+      const int64_t nc = w0.nc + c, left = w0.len - (int64_t)c * kC;
+      if (c >= L::kStages) mbar_wait(&empty[s], (c / L::kStages - 1) & 1, P.err);
+      if (tid == 0) {
+        mbar_arrive_expect_tx(&full[s], tma_bytes<NI>(L::kK) + L::kW + L::kU + 4 * kGateFloats<NM>);
+        bulk_load(st + L::kK, P.W + nc * L::kW, L::kW, &full[s]);
+        bulk_columns(Tile<2 * WARPS, NM>{st + L::kK + L::kW}, P.U + (nc * dvb + block) * Tile<8, NM>::kBytes, c8,
+                     &full[s]);
+        bulk_load(st + L::kK + L::kW + L::kU, P.gates + nc * kGates, 4 * kGateFloats<NM>, &full[s]);
+      }
+      load_rows<32 * kLoadWarps<NI>>(InTile<DK / 8, NI>{st}, &M.k, &full[s], k, P.ldk, w0.hk * DK,
+                                     w0.t + (int64_t)c * kC, w0.b, P.L, (int)(left < kC ? left : kC), tid);
+      if constexpr (NI == 3) mbar_arrive(&full[s]);
     }
     return;
   }
@@ -328,13 +364,13 @@ chain_kernel(const Problem P, const TI* __restrict__ k, const float* __restrict_
     for (int e = 0; e < 4; ++e)
       S[nb][e] = s0 == nullptr ? 0.0f : s0[((int64_t)bh * DK + 8 * nb + row + (e & 1)) * P.Dv + col + 8 * (e >> 1)];
   for (int c = 0; c < chunks; ++c) {
-    __syncthreads();
     const int s = c % L::kStages;
-    const uint32_t st = smem_u32(smem) + s * L::kStage;
-    const Tile<DK / 8, NM> tw{st};
-    const Tile<DK / 8, NI> tk{st + L::kW};
-    const Tile<2 * WARPS, NM> tu{st + L::kW + L::kK};
-    const float* G = reinterpret_cast<const float*>(smem + s * L::kStage + L::kW + L::kK + L::kU);
+    mbar_wait(&full[s], (c / L::kStages) & 1, P.err);
+    const uint32_t st = smem_addr(smem) + s * L::kStage;
+    const InTile<DK / 8, NI> tk{st};
+    const Tile<DK / 8, NM> tw{st + L::kK};
+    const Tile<2 * WARPS, NM> tu{st + L::kK + L::kW};
+    const float* G = reinterpret_cast<const float*>(smem + s * L::kStage + L::kK + L::kW + L::kU);
     const int64_t tile = (w0.nc + c) * dvb + block;
     float u[8][4];
 #pragma unroll
@@ -343,8 +379,7 @@ chain_kernel(const Problem P, const TI* __restrict__ k, const float* __restrict_
       const int i = l >> 3;
 #pragma unroll
       for (int p = 0; p < kPl<NM>; ++p)
-        ldsm_t(tu.at(p, nb + (i >> 1), 2 * warp + (i & 1)) + (l & 7) * 16, f[0][p][0], f[0][p][1], f[1][p][0],
-               f[1][p][1]);
+        ldsm_t(tu.at(p, nb + (i >> 1), 2 * warp + (i & 1), l & 7), f[0][p][0], f[0][p][1], f[1][p][0], f[1][p][1]);
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -414,6 +449,8 @@ chain_kernel(const Problem P, const TI* __restrict__ k, const float* __restrict_
             mma_p<NM, NI>(S[n0 + 2 * nn + 1], a, b[nn][1]);
           }
         });
+    __syncwarp();
+    if (l == 0) mbar_arrive(&empty[s]);
   }
   if (s_last != nullptr) {
 #pragma unroll
@@ -427,14 +464,15 @@ chain_kernel(const Problem P, const TI* __restrict__ k, const float* __restrict_
 template <int DK, int NI, int NM>
 struct OutputSmem {
   static constexpr int kQ = Tile<DK / 8, NI>::kBytes, kU = Tile<8, NM>::kBytes, kS = Tile<DK / 8, NM>::kBytes;
-  static constexpr int kBytes = 2 * kQ + kU + kS + kGates * 4;
+  static constexpr int kBytes = 2 * kQ + kU + kS + kGates * 4 + 16;
 };
 
 // O = scale (diag(gamma) Q S + P U) of one chunk of one head; zero on the row's padding.
 template <typename TI, int DK, int NI, int NM>
 __global__ void __launch_bounds__(128)
-output_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ k, TI* __restrict__ o) {
-  extern __shared__ __align__(128) unsigned char smem[];
+output_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restrict__ q, const TI* __restrict__ k,
+              TI* __restrict__ o) {
+  extern __shared__ __align__(1024) unsigned char smem[];
   using L = OutputSmem<DK, NI, NM>;
   const Where w = locate(P);
   const int tid = threadIdx.x, warp = tid >> 5, l = tid & 31;
@@ -445,25 +483,30 @@ output_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ 
     }
   }
   if (w.rows <= 0) return;
-  const uint32_t base = smem_u32(smem);
-  const Tile<DK / 8, NI> tq{base}, tk{base + L::kQ};
+  const uint32_t base = smem_addr(smem);
+  const InTile<DK / 8, NI> tq{base}, tk{base + L::kQ};
   const Tile<8, NM> tu{base + 2 * L::kQ};
   const Tile<DK / 8, NM> ts{base + 2 * L::kQ + L::kU};
   float* G = reinterpret_cast<float*>(smem + 2 * L::kQ + L::kU + L::kS);
-  const int64_t row0 = w.step;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(G + kGates);
   const int dvb = P.Dv / 64;
-  load_rows<128>(tq, q + row0 * P.ldq + w.hk * DK, P.ldq, w.rows, tid);
-  load_rows<128>(tk, k + row0 * P.ldk + w.hk * DK, P.ldk, w.rows, tid);
-  copy_ws<4 * kGateFloats<NM>, 128>(smem_u32(G), P.gates + w.nc * kGates, tid);
-  cp_async_commit();
   const auto load = [&](int part) {
-    copy_ws<L::kU, 128>(tu.base, P.U + (w.nc * dvb + part) * L::kU, tid);
-    copy_ws<L::kS, 128>(ts.base, P.S + (w.nc * dvb + part) * L::kS, tid);
-    cp_async_commit();
+    mbar_arrive_expect_tx(&bars[1], L::kU + L::kS);
+    bulk_load(ts.base, P.S + (w.nc * dvb + part) * L::kS, L::kS, &bars[1]);
+    bulk_load(tu.base, P.U + (w.nc * dvb + part) * L::kU, L::kU, &bars[1]);
   };
-  load(0);
-  cp_async_wait<1>();
+  if (tid == 0) {
+    mbar_init(&bars[0], 1);
+    mbar_init(&bars[1], 1);
+    fence_mbar_init();
+    mbar_arrive_expect_tx(&bars[0], 2 * tma_bytes<NI>(L::kQ) + 4 * kGateFloats<NM>);
+    bulk_load(smem_addr(G), P.gates + w.nc * kGates, 4 * kGateFloats<NM>, &bars[0]);
+  }
+  load_rows<128>(tq, &M.q, &bars[0], q, P.ldq, w.hk * DK, w.t, w.b, P.L, w.rows, tid);
+  load_rows<128>(tk, &M.k, &bars[0], k, P.ldk, w.hk * DK, w.t, w.b, P.L, w.rows, tid);
+  if (tid == 0) load(0);
   __syncthreads();
+  mbar_wait(&bars[0], 0, P.err);
   const int r = l >> 2, c0 = 2 * (l & 3), r0 = 16 * warp + r;
   uint32_t p[4][kPl<NM>][4];  // P, as left operands
   {
@@ -495,10 +538,9 @@ output_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ 
   for (int part = 0; part < dvb; ++part) {
     if (part > 0) {
       __syncthreads();
-      load(part);
+      if (tid == 0) load(part);
     }
-    cp_async_wait<0>();
-    __syncthreads();
+    mbar_wait(&bars[1], part & 1, P.err);
     float acc[8][4] = {};
 #pragma unroll
     for (int kk = 0; kk < DK / 16; ++kk) {
@@ -530,7 +572,7 @@ output_kernel(const Problem P, const TI* __restrict__ q, const TI* __restrict__ 
           mma_p<NM, NM>(acc[2 * nn + 1], p[kk], b[1]);
         }
       }
-    TI* out = o + ((row0 + r0) * P.Hv + w.h) * P.Dv + 64 * part + c0;
+    TI* out = o + ((w.step + r0) * P.Hv + w.h) * P.Dv + 64 * part + c0;
 #pragma unroll
     for (int nb = 0; nb < 8; ++nb) {
       if (r0 < w.rows) store_pair(out + 8 * nb, P.scale * acc[nb][0], P.scale * acc[nb][1]);

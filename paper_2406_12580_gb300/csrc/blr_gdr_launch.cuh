@@ -28,14 +28,14 @@ blr_status fwd_dk(const Problem& p, const FwdCall& c) {
   const TI *q = static_cast<const TI*>(c.q), *k = static_cast<const TI*>(c.k), *v = static_cast<const TI*>(c.v),
            *g = static_cast<const TI*>(c.g), *beta = static_cast<const TI*>(c.beta);
   BLR_TRY(start("prepare", c.train ? prepare_kernel<TI, DK, NI, NM, true> : prepare_kernel<TI, DK, NI, NM, false>,
-                chunks, 128, PrepareSmem<DK, NI, NM>::kBytes, c.stream, p, k, v, g, beta));
+                chunks, 128, PrepareSmem<DK, NI, NM>::kBytes, c.stream, p, c.maps, k, v, g, beta));
   if (wide_chains(p))
-    BLR_TRY(start("chain", chain_kernel<TI, DK, NI, NM, 4>, p.B * p.Hv * (p.Dv / 64), 32 * (4 + kLoadWarps),
-                  ChainSmem<DK, NI, NM, 4>::kBytes, c.stream, p, k, c.s0, c.s_last));
+    BLR_TRY(start("chain", chain_kernel<TI, DK, NI, NM, 4>, p.B * p.Hv * (p.Dv / 64), 32 * (4 + kLoadWarps<NI>),
+                  ChainSmem<DK, NI, NM, 4>::kBytes, c.stream, p, c.maps, k, c.s0, c.s_last));
   else
-    BLR_TRY(start("chain", chain_kernel<TI, DK, NI, NM, 2>, p.B * p.Hv * (p.Dv / 32), 32 * (2 + kLoadWarps),
-                  ChainSmem<DK, NI, NM, 2>::kBytes, c.stream, p, k, c.s0, c.s_last));
-  return start("output", output_kernel<TI, DK, NI, NM>, chunks, 128, OutputSmem<DK, NI, NM>::kBytes, c.stream, p, q, k,
+    BLR_TRY(start("chain", chain_kernel<TI, DK, NI, NM, 2>, p.B * p.Hv * (p.Dv / 32), 32 * (2 + kLoadWarps<NI>),
+                  ChainSmem<DK, NI, NM, 2>::kBytes, c.stream, p, c.maps, k, c.s0, c.s_last));
+  return start("output", output_kernel<TI, DK, NI, NM>, chunks, 128, OutputSmem<DK, NI, NM>::kBytes, c.stream, p, c.maps, q, k,
                static_cast<TI*>(c.o));
 }
 
@@ -46,21 +46,21 @@ blr_status bwd_dk(const Problem& p, const BwdCall& c) {
            *d_o = static_cast<const TI*>(c.d_o);
   TI *dq = static_cast<TI*>(c.dq), *dk = static_cast<TI*>(c.dk_out), *dv = static_cast<TI*>(c.dv),
      *dg = static_cast<TI*>(c.dg), *dbeta = static_cast<TI*>(c.dbeta);
-  BLR_TRY(start("du", du_kernel<TI, DK, NI, NM>, chunks, 128, DuSmem<DK, NI>::kBytes, c.stream, p, q, k, d_o));
+  BLR_TRY(start("du", du_kernel<TI, DK, NI, NM>, chunks, 128, DuSmem<DK, NI>::kBytes, c.stream, p, c.maps, q, k, d_o));
   // two stages of float32 tiles and 64 columns do not fit beside each other
   constexpr int kWide = 2 * BackSmem<DK, NI, NM, 4>::kStage <= 227 * 1024 ? 4 : 2;
   if (wide_chains(p))
-    BLR_TRY(start("back", back_kernel<TI, DK, NI, NM, kWide>, p.B * p.Hv * (p.Dv / (16 * kWide)), 32 * (kWide + kLoadWarps),
-                  BackSmem<DK, NI, NM, kWide>::kBytes, c.stream, p, q, k, d_o, c.ds_last, c.ds0));
+    BLR_TRY(start("back", back_kernel<TI, DK, NI, NM, kWide>, p.B * p.Hv * (p.Dv / (16 * kWide)), 32 * (kWide + kLoadWarps<NI>),
+                  BackSmem<DK, NI, NM, kWide>::kBytes, c.stream, p, c.maps, q, k, d_o, c.ds_last, c.ds0));
   else
-    BLR_TRY(start("back", back_kernel<TI, DK, NI, NM, 2>, p.B * p.Hv * (p.Dv / 32), 32 * (2 + kLoadWarps),
-                  BackSmem<DK, NI, NM, 2>::kBytes, c.stream, p, q, k, d_o, c.ds_last, c.ds0));
+    BLR_TRY(start("back", back_kernel<TI, DK, NI, NM, 2>, p.B * p.Hv * (p.Dv / 32), 32 * (2 + kLoadWarps<NI>),
+                  BackSmem<DK, NI, NM, 2>::kBytes, c.stream, p, c.maps, q, k, d_o, c.ds_last, c.ds0));
   // 16 warps an SM hide each other's latencies; float32's operands take the registers of 8
   constexpr int kParts = NM == 3 || DK == 64 ? 2 : 4, bytes = GradSmem<DK, NI, NM, kParts>::kBytes;
   if (p.Hk == p.Hv)
-    return start("grad", grad_kernel<TI, TI, DK, NI, NM, kParts>, chunks, 128 * kParts, bytes, c.stream, p, q, k, v,
+    return start("grad", grad_kernel<TI, TI, DK, NI, NM, kParts>, chunks, 128 * kParts, bytes, c.stream, p, c.maps, q, k, v,
                  d_o, dq, dk, p.Hk, dv, dg, dbeta);
-  BLR_TRY(start("grad", grad_kernel<TI, float, DK, NI, NM, kParts>, chunks, 128 * kParts, bytes, c.stream, p, q, k, v,
+  BLR_TRY(start("grad", grad_kernel<TI, float, DK, NI, NM, kParts>, chunks, 128 * kParts, bytes, c.stream, p, c.maps, q, k, v,
                 d_o, p.pq, p.pk, p.Hv, dv, dg, dbeta));
   const int64_t pairs = p.B * p.L * p.Hk * (DK / 2), blocks = (pairs + 255) / 256;
   return start("share", share_kernel<TI>, blocks < 152 * 16 ? blocks : 152 * 16, 256, 0, c.stream,

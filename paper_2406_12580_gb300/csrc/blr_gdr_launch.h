@@ -16,6 +16,7 @@ struct FwdCall {
   void* o;
   float* s_last;
   cudaStream_t stream;
+  Maps maps;
 };
 struct BwdCall {
   int dk;
@@ -25,6 +26,7 @@ struct BwdCall {
   void *dq, *dk_out, *dv, *dg, *dbeta;
   float* ds0;
   cudaStream_t stream;
+  Maps maps;
 };
 
 blr_status fwd_f32(const Problem& p, const FwdCall& c);

@@ -5,7 +5,10 @@
 // bytes, block rows one after the other: a fragment load reads whole blocks
 // (no bank conflicts, no padding, no swizzle), a register of an accumulator
 // tile is one block (a 128-byte store), and a tile of the workspace is copied
-// linearly. A matrix comes in one of three forms P:
+// linearly. Callers' bfloat16 tensors arrive by TMA instead, 64 columns at a
+// time as rows of 128 bytes under the 128-byte swizzle (gathering their rows
+// with 16-byte copies kept the load pipe busy for 160 us of the chain's 590 on
+// 8 x 32768 x 512). A matrix comes in one of three forms P:
 //   1  bfloat16;
 //   2  two bfloat16 planes, x = hi + lo with 16 significant bits together; a
 //      product of two such operands is hi hi + lo hi + hi lo;
@@ -23,18 +26,16 @@
 
 #include <type_traits>
 
+#include <cuda.h>
 #include <cuda_bf16.h>
+
+#include "blr_device.cuh"
 
 namespace blr {
 namespace gdr {
 
 constexpr int kC = 64;               // steps of a chunk
-constexpr int kLoadWarps = 2;        // warps of a chain kernel's block that only load
 constexpr float kMinDecay = -120.0f;  // exp(-120) is 0 in float32
-
-__device__ __forceinline__ uint32_t smem_u32(const void* p) {
-  return (uint32_t)__cvta_generic_to_shared(p);
-}
 
 __device__ __forceinline__ uint32_t pack2(float a, float b) {  // a in the low half
   const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
@@ -157,59 +158,66 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
   return y;
 }
 
-// A tile of 64 rows x C8 * 8 columns in shared memory, P planes.
-template <int C8, int P>
+// A tile of 64 rows x C8 * 8 columns in shared memory, in the planes of form P. SW: the layout that TMA
+// writes (1024-byte aligned, one plane).
+template <int C8, int P, bool SW = false>
 struct Tile {
   static constexpr int kPlane = 8 * C8 * 128;  // bytes
   static constexpr int kBytes = kPl<P> * kPlane;
   uint32_t base;
-  __device__ __forceinline__ uint32_t at(int p, int r8, int c8) const {
-    return base + p * kPlane + (r8 * C8 + c8) * 128;
+  // Row i of block (r8, c8): 16 bytes.
+  __device__ __forceinline__ uint32_t at(int p, int r8, int c8, int i) const {
+    if constexpr (SW) return base + (c8 >> 3) * 8192 + r8 * 1024 + i * 128 + (((c8 & 7) ^ i) << 4);
+    return base + p * kPlane + (r8 * C8 + c8) * 128 + i * 16;
   }
   // Left operand, rows 8 m8 .. + 16, columns 8 k8 .. + 16, of the tile.
   __device__ __forceinline__ void a(int m8, int k8, uint32_t (&f)[kPl<P>][4]) const {
     const int l = threadIdx.x & 31, i = l >> 3;
 #pragma unroll
     for (int p = 0; p < kPl<P>; ++p)
-      ldsm(at(p, m8 + (i & 1), k8 + (i >> 1)) + (l & 7) * 16, f[p][0], f[p][1], f[p][2], f[p][3]);
+      ldsm(at(p, m8 + (i & 1), k8 + (i >> 1), l & 7), f[p][0], f[p][1], f[p][2], f[p][3]);
   }
   // Left operand of the transposed tile: rows 8 m8 .. are the tile's columns.
   __device__ __forceinline__ void a_t(int m8, int k8, uint32_t (&f)[kPl<P>][4]) const {
     const int l = threadIdx.x & 31, i = l >> 3;
 #pragma unroll
     for (int p = 0; p < kPl<P>; ++p)
-      ldsm_t(at(p, k8 + (i >> 1), m8 + (i & 1)) + (l & 7) * 16, f[p][0], f[p][1], f[p][2], f[p][3]);
+      ldsm_t(at(p, k8 + (i >> 1), m8 + (i & 1), l & 7), f[p][0], f[p][1], f[p][2], f[p][3]);
   }
   // Right operands of two 8-column blocks n8, n8 + 1 of X^T, X this tile (its rows are the columns).
   __device__ __forceinline__ void b_t(int n8, int k8, uint32_t (&f)[2][kPl<P>][2]) const {
     const int l = threadIdx.x & 31, i = l >> 3;
 #pragma unroll
     for (int p = 0; p < kPl<P>; ++p)
-      ldsm(at(p, n8 + (i >> 1), k8 + (i & 1)) + (l & 7) * 16, f[0][p][0], f[0][p][1], f[1][p][0], f[1][p][1]);
+      ldsm(at(p, n8 + (i >> 1), k8 + (i & 1), l & 7), f[0][p][0], f[0][p][1], f[1][p][0], f[1][p][1]);
   }
   // Right operands of two 8-column blocks of X, X this tile.
   __device__ __forceinline__ void b(int n8, int k8, uint32_t (&f)[2][kPl<P>][2]) const {
     const int l = threadIdx.x & 31, i = l >> 3;
 #pragma unroll
     for (int p = 0; p < kPl<P>; ++p)
-      ldsm_t(at(p, k8 + (i & 1), n8 + (i >> 1)) + (l & 7) * 16, f[0][p][0], f[0][p][1], f[1][p][0], f[1][p][1]);
+      ldsm_t(at(p, k8 + (i & 1), n8 + (i >> 1), l & 7), f[0][p][0], f[0][p][1], f[1][p][0], f[1][p][1]);
   }
   // The pair of values (row 8 r8 + lane / 4, columns 8 c8 + 2 (lane % 4) + {0, 1}).
   __device__ __forceinline__ float2 pair(int r8, int c8) const {
+    const int l = threadIdx.x & 31;
     uint32_t w[kPl<P>];
 #pragma unroll
     for (int p = 0; p < kPl<P>; ++p)
-      asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[p]) : "r"(at(p, r8, c8) + (threadIdx.x & 31) * 4) : "memory");
+      asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[p]) : "r"(at(p, r8, c8, l >> 2) + (l & 3) * 4) : "memory");
     return join2<P>(w);
   }
   __device__ __forceinline__ void put(int r8, int c8, float x, float y) const {
+    const int l = threadIdx.x & 31;
     uint32_t w[kPl<P>];
     split2<P>(x, y, w);
 #pragma unroll
     for (int p = 0; p < kPl<P>; ++p)
-      asm volatile("st.shared.b32 [%0], %1;" ::"r"(at(p, r8, c8) + (threadIdx.x & 31) * 4), "r"(w[p]) : "memory");
+      asm volatile("st.shared.b32 [%0], %1;" ::"r"(at(p, r8, c8, l >> 2) + (l & 3) * 4), "r"(w[p]) : "memory");
   }
 };
+template <int C8, int P>
+using InTile = Tile<C8, P, P == 1>;  // of a caller's tensor
 
 // An accumulator tile (16 rows x 8 columns in d[0], d[1]: row lane / 4; d[2], d[3]: row + 8) as half
 // of a left operand: blocks (x, y) give its columns 0..7 and 8..15.
@@ -230,22 +238,21 @@ __device__ __forceinline__ void to_a(const float (&x)[4], const float (&y)[4], u
   for (int p = 0; p < kPl<P>; ++p) f[p][3] = w[p];
 }
 
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool real) {
-  const int n = real ? 16 : 0;  // the rest of the 16 bytes becomes zero
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
-}
-__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+// ---- loads. What a block streams is counted, in bytes, on an mbarrier; one thread issues it.
 
-// A linear copy of BYTES (a multiple of 16) from the workspace by THREADS threads.
-template <int BYTES, int THREADS>
-__device__ __forceinline__ void copy_ws(uint32_t dst, const void* src, int tid) {
-  const char* p = static_cast<const char*>(src) + tid * 16;
-#pragma unroll
-  for (int i = 0; i < BYTES; i += THREADS * 16)
-    if (i + THREADS * 16 <= BYTES || i + tid * 16 < BYTES) cp_async16(dst + tid * 16 + i, p + i, true);
+// A linear copy of `bytes` (a multiple of 16) from the workspace.
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
+               "l"(src), "r"(bytes), "r"(smem_addr(bar)) : "memory");
 }
+
+template <int P>
+__host__ __device__ constexpr uint32_t tma_bytes(int bytes) { return P == 1 ? bytes : 0; }  // of a caller's tile that TMA brings
+
+// The callers' tensors as TMA sees them (bfloat16 only): (columns of all heads, steps, batch rows).
+struct Maps {
+  CUtensorMap q, k, v, d_o;
+};
 
 // Calls f(piece, row, column block) for a thread's 16-byte pieces of a 64 x 8 C8 tile: piece i is row
 // 8 (i / (8 C8)) + i % 8, column block (i / 8) % C8, so that a warp reads at least 64 bytes of 8 rows.
@@ -265,18 +272,25 @@ __device__ __forceinline__ void each_piece(int tid, F f) {
   }
 }
 
-// 64 rows of a caller's tensor (row r at p + r ld; rows from `rows` on are zero and not read) as a
-// tile. bfloat16 arrives asynchronously; float32 is taken apart into its planes on the way.
-template <int THREADS, int C8>
-__device__ __forceinline__ void load_rows(const Tile<C8, 1>& t, const __nv_bfloat16* p, int64_t ld, int rows,
-                                          int tid) {
-  each_piece<C8, THREADS>(tid, [&](int i, int r, int c8) {
-    const bool real = r < rows;
-    cp_async16(t.base + i * 16, real ? p + r * ld + c8 * 8 : p, real);
-  });
+// 64 rows of a caller's tensor as a tile: from step t of batch row b, columns col .. of the row; steps past
+// the row's end are zero. bfloat16: one thread, counted on `bar` (kBytes of it). float32: THREADS threads,
+// taken apart into its planes on the way (rows from `rows` on are not read); complete on return.
+template <int THREADS, int C8, typename TI>
+__device__ __forceinline__ void load_rows(const Tile<C8, 1, true>& t, const CUtensorMap* map, uint64_t* bar, const TI*,
+                                          int64_t, int col, int64_t step, int b, int64_t, int, int tid) {
+  if (tid == 0) {
+#pragma unroll
+    for (int j = 0; j < C8 / 8; ++j)
+      asm volatile(
+          "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+          " [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(t.base + 8192 * j),
+          "l"(map), "r"(col + 64 * j), "r"((int)step), "r"(b), "r"(smem_addr(bar)) : "memory");
+  }
 }
 template <int THREADS, int C8>
-__device__ __forceinline__ void load_rows(const Tile<C8, 3>& t, const float* p, int64_t ld, int rows, int tid) {
+__device__ __forceinline__ void load_rows(const Tile<C8, 3>& t, const CUtensorMap*, uint64_t*, const float* base,
+                                          int64_t ld, int col, int64_t step, int b, int64_t L, int rows, int tid) {
+  const float* p = base + (b * L + step) * ld + col;
   each_piece<C8, THREADS>(tid, [&](int i, int r, int c8) {
     float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f), y = x;
     if (r < rows) {
@@ -296,15 +310,19 @@ __device__ __forceinline__ void load_rows(const Tile<C8, 3>& t, const float* p, 
   });
 }
 
-// Columns [8 c8, 8 c8 + 8 C) of a 64 x 64 tile of the workspace.
-template <int THREADS, int C, int P>
-__device__ __forceinline__ void copy_columns(const Tile<C, P>& t, const char* src, int c8, int tid) {
+// Columns [8 c8, 8 c8 + 8 C) of a 64 x 64 tile of the workspace, by one thread.
+template <int C, int P>
+__device__ __forceinline__ void bulk_columns(const Tile<C, P>& t, const char* src, int c8, uint64_t* bar) {
+  if constexpr (C == 8) {
+    bulk_load(t.base, src, Tile<C, P>::kBytes, bar);
+  } else {
 #pragma unroll
-  for (int p = 0; p < kPl<P>; ++p)
+    for (int p = 0; p < kPl<P>; ++p)
 #pragma unroll
-    for (int i = tid; i < 64 * C; i += THREADS)
-      cp_async16(t.base + p * Tile<C, P>::kPlane + i * 16,
-                 src + p * Tile<8, P>::kPlane + ((i / (8 * C)) * 8 + c8) * 128 + (i % (8 * C)) * 16, true);
+      for (int r8 = 0; r8 < 8; ++r8)
+        bulk_load(t.base + p * Tile<C, P>::kPlane + r8 * C * 128, src + p * Tile<8, P>::kPlane + (r8 * 8 + c8) * 128,
+                  C * 128, bar);
+  }
 }
 
 // N steps of which each loads right operands and multiplies by them: the next step's are on their way
@@ -362,6 +380,7 @@ struct Problem {
   float scale;
   const int32_t* lengths;
   // workspace
+  uint32_t* err;  // kErrTimeout if a wait for a load ran out
   float* gates;  // per chunk: kGates
   char *W, *U, *S, *T, *dU, *dS;
   float *pq, *pk;  // per value head gradients of q and k, when heads are shared
@@ -372,7 +391,8 @@ struct Where {
   int b, h, hk, c;  // batch row, value head, key head, chunk of the row
   int rows;         // real steps in the chunk (may be <= 0)
   int64_t nc, len;  // chunk number over everything; the row's real steps
-  int64_t step;     // the chunk's first slot as a step of the whole batch, b L + t
+  int64_t t;        // the step of the chunk's first slot
+  int64_t step;     // as a step of the whole batch, b L + t
 };
 __device__ __forceinline__ int64_t row_length(const Problem& P, int b) {
   if (P.lengths == nullptr) return P.L;
@@ -387,7 +407,8 @@ __device__ __forceinline__ Where locate(const Problem& P, uint32_t bh, int c) {
   w.c = c;
   w.nc = (int64_t)bh * P.n + c;
   w.len = row_length(P, w.b);
-  w.step = w.b * P.L + P.L - w.len + (int64_t)c * kC;
+  w.t = P.L - w.len + (int64_t)c * kC;
+  w.step = w.b * P.L + w.t;
   const int64_t left = w.len - (int64_t)c * kC;
   w.rows = (int)(left < kC ? left : kC);
   return w;

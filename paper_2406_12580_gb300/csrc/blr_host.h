@@ -4,6 +4,7 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <cudaTypedefs.h>
 #include <cuda_runtime.h>
 
 #include "blr.h"
@@ -13,6 +14,9 @@ namespace blr {
 // Records the text of blr_last_error_string() and returns `s`.
 blr_status fail(blr_status s, const char* fmt, ...);
 blr_status cuda_check(cudaError_t e, const char* what);
+
+// cuTensorMapEncodeTiled, through the runtime's driver entry point.
+blr_status tensor_map_encoder(PFN_cuTensorMapEncodeTiled_v12000* out);
 
 inline bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
 
