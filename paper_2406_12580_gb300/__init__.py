@@ -102,7 +102,7 @@ def _ptr(t, name: str):
 def _stream(stream):
     if stream is None:
         import torch
-        return torch.cuda.current_stream().cuda_stream
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -240,20 +240,24 @@ def GDRDesc(B: int, L: int, Hk: int, Hv: int, Dk: int, Dv: int, ldq: int = 0, ld
     return blr_gdr_desc(B, L, Hk, Hv, Dk, Dv, ldq, ldk, ldv, io, scale)
 
 
-def _row_ptr(t, name: str):
-    """_ptr of a tensor that may be a slice of wider rows (its strides are the descriptor's)."""
-    if t is None or isinstance(t, int):
-        return t
+def _pointers(names: str, *tensors) -> list:
+    """_ptr of many tensors at once; a name with a star may be a slice of wider rows (its strides are
+    the descriptor's)."""
     import torch
-    if not isinstance(t, torch.Tensor):
-        raise TypeError(f"{name}: expected a CUDA tensor, an int pointer or None")
-    if t.numel() == 0:
-        return None
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name}: tensor must be on the current CUDA device")
-    if t.stride(-1) != 1:
-        raise ValueError(f"{name}: the last dimension must be contiguous")
-    return t.data_ptr()
+    device = torch._C._cuda_getDevice()
+    out = []
+    for name, t in zip(names.split(), tensors):
+        if t is None or isinstance(t, int):
+            out.append(t)
+            continue
+        if not isinstance(t, torch.Tensor):
+            raise TypeError(f"{name}: expected a CUDA tensor, an int pointer or None")
+        if t.get_device() != device and t.numel() > 0:
+            raise ValueError(f"{name}: tensor must be on the current CUDA device")
+        if not t.is_contiguous() and not (name[0] == "*" and t.stride(-1) == 1):
+            raise ValueError(f"{name}: tensor must be contiguous")
+        out.append(t.data_ptr() or None)
+    return out
 
 
 def _ws_bytes(ws) -> int:
@@ -266,21 +270,19 @@ def blr_gdr_workspace_bytes(desc: blr_gdr_desc, flags: int) -> int:
 
 def blr_gdr_fwd(desc, flags, lengths, q, k, v, g, beta, s0, o, s_last, ws, stream=None):
     """Gated delta rule over whole sequences (see include/blr.h)."""
-    _check(load().blr_gdr_fwd(ctypes.byref(desc), flags, _ptr(lengths, "lengths"), _row_ptr(q, "q"),
-                              _row_ptr(k, "k"), _row_ptr(v, "v"), _ptr(g, "g"), _ptr(beta, "beta"),
-                              _ptr(s0, "s0"), _ptr(o, "o"), _ptr(s_last, "s_last"), _ptr(ws, "ws"),
+    _check(load().blr_gdr_fwd(ctypes.byref(desc), flags,
+                              *_pointers("lengths *q *k *v g beta s0 o s_last ws", lengths, q, k, v, g, beta, s0,
+                                         o, s_last, ws),
                               _ws_bytes(ws), _stream(stream)),
            "blr_gdr_fwd")
 
 
 def blr_gdr_bwd(desc, flags, lengths, d_o, ds_last, q, k, v, g, beta, s0, dq, dk, dv, dg, dbeta, ds0, ws,
                 stream=None):
-    _check(load().blr_gdr_bwd(ctypes.byref(desc), flags, _ptr(lengths, "lengths"), _ptr(d_o, "d_o"),
-                              _ptr(ds_last, "ds_last"), _row_ptr(q, "q"), _row_ptr(k, "k"),
-                              _row_ptr(v, "v"), _ptr(g, "g"), _ptr(beta, "beta"), _ptr(s0, "s0"),
-                              _ptr(dq, "dq"), _ptr(dk, "dk"), _ptr(dv, "dv"), _ptr(dg, "dg"),
-                              _ptr(dbeta, "dbeta"), _ptr(ds0, "ds0"), _ptr(ws, "ws"), _ws_bytes(ws),
-                              _stream(stream)),
+    _check(load().blr_gdr_bwd(ctypes.byref(desc), flags,
+                              *_pointers("lengths d_o ds_last *q *k *v g beta s0 dq dk dv dg dbeta ds0 ws", lengths,
+                                         d_o, ds_last, q, k, v, g, beta, s0, dq, dk, dv, dg, dbeta, ds0, ws),
+                              _ws_bytes(ws), _stream(stream)),
            "blr_gdr_bwd")
 
 
@@ -291,9 +293,9 @@ def blr_gdr_status(ws, stream=None) -> int:
 
 def blr_gdr_steps(desc, state, s_prev, q, k, v, g, beta, s_out, o=None, stream=None):
     """desc.L recurrent steps per row (state dtype `state`, BLR_F32 or BLR_BF16); s_out may be s_prev."""
-    _check(load().blr_gdr_steps(ctypes.byref(desc), state, _ptr(s_prev, "s_prev"), _row_ptr(q, "q"),
-                                _row_ptr(k, "k"), _row_ptr(v, "v"), _ptr(g, "g"), _ptr(beta, "beta"),
-                                _ptr(s_out, "s_out"), _ptr(o, "o"), _stream(stream)),
+    _check(load().blr_gdr_steps(ctypes.byref(desc), state,
+                                *_pointers("s_prev *q *k *v g beta s_out o", s_prev, q, k, v, g, beta, s_out, o),
+                                _stream(stream)),
            "blr_gdr_steps")
 
 
@@ -319,9 +321,7 @@ def blr_adamw_step(params, grads, m, v, *, lr: float, step: int, beta1: float = 
     dtypes = {"params": params[0].dtype, "grads": params[0].dtype, "m": m[0].dtype, "v": m[0].dtype}
     if dtypes["m"] not in (torch.float32, torch.float8_e4m3fn):
         raise TypeError("moments are float32 or float8_e4m3fn")
-    device = params[0].device
-    if device.type != "cuda" or device.index != torch.cuda.current_device():
-        raise ValueError("tensors must be on the current CUDA device")
+    device = torch._C._cuda_getDevice()
     table = np.zeros((n, 8), dtype=np.int64)
     sizes = [t.numel() for t in params]
     blocks = [-(-x // 256) for x in sizes] if eight else None
@@ -329,9 +329,12 @@ def blr_adamw_step(params, grads, m, v, *, lr: float, step: int, beta1: float = 
         if ts is None:
             continue
         dtype, want = dtypes.get(name, torch.float32), blocks if "scales" in name else sizes
-        if (len(ts) != n or any(t.dtype != dtype or t.device != device for t in ts)
-                or not all([t.is_contiguous() for t in ts]) or [t.numel() for t in ts] != want):
-            raise ValueError(f"{name}: {n} contiguous {dtype} tensors of the parameters' sizes on {device} are wanted")
+        if len(ts) == n:
+            fit = [t.dtype is dtype and t.get_device() == device and t.is_contiguous() and t.numel() == x
+                   for t, x in zip(ts, want)]
+        if len(ts) != n or not all(fit):
+            raise ValueError(f"{name}: {n} contiguous {dtype} tensors of the parameters' sizes on the current CUDA "
+                             "device are wanted")
         table[:, column] = [t.data_ptr() for t in ts]
     table[:, 7] = sizes
     _check(load().blr_adamw_step(n, table.ctypes.data, io, 8 if eight else 32, lr, beta1, beta2, eps,

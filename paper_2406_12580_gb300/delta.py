@@ -15,7 +15,6 @@ from typing import Optional
 
 import torch
 from torch import nn
-from torch.autograd.function import once_differentiable
 
 from . import (BLR_F32, BLR_GDR_STATE, BLR_GDR_TRAIN, GDRDesc, _dtype_code, blr_gdr_bwd, blr_gdr_fwd,
                blr_gdr_steps, blr_gdr_workspace_bytes)
@@ -76,12 +75,13 @@ class GatedDeltaRule(torch.autograd.Function):
         return o, s_last
 
     @staticmethod
-    @once_differentiable
     def backward(ctx, do, ds_last):
+        if torch.is_grad_enabled():
+            raise RuntimeError("the gated delta rule has no second derivative (create_graph=True)")
         q, k, v, g, beta, s0, lengths, ws = ctx.saved_tensors
         do = torch.zeros_like(v, memory_format=torch.contiguous_format) if do is None else do.contiguous()
         ds_last = None if ds_last is None else ds_last.contiguous()
-        new = lambda t: torch.empty(t.shape, dtype=t.dtype, device=t.device)  # noqa: E731
+        new = lambda t: torch.empty_like(t, memory_format=torch.contiguous_format)  # noqa: E731
         dq, dk, dv, dg, dbeta = new(q), new(k), new(v), new(g), new(beta)
         ds0 = new(s0) if s0 is not None and ctx.needs_input_grad[6] else None
         blr_gdr_bwd(ctx.desc, ctx.flags, lengths, do, ds_last, q, k, v, g, beta, s0, dq, dk, dv, dg, dbeta, ds0, ws)

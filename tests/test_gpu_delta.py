@@ -260,3 +260,11 @@ def test_refusals():
     with pytest.raises(BLRError):  # a workspace too small
         blr_gdr_fwd(desc, 2, None, *args, None, o, None, ws[:-16])
     assert ctypes.sizeof(desc) == 80
+
+
+def test_no_second_derivative():
+    d = make(1, 20, 1, 1, 64, 64, torch.float32, seed=18, device="cuda")
+    q = d["q"].requires_grad_(True)
+    o, _ = gated_delta_rule(q, *(d[n] for n in ("k", "v", "g", "beta")))
+    with pytest.raises(RuntimeError):
+        torch.autograd.grad(o.sum(), q, create_graph=True)
