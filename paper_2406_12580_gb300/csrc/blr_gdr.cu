@@ -12,12 +12,14 @@ constexpr int64_t kC = 64;
 // Under this many steps a gradient is a sum of so few products that the rounding of a single score
 // shows in the whole row (one step: 5e-3 of dq, against 3e-3 from 64 steps on): operands take two planes.
 constexpr int64_t kFewSteps = 16;
+constexpr int64_t kSms = 152, kSegChunks = 8, kMinSegs = 5;
 
 // The workspace: for every chunk of every value head, tiles of 64 rows in `np` planes.
 struct Layout {
   int64_t n, nc;
   int np;
-  size_t gates, W, U, S, T, dU, dS, pq, pk, bytes;
+  int64_t nseg, seg_chunks;
+  size_t phi, carry, back_carry, gates, W, U, S, T, dU, dS, pq, pk, bytes;
 };
 
 size_t up(size_t v) { return (v + 255) / 256 * 256; }
@@ -30,6 +32,16 @@ blr_status make_layout(const blr_gdr_desc* d, int flags, const GdrSizes& s, Layo
   if (l->nc >= 0x7fffffff || s.B * s.Hv * (s.Dv / 32) >= 0x7fffffff)
     return fail(BLR_ERR_UNSUPPORTED, "too many chunks (%lld)", (long long)l->nc);
   l->np = d->io == BLR_F32 || (flags & BLR_GDR_STATE) || s.L < kFewSteps ? 2 : 1;
+  // Segments: enough for a block of 64 columns on every SM, of at least kSegChunks chunks. Three passes'
+  // products (see chain_kernel) over nseg times the warps gain from five segments on.
+  const int64_t blocks = s.B * s.Hv * (s.Dv / 64);
+  l->nseg = 1;
+  if (blocks * kMinSegs <= kSms) l->nseg = l->n / kSegChunks < kSms / blocks ? l->n / kSegChunks : kSms / blocks;
+  // the maps are chained one after the other, at about the time of a chunk each
+  while (l->nseg * l->nseg > 3 * l->n) --l->nseg;
+  if (l->nseg < kMinSegs) l->nseg = 1;
+  l->seg_chunks = (l->n + l->nseg - 1) / l->nseg;
+  l->nseg = (l->n + l->seg_chunks - 1) / l->seg_chunks;
   const size_t tile = (size_t)l->nc * l->np * 64 * 2;  // bytes per column of a tile
   const size_t dk = (size_t)s.Dk, dv = (size_t)s.Dv;
   size_t o = 256;  // the error word
@@ -41,7 +53,13 @@ blr_status make_layout(const blr_gdr_desc* d, int flags, const GdrSizes& s, Layo
   take(&l->W, tile * dk);
   take(&l->U, tile * dv);
   take(&l->S, tile / 64 * dv * dk);
-  l->T = l->dU = l->dS = l->pq = l->pk = 0;
+  l->T = l->dU = l->dS = l->pq = l->pk = l->phi = l->carry = l->back_carry = 0;
+  const size_t segs = (size_t)(s.B * s.Hv * l->nseg);
+  if (l->nseg > 1) {
+    take(&l->phi, segs * dk * dk * 4);  // two planes
+    take(&l->carry, segs * dv * dk * 4);
+    if (flags & BLR_GDR_TRAIN) take(&l->back_carry, segs * dv * dk * 4);
+  }
   if (flags & BLR_GDR_TRAIN) {
     take(&l->T, tile * 64);
     take(&l->dU, tile * dv);
@@ -75,9 +93,14 @@ Problem make_problem(const blr_gdr_desc* d, const GdrSizes& s, const Layout& l, 
   p.W = w + l.W;
   p.U = w + l.U;
   p.S = w + l.S;
-  p.T = w + l.T;
+  p.T = l.T != 0 ? w + l.T : nullptr;
   p.dU = w + l.dU;
   p.dS = w + l.dS;
+  p.nseg = (int)l.nseg;
+  p.seg_chunks = (int)l.seg_chunks;
+  p.phi = w + l.phi;
+  p.carry = reinterpret_cast<float*>(w + l.carry);
+  p.back_carry = reinterpret_cast<float*>(w + l.back_carry);
   p.pq = reinterpret_cast<float*>(w + l.pq);
   p.pk = reinterpret_cast<float*>(w + l.pk);
   return p;

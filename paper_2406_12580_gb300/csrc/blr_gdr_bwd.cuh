@@ -117,19 +117,21 @@ struct BackSmem {
 };
 
 // The states' gradients from chunk to chunk, last to first: as chain_kernel, a warp holds dS^T of 16
-// columns in accumulators, and further warps load.
-template <typename TI, int DK, int NI, int NM, int WARPS>
+// columns in accumulators, and further warps load. MAPS: a segment's N; its phi is the forward's, transposed.
+template <typename TI, int DK, int NI, int NM, int WARPS, bool MAPS>
 __global__ void __launch_bounds__(32 * (WARPS + kLoadWarps<NI>), WARPS == 4 && NM < 3 ? 2 : 1)
 back_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restrict__ q, const TI* __restrict__ k,
             const TI* __restrict__ d_o, const float* __restrict__ ds_last, float* __restrict__ ds0) {
   extern __shared__ __align__(1024) unsigned char smem[];
   using L = BackSmem<DK, NI, NM, WARPS>;
   const int parts = P.Dv / (16 * WARPS), dvb = P.Dv / 64;
-  const uint32_t bh = blockIdx.x / parts;
-  const int part = blockIdx.x - bh * parts;
+  const uint32_t bs = blockIdx.x / parts, bh = bs / P.nseg;
+  const int part = blockIdx.x - bs * parts, seg = bs - bh * P.nseg;
   const int warp = threadIdx.x >> 5, l = threadIdx.x & 31;
   const Where w0 = locate(P, bh, 0);
-  const int chunks = (int)((w0.len + kC - 1) / kC);
+  const Segment sg = segment(P, w0, seg);
+  if (P.nseg > 1 && sg.count <= 0 && seg > 0) return;
+  if (MAPS && (seg == 0 || sg.chunks == 0)) return;
   const int block = part * WARPS / 4, c8 = 2 * ((part * WARPS) & 3);
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kStages * L::kStage);
   uint64_t* empty = full + L::kStages;
@@ -138,8 +140,8 @@ back_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restric
     const int tid = threadIdx.x - 32 * WARPS;
     if (NI == 1 && tid > 0) return;
     const int64_t ldo = (int64_t)P.Hv * P.Dv;
-    for (int n = 0; n < chunks; ++n) {
-      const int c = chunks - 1 - n, s = n % L::kStages;
+    for (int n = 0; n < sg.count; ++n) {
+      const int c = sg.first + sg.count - 1 - n, s = n % L::kStages;
       const uint32_t st = smem_addr(smem) + s * L::kStage;
       const int64_t nc = w0.nc + c, left = w0.len - (int64_t)c * kC, t = w0.t + (int64_t)c * kC;
       const int rows = (int)(left < kC ? left : kC);
@@ -164,16 +166,23 @@ back_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restric
     return;
   }
   const int col = 16 * (part * WARPS + warp) + (l >> 2), row = 2 * (l & 3);
+  float* carry = P.back_carry + (int64_t)bs * P.Dv * DK + (int64_t)col * DK + row;
   float S[DK / 8][4];
 #pragma unroll
   for (int nb = 0; nb < DK / 8; ++nb)
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      S[nb][e] = ds_last == nullptr
-                     ? 0.0f
-                     : ds_last[((int64_t)bh * DK + 8 * nb + row + (e & 1)) * P.Dv + col + 8 * (e >> 1)];
-  for (int n = 0; n < chunks; ++n) {
-    const int c = chunks - 1 - n, s = n % L::kStages;
+    for (int e = 0; e < 4; ++e) {
+      if (MAPS)
+        S[nb][e] = 0.0f;
+      else if (P.nseg > 1 && sg.chunks > 0)
+        S[nb][e] = carry[8 * (e >> 1) * DK + 8 * nb + (e & 1)];
+      else
+        S[nb][e] = ds_last == nullptr
+                       ? 0.0f
+                       : ds_last[((int64_t)bh * DK + 8 * nb + row + (e & 1)) * P.Dv + col + 8 * (e >> 1)];
+    }
+  for (int n = 0; n < sg.count; ++n) {
+    const int c = sg.first + sg.count - 1 - n, s = n % L::kStages;
     mbar_wait(&full[s], (n / L::kStages) & 1, P.err);
     const uint32_t st = smem_addr(smem) + s * L::kStage;
     const InTile<DK / 8, NI> tk{st}, tq{st + L::kK};
@@ -194,6 +203,7 @@ back_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restric
         [&](int kk, auto& b) {
           uint32_t a[kPl<NM>][4];
           to_a<NM>(S[2 * kk], S[2 * kk + 1], a);
+          if (!MAPS)
 #pragma unroll
           for (int p = 0; p < kPl<NM>; ++p)
 #pragma unroll
@@ -272,7 +282,7 @@ back_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restric
                 const float2 v = join2<NM>(x);
                 y[2 * e] = fmaf(y[2 * e], down.x, v.x);
                 y[2 * e + 1] = fmaf(y[2 * e + 1], down.y, v.y);
-                store_block_t<8, NM>(uo, 2 * kk + h, c8 + 2 * warp + e, y[2 * e], y[2 * e + 1]);
+                if (!MAPS) store_block_t<8, NM>(uo, 2 * kk + h, c8 + 2 * warp + e, y[2 * e], y[2 * e + 1]);
               }
             }
             to_a<NM>(u[2 * kk], u[2 * kk + 1], a);
@@ -286,7 +296,13 @@ back_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restric
     __syncwarp();
     if (l == 0) mbar_arrive(&empty[s]);
   }
-  if (ds0 != nullptr) {
+  if constexpr (MAPS) {
+#pragma unroll
+    for (int nb = 0; nb < DK / 8; ++nb) {
+      store_pair(carry + 8 * nb, S[nb][0], S[nb][1]);
+      store_pair(carry + 8 * DK + 8 * nb, S[nb][2], S[nb][3]);
+    }
+  } else if (ds0 != nullptr && seg == 0) {
 #pragma unroll
     for (int nb = 0; nb < DK / 8; ++nb)
 #pragma unroll

@@ -307,6 +307,10 @@ __device__ __forceinline__ void init_ring(uint64_t* full, uint64_t* empty, int s
   __syncthreads();
 }
 
+// The segments' maps carry states over hundreds of steps: two planes at least.
+template <int NM>
+constexpr int kMapForm = NM == 3 ? 3 : 2;
+
 template <int DK, int NI, int NM, int WARPS>
 struct ChainSmem {
   static constexpr int kW = Tile<DK / 8, NM>::kBytes, kK = Tile<DK / 8, NI>::kBytes, kU = Tile<2 * WARPS, NM>::kBytes;
@@ -319,18 +323,26 @@ struct ChainSmem {
 // S^T (16 x Dk) in accumulators: U^T = U0^T + S^T (-W)^T and S'^T = gamma_C S^T + (U^T diag(e^{G_C - G})) K
 // take their left operands from registers, so the warps of a head never exchange anything; the block
 // shares only the tiles that it streams.
-template <typename TI, int DK, int NI, int NM, int WARPS>
+//
+// Where rows are cut into segments, every segment's map (see Problem) is computed first, all segments at
+// once: MAPS. Its Dv columns N start from zero; its phi is what becomes of the identity's Dk columns without
+// U0. combine_kernel chains the maps, and this kernel then runs every segment from the state before it:
+// three times the products of the single pass, over nseg times the warps.
+template <typename TI, int DK, int NI, int NM, int WARPS, bool MAPS>
 __global__ void __launch_bounds__(32 * (WARPS + kLoadWarps<NI>), WARPS == 4 && NM < 3 ? 2 : 1)
 chain_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restrict__ k, const float* __restrict__ s0,
              float* __restrict__ s_last) {
   extern __shared__ __align__(1024) unsigned char smem[];
   using L = ChainSmem<DK, NI, NM, WARPS>;
-  const int parts = P.Dv / (16 * WARPS), dvb = P.Dv / 64;
-  const uint32_t bh = blockIdx.x / parts;
-  const int part = blockIdx.x - bh * parts;
+  const int parts = (P.Dv + (MAPS ? DK : 0)) / (16 * WARPS), dvb = P.Dv / 64;
+  const uint32_t bs = blockIdx.x / parts, bh = bs / P.nseg;
+  const int part = blockIdx.x - bs * parts, seg = bs - bh * P.nseg;
   const int warp = threadIdx.x >> 5, l = threadIdx.x & 31;
   const Where w0 = locate(P, bh, 0);
-  const int chunks = (int)((w0.len + kC - 1) / kC);
+  const Segment sg = segment(P, w0, seg);
+  const bool ident = MAPS && 16 * WARPS * part >= P.Dv;
+  if (P.nseg > 1 && sg.count <= 0 && seg > 0) return;
+  if (MAPS && seg == sg.last && (!ident || P.T == nullptr)) return;  // only the backward takes its phi
   const int block = part * WARPS / 4, c8 = 2 * ((part * WARPS) & 3);  // this part's 64 columns, and where in them
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kStages * L::kStage);
   uint64_t* empty = full + L::kStages;
@@ -338,16 +350,17 @@ chain_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restri
   if (warp >= WARPS) {  // loads
     const int tid = threadIdx.x - 32 * WARPS;
     if (NI == 1 && tid > 0) return;
-    for (int c = 0; c < chunks; ++c) {
-      const int s = c % L::kStages;
+    for (int n = 0; n < sg.count; ++n) {
+      const int c = sg.first + n, s = n % L::kStages;
       const uint32_t st = smem_addr(smem) + s * L::kStage;
       const int64_t nc = w0.nc + c, left = w0.len - (int64_t)c * kC;
-      if (c >= L::kStages) mbar_wait(&empty[s], (c / L::kStages - 1) & 1, P.err);
+      if (n >= L::kStages) mbar_wait(&empty[s], (n / L::kStages - 1) & 1, P.err);
       if (tid == 0) {
-        mbar_arrive_expect_tx(&full[s], tma_bytes<NI>(L::kK) + L::kW + L::kU + 4 * kGateFloats<NM>);
+        mbar_arrive_expect_tx(&full[s], tma_bytes<NI>(L::kK) + L::kW + (ident ? 0 : L::kU) + 4 * kGateFloats<NM>);
         bulk_load(st + L::kK, P.W + nc * L::kW, L::kW, &full[s]);
-        bulk_columns(Tile<2 * WARPS, NM>{st + L::kK + L::kW}, P.U + (nc * dvb + block) * Tile<8, NM>::kBytes, c8,
-                     &full[s]);
+        if (!ident)
+          bulk_columns(Tile<2 * WARPS, NM>{st + L::kK + L::kW}, P.U + (nc * dvb + block) * Tile<8, NM>::kBytes, c8,
+                       &full[s]);
         bulk_load(st + L::kK + L::kW + L::kU, P.gates + nc * kGates, 4 * kGateFloats<NM>, &full[s]);
       }
       load_rows<32 * kLoadWarps<NI>>(InTile<DK / 8, NI>{st}, &M.k, &full[s], k, P.ldk, w0.hk * DK,
@@ -357,15 +370,24 @@ chain_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restri
     return;
   }
   const int col = 16 * (part * WARPS + warp) + (l >> 2), row = 2 * (l & 3);  // of S (row + 8 nb, col (+ 8))
+  // this warp's rows of a segment's map or carry
+  float* carry = P.carry + (int64_t)bs * P.Dv * DK + (int64_t)col * DK + row;
+  const int unit = col - P.Dv;  // row of the identity
   float S[DK / 8][4];
 #pragma unroll
   for (int nb = 0; nb < DK / 8; ++nb)
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      S[nb][e] = s0 == nullptr ? 0.0f : s0[((int64_t)bh * DK + 8 * nb + row + (e & 1)) * P.Dv + col + 8 * (e >> 1)];
-  for (int c = 0; c < chunks; ++c) {
-    const int s = c % L::kStages;
-    mbar_wait(&full[s], (c / L::kStages) & 1, P.err);
+    for (int e = 0; e < 4; ++e) {
+      if (MAPS)
+        S[nb][e] = ident && 8 * nb + row + (e & 1) == unit + 8 * (e >> 1) ? 1.0f : 0.0f;
+      else if (P.nseg > 1 && sg.chunks > 0)
+        S[nb][e] = carry[8 * (e >> 1) * DK + 8 * nb + (e & 1)];
+      else
+        S[nb][e] = s0 == nullptr ? 0.0f : s0[((int64_t)bh * DK + 8 * nb + row + (e & 1)) * P.Dv + col + 8 * (e >> 1)];
+    }
+  for (int n = 0; n < sg.count; ++n) {
+    const int c = sg.first + n, s = n % L::kStages;
+    mbar_wait(&full[s], (n / L::kStages) & 1, P.err);
     const uint32_t st = smem_addr(smem) + s * L::kStage;
     const InTile<DK / 8, NI> tk{st};
     const Tile<DK / 8, NM> tw{st + L::kK};
@@ -373,6 +395,11 @@ chain_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restri
     const float* G = reinterpret_cast<const float*>(smem + s * L::kStage + L::kK + L::kW + L::kU);
     const int64_t tile = (w0.nc + c) * dvb + block;
     float u[8][4];
+#pragma unroll
+    for (int nb = 0; nb < 8; ++nb)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) u[nb][e] = 0.0f;
+    if (!ident)
 #pragma unroll
     for (int nb = 0; nb < 8; nb += 2) {  // U0^T: blocks (tokens 8 nb, columns 16 warp), transposed
       uint32_t f[2][kPl<NM>][2];
@@ -402,6 +429,7 @@ chain_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restri
         [&](int kk, auto& b) {
           uint32_t a[kPl<NM>][4];
           to_a<NM>(S[2 * kk], S[2 * kk + 1], a);
+          if (!MAPS)
 #pragma unroll
           for (int p = 0; p < kPl<NM>; ++p)
 #pragma unroll
@@ -433,8 +461,10 @@ chain_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restri
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               float(&x)[4] = u[2 * kk + h];
-              store_block_t<8, NM>(uo, 2 * kk + h, c8 + 2 * warp, x[0], x[1]);
-              store_block_t<8, NM>(uo, 2 * kk + h, c8 + 2 * warp + 1, x[2], x[3]);
+              if (!MAPS) {
+                store_block_t<8, NM>(uo, 2 * kk + h, c8 + 2 * warp, x[0], x[1]);
+                store_block_t<8, NM>(uo, 2 * kk + h, c8 + 2 * warp + 1, x[2], x[3]);
+              }
               const float2 down = *reinterpret_cast<const float2*>(&G[kDown + 16 * kk + 8 * h + row]);
               x[0] *= down.x;
               x[1] *= down.y;
@@ -452,12 +482,111 @@ chain_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restri
     __syncwarp();
     if (l == 0) mbar_arrive(&empty[s]);
   }
-  if (s_last != nullptr) {
+  if constexpr (MAPS) {
+    if (ident) {
+      constexpr int kTile = Tile<DK / 8, kMapForm<NM>>::kBytes;
+      char* phi = P.phi + ((int64_t)bs * (DK / 64) + (unit >> 6)) * kTile;
+      const int r8 = (unit & 63) >> 3;
+#pragma unroll
+      for (int nb = 0; nb < DK / 8; ++nb) {
+        store_block<DK / 8, kMapForm<NM>>(phi, r8, nb, S[nb][0], S[nb][1]);
+        store_block<DK / 8, kMapForm<NM>>(phi, r8 + 1, nb, S[nb][2], S[nb][3]);
+      }
+    } else {
+#pragma unroll
+      for (int nb = 0; nb < DK / 8; ++nb) {
+        store_pair(carry + 8 * nb, S[nb][0], S[nb][1]);
+        store_pair(carry + 8 * DK + 8 * nb, S[nb][2], S[nb][3]);
+      }
+    }
+  } else if (s_last != nullptr && seg == sg.last) {
 #pragma unroll
     for (int nb = 0; nb < DK / 8; ++nb)
 #pragma unroll
       for (int e = 0; e < 4; ++e)
         s_last[((int64_t)bh * DK + 8 * nb + row + (e & 1)) * P.Dv + col + 8 * (e >> 1)] = S[nb][e];
+  }
+}
+
+template <int DK, int NM>
+struct CombineSmem {
+  static constexpr int kPhi = DK / 64 * Tile<DK / 8, kMapForm<NM>>::kBytes;
+  static constexpr int kBytes = 2 * kPhi + 16;
+};
+
+// Chains the segments' maps of a head, 64 columns a block: S -> phi S + N (back: dS -> phi^T dS + N, last
+// segment first), and leaves the state before (after) every segment in N's place.
+template <int DK, int NM, bool BACK>
+__global__ void __launch_bounds__(128)
+combine_kernel(const Problem P, float* __restrict__ carry, const float* __restrict__ start) {
+  extern __shared__ __align__(1024) unsigned char smem[];
+  constexpr int MP = kMapForm<NM>, kPhi = CombineSmem<DK, NM>::kPhi;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + 2 * kPhi);
+  const int dvb = P.Dv / 64;
+  const uint32_t bh = blockIdx.x / dvb;
+  const int warp = threadIdx.x >> 5, l = threadIdx.x & 31;
+  const int col = 64 * (blockIdx.x - bh * dvb) + 16 * warp + (l >> 2), row = 2 * (l & 3);
+  const Segment sg = segment(P, locate(P, bh, 0), 0);
+  if (sg.chunks == 0) return;
+  if (threadIdx.x == 0) {
+    mbar_init(&bars[0], 1);
+    mbar_init(&bars[1], 1);
+    fence_mbar_init();
+  }
+  const auto load = [&](int i) {
+    if (threadIdx.x == 0 && i < sg.last) {
+      mbar_arrive_expect_tx(&bars[i & 1], kPhi);
+      bulk_load(smem_addr(smem) + (i & 1) * kPhi, P.phi + ((int64_t)bh * P.nseg + (BACK ? sg.last - i : i)) * kPhi, kPhi,
+                &bars[i & 1]);
+    }
+  };
+  load(0);
+  float S[DK / 8][4];
+#pragma unroll
+  for (int nb = 0; nb < DK / 8; ++nb)
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      S[nb][e] = start == nullptr
+                     ? 0.0f
+                     : start[((int64_t)bh * DK + 8 * nb + row + (e & 1)) * P.Dv + col + 8 * (e >> 1)];
+  __syncthreads();
+  for (int i = 0; i <= sg.last; ++i) {
+    load(i + 1);
+    float* at = carry + (((int64_t)bh * P.nseg + (BACK ? sg.last - i : i)) * P.Dv + col) * DK + row;
+    float N[DK / 8][4];
+#pragma unroll
+    for (int nb = 0; nb < DK / 8; ++nb)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float2 x = i < sg.last ? *reinterpret_cast<const float2*>(at + 8 * h * DK + 8 * nb) : make_float2(0.0f, 0.0f);
+        N[nb][2 * h] = x.x;
+        N[nb][2 * h + 1] = x.y;
+        store_pair(at + 8 * h * DK + 8 * nb, S[nb][2 * h], S[nb][2 * h + 1]);
+      }
+    if (i == sg.last) break;
+    mbar_wait(&bars[i & 1], (i >> 1) & 1, P.err);
+    const uint32_t phi = smem_addr(smem) + (i & 1) * kPhi;
+#pragma unroll
+    for (int kk = 0; kk < DK / 16; ++kk) {
+      uint32_t a[kPl<MP>][4];
+      to_a<MP>(S[2 * kk], S[2 * kk + 1], a);
+#pragma unroll
+      for (int nn = 0; nn < DK / 16; ++nn) {
+        uint32_t b[2][kPl<MP>][2];
+        // phi^T's rows are its index k (forward) or its columns (backward)
+        if constexpr (BACK)
+          Tile<DK / 8, MP>{phi + (2 * nn / 8) * Tile<DK / 8, MP>::kBytes}.b_t((2 * nn) & 7, 2 * kk, b);
+        else
+          Tile<DK / 8, MP>{phi + (2 * kk / 8) * Tile<DK / 8, MP>::kBytes}.b(2 * nn, (2 * kk) & 7, b);
+        mma_p<MP, MP>(N[2 * nn], a, b[0]);
+        mma_p<MP, MP>(N[2 * nn + 1], a, b[1]);
+      }
+    }
+#pragma unroll
+    for (int nb = 0; nb < DK / 8; ++nb)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) S[nb][e] = N[nb][e];
+    __syncthreads();  // this map has been read: its place may be filled again
   }
 }
 

@@ -20,7 +20,7 @@ blr_status start(const char* name, K kernel, int64_t blocks, int threads, int by
 
 // Whether the chains of states go 64 columns to a block: with fewer such blocks than SMs, 32 to a block
 // put each chain's warps on more of them (twice the loads of W and K, half the shared-memory reads of an SM).
-inline bool wide_chains(const Problem& p) { return p.B * p.Hv * (p.Dv / 64) > 152; }
+inline bool wide_chains(const Problem& p) { return p.nseg > 1 || p.B * p.Hv * (p.Dv / 64) > 152; }
 
 template <typename TI, int DK, int NI, int NM>
 blr_status fwd_dk(const Problem& p, const FwdCall& c) {
@@ -29,12 +29,20 @@ blr_status fwd_dk(const Problem& p, const FwdCall& c) {
            *g = static_cast<const TI*>(c.g), *beta = static_cast<const TI*>(c.beta);
   BLR_TRY(start("prepare", c.train ? prepare_kernel<TI, DK, NI, NM, true> : prepare_kernel<TI, DK, NI, NM, false>,
                 chunks, 128, PrepareSmem<DK, NI, NM>::kBytes, c.stream, p, c.maps, k, v, g, beta));
+  constexpr int wide = ChainSmem<DK, NI, NM, 4>::kBytes, narrow = ChainSmem<DK, NI, NM, 2>::kBytes;
+  const int64_t heads = p.B * p.Hv;
+  if (p.nseg > 1) {
+    BLR_TRY(start("chain maps", chain_kernel<TI, DK, NI, NM, 4, true>, heads * p.nseg * ((p.Dv + DK) / 64),
+                  32 * (4 + kLoadWarps<NI>), wide, c.stream, p, c.maps, k, c.s0, c.s_last));
+    BLR_TRY(start("combine", combine_kernel<DK, NM, false>, heads * (p.Dv / 64), 128, CombineSmem<DK, NM>::kBytes,
+                  c.stream, p, p.carry, c.s0));
+  }
   if (wide_chains(p))
-    BLR_TRY(start("chain", chain_kernel<TI, DK, NI, NM, 4>, p.B * p.Hv * (p.Dv / 64), 32 * (4 + kLoadWarps<NI>),
-                  ChainSmem<DK, NI, NM, 4>::kBytes, c.stream, p, c.maps, k, c.s0, c.s_last));
+    BLR_TRY(start("chain", chain_kernel<TI, DK, NI, NM, 4, false>, heads * p.nseg * (p.Dv / 64),
+                  32 * (4 + kLoadWarps<NI>), wide, c.stream, p, c.maps, k, c.s0, c.s_last));
   else
-    BLR_TRY(start("chain", chain_kernel<TI, DK, NI, NM, 2>, p.B * p.Hv * (p.Dv / 32), 32 * (2 + kLoadWarps<NI>),
-                  ChainSmem<DK, NI, NM, 2>::kBytes, c.stream, p, c.maps, k, c.s0, c.s_last));
+    BLR_TRY(start("chain", chain_kernel<TI, DK, NI, NM, 2, false>, heads * p.nseg * (p.Dv / 32),
+                  32 * (2 + kLoadWarps<NI>), narrow, c.stream, p, c.maps, k, c.s0, c.s_last));
   return start("output", output_kernel<TI, DK, NI, NM>, chunks, 128, OutputSmem<DK, NI, NM>::kBytes, c.stream, p, c.maps, q, k,
                static_cast<TI*>(c.o));
 }
@@ -49,12 +57,20 @@ blr_status bwd_dk(const Problem& p, const BwdCall& c) {
   BLR_TRY(start("du", du_kernel<TI, DK, NI, NM>, chunks, 128, DuSmem<DK, NI>::kBytes, c.stream, p, c.maps, q, k, d_o));
   // two stages of float32 tiles and 64 columns do not fit beside each other
   constexpr int kWide = 2 * BackSmem<DK, NI, NM, 4>::kStage <= 227 * 1024 ? 4 : 2;
+  constexpr int wide = BackSmem<DK, NI, NM, kWide>::kBytes, narrow = BackSmem<DK, NI, NM, 2>::kBytes;
+  const int64_t heads = p.B * p.Hv;
+  if (p.nseg > 1) {
+    BLR_TRY(start("back maps", back_kernel<TI, DK, NI, NM, kWide, true>, heads * p.nseg * (p.Dv / (16 * kWide)),
+                  32 * (kWide + kLoadWarps<NI>), wide, c.stream, p, c.maps, q, k, d_o, c.ds_last, c.ds0));
+    BLR_TRY(start("combine", combine_kernel<DK, NM, true>, heads * (p.Dv / 64), 128, CombineSmem<DK, NM>::kBytes,
+                  c.stream, p, p.back_carry, c.ds_last));
+  }
   if (wide_chains(p))
-    BLR_TRY(start("back", back_kernel<TI, DK, NI, NM, kWide>, p.B * p.Hv * (p.Dv / (16 * kWide)), 32 * (kWide + kLoadWarps<NI>),
-                  BackSmem<DK, NI, NM, kWide>::kBytes, c.stream, p, c.maps, q, k, d_o, c.ds_last, c.ds0));
+    BLR_TRY(start("back", back_kernel<TI, DK, NI, NM, kWide, false>, heads * p.nseg * (p.Dv / (16 * kWide)),
+                  32 * (kWide + kLoadWarps<NI>), wide, c.stream, p, c.maps, q, k, d_o, c.ds_last, c.ds0));
   else
-    BLR_TRY(start("back", back_kernel<TI, DK, NI, NM, 2>, p.B * p.Hv * (p.Dv / 32), 32 * (2 + kLoadWarps<NI>),
-                  BackSmem<DK, NI, NM, 2>::kBytes, c.stream, p, c.maps, q, k, d_o, c.ds_last, c.ds0));
+    BLR_TRY(start("back", back_kernel<TI, DK, NI, NM, 2, false>, heads * p.nseg * (p.Dv / 32),
+                  32 * (2 + kLoadWarps<NI>), narrow, c.stream, p, c.maps, q, k, d_o, c.ds_last, c.ds0));
   // 16 warps an SM hide each other's latencies; float32's operands take the registers of 8
   constexpr int kParts = NM == 3 || DK == 64 ? 2 : 4, bytes = GradSmem<DK, NI, NM, kParts>::kBytes;
   if (p.Hk == p.Hv)

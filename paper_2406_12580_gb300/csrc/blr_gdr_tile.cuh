@@ -383,6 +383,12 @@ struct Problem {
   uint32_t* err;  // kErrTimeout if a wait for a load ran out
   float* gates;  // per chunk: kGates
   char *W, *U, *S, *T, *dU, *dS;
+  // Long rows of few heads are cut into nseg segments of seg_chunks chunks (nseg 1: not). A segment maps the
+  // state before it affinely, S -> phi S + N: `phi` holds phi^T of every segment as Dk / 64 tiles, `carry`
+  // N^T and later the state before the segment, `back_carry` the same of the states' gradients (Dv x Dk each).
+  int nseg, seg_chunks;
+  char* phi;
+  float *carry, *back_carry;
   float *pq, *pk;  // per value head gradients of q and k, when heads are shared
 };
 
@@ -416,6 +422,18 @@ __device__ __forceinline__ Where locate(const Problem& P, uint32_t bh, int c) {
 __device__ __forceinline__ Where locate(const Problem& P) {  // of a grid with a block for every chunk
   const uint32_t bh = blockIdx.x / (uint32_t)P.n;
   return locate(P, bh, (int)(blockIdx.x - bh * P.n));
+}
+// The chunks of a row, and of one of its segments.
+struct Segment {
+  int chunks, first, count, last;  // of the row; first chunk and chunks (<= 0: none) here; the row's last segment
+};
+__device__ __forceinline__ Segment segment(const Problem& P, const Where& w0, int seg) {
+  Segment s;
+  s.chunks = (int)((w0.len + kC - 1) / kC);
+  s.first = seg * P.seg_chunks;
+  s.count = min(P.seg_chunks, s.chunks - s.first);
+  s.last = max(0, (s.chunks - 1) / P.seg_chunks);
+  return s;
 }
 // The padding step that slot i of the chunk stands for, or -1.
 __device__ __forceinline__ int64_t padding_step(const Problem& P, const Where& w, int i) {

@@ -32,6 +32,10 @@ SHAPES = [  # B, L, Hk, Hv, Dk, Dv, lengths
     (1, 70, 1, 3, 128, 256, None),
     (5, 131, 1, 2, 64, 64, [0, 131, 1, 64, 77]),
     (3, 257, 2, 2, 128, 128, [300, -5, 65]),
+    # few heads and long rows: cut into segments
+    (1, 2700, 1, 1, 64, 64, None),
+    (3, 2600, 1, 1, 64, 128, [0, 2600, 130]),
+    (2, 3333, 1, 1, 128, 64, [1111, 3333]),
 ]
 
 
