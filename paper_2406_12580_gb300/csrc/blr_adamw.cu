@@ -90,6 +90,12 @@ template <> struct Eight<__nv_bfloat16> {
   static __device__ __forceinline__ void put(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
 };
 
+__device__ __forceinline__ float fast_sqrt(float x) {
+  float y;
+  asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
 // e4m3 codes (two at a time) to and from floats, by the conversion instructions.
 __device__ __forceinline__ float2 from_e4m3x2(uint16_t c) {
   const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)c, __NV_E4M3);
@@ -100,16 +106,15 @@ __device__ __forceinline__ uint16_t to_e4m3x2(float a, float b) {
 }
 
 // The codes of a lane's 8 values: 8 bytes, or single bytes of a ragged or unaligned group.
-__device__ __forceinline__ void load_codes(const uint8_t* p, int n, bool wide, float scale, float (&x)[8]) {
+__device__ __forceinline__ uint2 load_codes(const uint8_t* p, int n, bool wide) {
+  if (wide) return __ldcs(reinterpret_cast<const uint2*>(p));
   uint32_t w[2] = {0u, 0u};
-  if (wide) {
-    const uint2 r = __ldcs(reinterpret_cast<const uint2*>(p));
-    w[0] = r.x;
-    w[1] = r.y;
-  } else {
-    for (int i = 0; i < 8; ++i)
-      if (i < n) w[i >> 2] |= (uint32_t)p[i] << (8 * (i & 3));
-  }
+  for (int i = 0; i < 8; ++i)
+    if (i < n) w[i >> 2] |= (uint32_t)p[i] << (8 * (i & 3));
+  return make_uint2(w[0], w[1]);
+}
+__device__ __forceinline__ void decode(uint2 c, float scale, float (&x)[8]) {
+  const uint32_t w[2] = {c.x, c.y};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const float2 f = from_e4m3x2((uint16_t)(w[i >> 1] >> (16 * (i & 1))));
@@ -121,12 +126,11 @@ __device__ __forceinline__ void load_codes(const uint8_t* p, int n, bool wide, f
 // Writes the codes and the scale of a warp's group; `tiny`: the least code of a positive value.
 __device__ __forceinline__ void store_codes(uint8_t* p, float* scale, int n, bool wide, float tiny,
                                             const float (&x)[8]) {
-  float top = 0.0f;
+  // magnitudes order as their bits do, and a NaN's are above all others
+  uint32_t bits = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) asm("max.NaN.f32 %0, %1, %2;" : "=f"(top) : "f"(top), "f"(fabsf(x[i])));
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1)
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(top) : "f"(top), "f"(__shfl_xor_sync(0xffffffffu, top, d)));
+  for (int i = 0; i < 8; ++i) bits = max(bits, __float_as_uint(x[i]) & 0x7fffffffu);
+  const float top = __uint_as_float(__reduce_max_sync(0xffffffffu, bits));
   const float inverse = top > 0.0f ? fminf(__fmul_rn(__fdiv_rn(1.0f, top), kE4m3Max), 3.402823466e38f) : 0.0f;
   uint32_t w[2] = {0u, 0u};
 #pragma unroll
@@ -136,7 +140,7 @@ __device__ __forceinline__ void store_codes(uint8_t* p, float* scale, int n, boo
     for (int j = 0; j < 2; ++j) {
       const float v = x[2 * i + j];
       y[j] = __fmul_rn(v, inverse);
-      if (v > 0.0f && y[j] < tiny) y[j] = tiny;
+      if (tiny > 0.0f && v > 0.0f) y[j] = fmaxf(y[j], tiny);
     }
     w[i >> 1] |= (uint32_t)to_e4m3x2(y[0], y[1]) << (16 * (i & 1));
   }
@@ -184,55 +188,78 @@ adamw_kernel(const __grid_constant__ Table<CAP> table, const __grid_constant__ H
   const float gs = h.grad_scale == nullptr ? 1.0f : __ldg(h.grad_scale);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   constexpr int kStride = (kThreads / 32) * kGroup;
+  constexpr int kHeld = BITS == 8 ? kChunk / kStride : 1;  // groups whose loads are in flight together
 #pragma unroll
-  for (int it = 0; it < kChunk / kStride; ++it) {
-    const int64_t at = begin + it * kStride + warp * kGroup;
-    if (at >= n) break;  // by whole warps
-    const bool wide = aligned && at + kGroup <= n;
-    const int64_t i0 = at + lane * 8;
-    const int left = wide ? 8 : (int)max((int64_t)0, min((int64_t)8, n - i0));
-    float w[8], g[8], m[8], v[8];
-    if constexpr (MASTER) {
-      load8<float>(t.w + i0, left, wide, w);
-    } else {
-      load8<T>(static_cast<const T*>(t.p) + i0, left, wide, w);
-    }
-    load8<T>(static_cast<const T*>(t.g) + i0, left, wide, g);
-    if constexpr (BITS == 32) {
-      load8<float>(static_cast<const float*>(t.m) + i0, left, wide, m);
-      load8<float>(static_cast<const float*>(t.v) + i0, left, wide, v);
-    } else {
-      const int64_t block = at / kGroup;
-      load_codes(static_cast<const uint8_t*>(t.m) + i0, left, wide, t.m_scale[block], m);
-      load_codes(static_cast<const uint8_t*>(t.v) + i0, left, wide, t.v_scale[block], v);
+  for (int it0 = 0; it0 < kChunk / kStride; it0 += kHeld) {
+    float w[kHeld][8], g[kHeld][8], m[kHeld][8], v[kHeld][8];
+    uint2 mc[kHeld], vc[kHeld];
+    float ms[kHeld], vs[kHeld];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = __fmul_rn(v[i], v[i]);
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float gi = __fmul_rn(g[i], gs);
-      m[i] = __fadd_rn(__fmul_rn(m[i], h.b1), __fmul_rn(gi, h.c1));
-      v[i] = __fadd_rn(__fmul_rn(v[i], h.b2), __fmul_rn(__fmul_rn(gi, gi), h.c2));
-      const float r = __fsqrt_rn(v[i]);
-      const float d = __fadd_rn(__fmul_rn(r, h.root_scale), h.eps);
-      w[i] = __fsub_rn(__fmul_rn(w[i], h.keep), __fmul_rn(__fdiv_rn(m[i], d), h.rate));
-      if constexpr (BITS == 8) v[i] = r;
-    }
-    if constexpr (BITS == 32) {
-      store8<float>(static_cast<float*>(t.m) + i0, left, wide, m);
-      store8<float>(static_cast<float*>(t.v) + i0, left, wide, v);
-    } else {
-      const int64_t block = at / kGroup;
-      if (!wide) {  // values past the end have no part in the scale
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (i >= left) m[i] = v[i] = 0.0f;
+    for (int k = 0; k < kHeld; ++k) {
+      const int64_t at = begin + (it0 + k) * kStride + warp * kGroup;
+      if (at >= n) break;  // by whole warps
+      const bool wide = aligned && at + kGroup <= n;
+      const int64_t i0 = at + lane * 8;
+      const int left = wide ? 8 : (int)max((int64_t)0, min((int64_t)8, n - i0));
+      if constexpr (MASTER) {
+        load8<float>(t.w + i0, left, wide, w[k]);
+      } else {
+        load8<T>(static_cast<const T*>(t.p) + i0, left, wide, w[k]);
       }
-      store_codes(static_cast<uint8_t*>(t.m) + i0, t.m_scale + block, left, wide, 0.0f, m);
-      store_codes(static_cast<uint8_t*>(t.v) + i0, t.v_scale + block, left, wide, kE4m3Tiny, v);
+      load8<T>(static_cast<const T*>(t.g) + i0, left, wide, g[k]);
+      if constexpr (BITS == 32) {
+        load8<float>(static_cast<const float*>(t.m) + i0, left, wide, m[k]);
+        load8<float>(static_cast<const float*>(t.v) + i0, left, wide, v[k]);
+      } else {
+        const int64_t block = at / kGroup;
+        mc[k] = load_codes(static_cast<const uint8_t*>(t.m) + i0, left, wide);
+        vc[k] = load_codes(static_cast<const uint8_t*>(t.v) + i0, left, wide);
+        ms[k] = t.m_scale[block];
+        vs[k] = t.v_scale[block];
+      }
     }
-    if constexpr (MASTER) store8<float>(t.w + i0, left, wide, w);
-    store8<T>(static_cast<T*>(t.p) + i0, left, wide, w);
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k) {
+      const int64_t at = begin + (it0 + k) * kStride + warp * kGroup;
+      if (at >= n) break;
+      const bool wide = aligned && at + kGroup <= n;
+      const int64_t i0 = at + lane * 8;
+      const int left = wide ? 8 : (int)max((int64_t)0, min((int64_t)8, n - i0));
+      if constexpr (BITS == 8) {
+        decode(mc[k], ms[k], m[k]);
+        decode(vc[k], vs[k], v[k]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[k][i] = __fmul_rn(v[k][i], v[k][i]);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float gi = __fmul_rn(g[k][i], gs);
+        m[k][i] = __fadd_rn(__fmul_rn(m[k][i], h.b1), __fmul_rn(gi, h.c1));
+        v[k][i] = __fadd_rn(__fmul_rn(v[k][i], h.b2), __fmul_rn(__fmul_rn(gi, gi), h.c2));
+        // With 8-bit moments the instructions bound the kernel: root and quotient to two units in the
+        // last place there (a root is stored in 4 bits of precision, the quotient is a thousandth of w).
+        const float r = BITS == 8 ? fast_sqrt(v[k][i]) : __fsqrt_rn(v[k][i]);
+        const float d = __fadd_rn(__fmul_rn(r, h.root_scale), h.eps);
+        const float u = BITS == 8 ? __fdividef(m[k][i], d) : __fdiv_rn(m[k][i], d);
+        w[k][i] = __fsub_rn(__fmul_rn(w[k][i], h.keep), __fmul_rn(u, h.rate));
+        if constexpr (BITS == 8) v[k][i] = r;
+      }
+      if constexpr (BITS == 32) {
+        store8<float>(static_cast<float*>(t.m) + i0, left, wide, m[k]);
+        store8<float>(static_cast<float*>(t.v) + i0, left, wide, v[k]);
+      } else {
+        const int64_t block = at / kGroup;
+        if (!wide) {  // values past the end have no part in the scale
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (i >= left) m[k][i] = v[k][i] = 0.0f;
+        }
+        store_codes(static_cast<uint8_t*>(t.m) + i0, t.m_scale + block, left, wide, 0.0f, m[k]);
+        store_codes(static_cast<uint8_t*>(t.v) + i0, t.v_scale + block, left, wide, kE4m3Tiny, v[k]);
+      }
+      if constexpr (MASTER) store8<float>(t.w + i0, left, wide, w[k]);
+      store8<T>(static_cast<T*>(t.p) + i0, left, wide, w[k]);
+    }
   }
 }
 

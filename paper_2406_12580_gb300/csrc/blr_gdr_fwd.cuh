@@ -215,10 +215,12 @@ prepare_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __rest
   };
   if constexpr (TRAIN) {
     char* t = P.T + w.nc * Tile<8, NM>::kBytes;
-    for (int nb = 0; nb < 2 * warp + 2; ++nb)
+#pragma unroll
+    for (int nb = 0; nb < 8; ++nb)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const float2 x = *reinterpret_cast<const float2*>(&inv[(r0 + 8 * e) * kLd + 8 * nb + c0]);
+        float2 x = make_float2(0.0f, 0.0f);
+        if (nb < 2 * warp + 2) x = *reinterpret_cast<const float2*>(&inv[(r0 + 8 * e) * kLd + 8 * nb + c0]);
         store_block<8, NM>(t, 2 * warp + e, nb, x.x, x.y);
       }
   }

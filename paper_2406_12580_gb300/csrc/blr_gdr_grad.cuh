@@ -1,0 +1,512 @@
+// The gradients' kernel of the gated delta rule on the fifth-generation tensor cores (bfloat16 operands,
+// Dv 64 or 128): what grad_kernel computes, chunk by chunk, with tcgen05 products whose operands are read
+// from shared memory by the tensor cores themselves and whose sums stay in tensor memory.
+//
+// The products have 64 rows (the chunk's steps) and an accumulator 128 lanes, so two of one right operand
+// are stacked: [dO; dR] S and [dO; dR] U^T, [Q; K] K^T, [scale dP o D; M] K. Where one has no partner its
+// rows go to lanes 64.., beside whatever lies before its tile in shared memory, and lanes 0..63 are not
+// read. Lanes 0..63 then hold all of dQ's terms and lanes 64..127 all of dK's:
+//     X13 = [dO; dR] S^T   X2 = [-; U dS'^T]   DPA = [dO; dR] U^T   QKK = [Q; K] K^T
+//     Y1 = [P'; M] K       Y2 = [-; P'^T Q + M^T K]        P' = scale dP o D
+// Tiles of the workspace (8 x 8 blocks) are operands of either major-ness without a swizzle, the callers'
+// tensors and what is written here lie under the 128-byte swizzle.
+//
+// Bound by memory at Dk = Dv = 128: 216 KB a chunk, 0.52 ms of 16384 chunks. A persistent block an SM
+// works on one chunk at a time; each of its buffers is refilled for the next chunk as soon as its last
+// product is done, so the loads run beside the arithmetic on the scores and gradients (8 warps) and one
+// thread issues loads and products.
+#pragma once
+
+#include "blr_gdr_bwd.cuh"
+
+namespace blr {
+namespace gdr {
+
+namespace tc {
+
+// Shared-memory operand descriptors. `lead` and `stride` in bytes: without a swizzle the distance of
+// blocks adjacent along K and along M/N (K-major), or along K and along M/N exchanged roles (M/N-major,
+// where `lead` is along K too); under the 128-byte swizzle K-major only `stride` counts (1024: 8 rows),
+// M/N-major `lead` is the distance of 64-column tiles and `stride` 1024 (8 rows, along K).
+__device__ __forceinline__ uint64_t desc(uint32_t addr, uint32_t lead, uint32_t stride, bool swizzled) {
+  return (uint64_t)((addr & 0x3ffff) >> 4) | ((uint64_t)(lead >> 4) << 16) | ((uint64_t)(stride >> 4) << 32) |
+         (1ull << 46) | (swizzled ? 2ull << 61 : 0ull);
+}
+// bfloat16 x bfloat16 -> float32, M = 128; ta, tb: the operand is M/N-major.
+__device__ __forceinline__ constexpr uint32_t instr(int n, bool ta, bool tb) {
+  return (1u << 4) | (1u << 7) | (1u << 10) | ((ta ? 1u : 0u) << 15) | ((tb ? 1u : 0u) << 16) |
+         ((uint32_t)(n >> 3) << 17) | (8u << 24);
+}
+__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d), "l"(a), "l"(b), "r"(idesc),
+      "r"((uint32_t)add)
+      : "memory");
+}
+// STEPS products of 16 along K; the descriptors advance by da, db bytes.
+template <int STEPS>
+__device__ __forceinline__ void mma_k(uint32_t d, uint64_t a, uint32_t da, uint64_t b, uint32_t db, uint32_t idesc,
+                                      bool add) {
+#pragma unroll
+  for (int i = 0; i < STEPS; ++i) mma(d, a + ((i * da) >> 4), b + ((i * db) >> 4), idesc, add || i > 0);
+}
+// Arrives on `bar` when the products issued so far by this thread are done.
+__device__ __forceinline__ void commit(uint64_t* bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar))
+               : "memory");
+}
+// 32 columns of this thread's lane; complete on return.
+__device__ __forceinline__ void load32(uint32_t taddr, float (&v)[32]) {
+  uint32_t r[32];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+        "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+        "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr)
+      : "memory");
+#pragma unroll
+  for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+
+__device__ __forceinline__ void st_shared16(uint32_t addr, const uint32_t (&w)[4]) {
+  asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3])
+               : "memory");
+}
+__device__ __forceinline__ void ld_shared16(uint32_t addr, uint32_t (&w)[4]) {
+  asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(addr)
+               : "memory");
+}
+// 16-byte piece c of row `row` of a swizzled tile.
+__device__ __forceinline__ uint32_t piece(uint32_t tile, int row, int c) {
+  return tile + row * 128 + ((c ^ (row & 7)) << 4);
+}
+// 32 values of a row as bfloat16: pieces c .. c + 3.
+__device__ __forceinline__ void put32(uint32_t tile, int row, int c, const float (&x)[32]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = pack2(x[8 * i + 2 * j], x[8 * i + 2 * j + 1]);
+    st_shared16(piece(tile, row, c + i), w);
+  }
+}
+// The dot product of 32 values with pieces c .. c + 3 of a row.
+__device__ __forceinline__ float dot32(uint32_t tile, int row, int c, const float (&x)[32]) {
+  float s = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t w[4];
+    ld_shared16(piece(tile, row, c + i), w);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      s = fmaf(x[8 * i + 2 * j], lo_f(w[j]), s);
+      s = fmaf(x[8 * i + 2 * j + 1], hi_f(w[j]), s);
+    }
+  }
+  return s;
+}
+__device__ __forceinline__ void store32(__nv_bfloat16* p, const float (&x)[32]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = pack2(x[8 * i + 2 * j], x[8 * i + 2 * j + 1]);
+    *reinterpret_cast<uint4*>(p + 8 * i) = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+__device__ __forceinline__ void store32(float* p, const float (&x)[32]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    *reinterpret_cast<float4*>(p + 4 * i) = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+}
+// Sums over the warp of 32 values a lane: lane i returns the sum of x[i]. Halves are exchanged with the
+// lane 16, 8, 4, 2, 1 away: 31 shuffles, and each sum in one fixed order.
+__device__ __forceinline__ float column_sums(float (&x)[32]) {
+  const int l = threadIdx.x & 31;
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) {
+    const bool up = l & d;
+#pragma unroll
+    for (int i = 0; i < d; ++i) {
+      const float give = up ? x[i] : x[i + d], keep = up ? x[i + d] : x[i];
+      x[i] = keep + __shfl_xor_sync(0xffffffffu, give, d);
+    }
+  }
+  return x[0];
+}
+
+}  // namespace tc
+
+template <int DK, int DVB>
+struct TcSmem {
+  static constexpr int kT8 = 8192;  // a 64 x 64 tile
+  static constexpr int kS = DK * 128;
+  // offsets: [Q K] per 64 columns; per part of Dv [dO dR U S dS]; P' M; dU per part; T
+  static constexpr int kQK = 0, kPart0 = DK / 64 * 2 * kT8, kPart = 3 * kT8 + 2 * kS;
+  static constexpr int kP = kPart0 + DVB * kPart, kDU = kP + 2 * kT8, kT = kDU + DVB * kT8;
+  static constexpr int kGates0 = kT + kT8 + 1024;  // the product with T^T reads 1 KB past T
+  static constexpr int kGateStage = kGateFloats<1> * 4;
+  // row sums by column half, column sums by warp, <S, dS'> by warp: two sets in turn
+  static constexpr int kSums = 2 * 5 * 64 + 4 * 64 + 8;
+  static constexpr int kSums0 = kGates0 + 2 * kGateStage, kBars0 = kSums0 + 2 * 4 * kSums;
+  static constexpr int kBytes = kBars0 + 10 * 8 + 16;
+  static constexpr int kColumns = DK == 128 ? 512 : 256;
+  static constexpr int kX13 = 0, kX2 = DK, kDPA = 2 * DK, kQKK = 2 * DK + 64, kDR = DK /* X2's, and for Dk 64 DPA's */,
+                       kY1 = 2 * DK, kY2 = DK == 128 ? 384 : 192;
+};
+
+template <typename TG, int DK, int DVB>
+__global__ void __launch_bounds__(288, DK == 64 && DVB == 1 ? 2 : 1)
+grad_tc_kernel(const Problem P, const __grid_constant__ Maps M, const __nv_bfloat16* __restrict__ v,
+               TG* __restrict__ dq, TG* __restrict__ dk, int heads, __nv_bfloat16* __restrict__ dv,
+               __nv_bfloat16* __restrict__ dg, __nv_bfloat16* __restrict__ dbeta, uint32_t total) {
+  extern __shared__ __align__(1024) unsigned char smem[];
+  using L = TcSmem<DK, DVB>;
+  const uint32_t base = smem_addr(smem);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::kBars0);
+  // arrivals: loads of (T, dU, gates), (dO, U, S, dS), (Q, K); products dR, X and scores, Y; warps: dR is
+  // written, the scores' matrices are, everything has been read
+  uint64_t *la = bars, *lb = bars + 1, *lc = bars + 2, *m1 = bars + 3, *m2 = bars + 4, *m3 = bars + 5, *e1 = bars + 6,
+           *e2 = bars + 7, *e3 = bars + 8;
+  uint32_t* tmem_at = reinterpret_cast<uint32_t*>(bars + 10);
+  const int warp = threadIdx.x >> 5, l = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < 6; ++i) mbar_init(&bars[i], 1);
+    mbar_init(e1, 4);
+    mbar_init(e2, 8);
+    mbar_init(e3, 8);
+    fence_mbar_init();
+  }
+  if (warp == 8) tmem_alloc(tmem_at, L::kColumns);
+  tmem_fence_before_sync();
+  __syncthreads();
+  tmem_fence_after_sync();
+  const uint32_t tm = *tmem_at;
+  const auto where = [&](uint32_t item) {
+    const uint32_t bh = item / (uint32_t)P.n;
+    return locate(P, bh, (int)(item - bh * P.n));
+  };
+  // the next chunk with real steps, or `total`
+  const auto next = [&](uint32_t item) {
+    while (item < total && where(item).rows <= 0) item += gridDim.x;
+    return item;
+  };
+  if (warp == 8) {
+    if (l == 0) {
+      const auto load_a = [&](uint32_t item, int n) {
+        if (item >= total) return;
+        const Where w = where(item);
+        mbar_arrive_expect_tx(la, L::kT8 + DVB * L::kT8 + L::kGateStage);
+        bulk_load(base + L::kT, P.T + w.nc * L::kT8, L::kT8, la);
+        bulk_load(base + L::kDU, P.dU + w.nc * DVB * L::kT8, DVB * L::kT8, la);
+        bulk_load(base + L::kGates0 + (n & 1) * L::kGateStage, P.gates + w.nc * kGates, L::kGateStage, la);
+      };
+      const auto load_b = [&](uint32_t item) {
+        if (item >= total) return;
+        const Where w = where(item);
+        mbar_arrive_expect_tx(lb, DVB * (2 * L::kT8 + 2 * L::kS));
+#pragma unroll
+        for (int p = 0; p < DVB; ++p) {
+          const uint32_t at = base + L::kPart0 + p * L::kPart;
+          const int64_t tile = w.nc * DVB + p;
+          load_rows<1>(Tile<8, 1, true>{at}, &M.d_o, lb, v, 0, w.h * P.Dv + 64 * p, w.t, w.b, P.L, 0, 0);
+          bulk_load(at + 2 * L::kT8, P.U + tile * L::kT8, L::kT8, lb);
+          bulk_load(at + 3 * L::kT8, P.S + tile * L::kS, L::kS, lb);
+          bulk_load(at + 3 * L::kT8 + L::kS, P.dS + tile * L::kS, L::kS, lb);
+        }
+      };
+      const auto load_c = [&](uint32_t item) {
+        if (item >= total) return;
+        const Where w = where(item);
+        mbar_arrive_expect_tx(lc, DK / 64 * 2 * L::kT8);
+#pragma unroll
+        for (int j = 0; j < DK / 64; ++j) {
+          load_rows<1>(Tile<8, 1, true>{base + 2 * j * L::kT8}, &M.q, lc, v, 0, w.hk * DK + 64 * j, w.t, w.b, P.L, 0, 0);
+          load_rows<1>(Tile<8, 1, true>{base + (2 * j + 1) * L::kT8}, &M.k, lc, v, 0, w.hk * DK + 64 * j, w.t, w.b, P.L,
+                       0, 0);
+        }
+      };
+      uint32_t item = next(blockIdx.x);
+      load_a(item, 0);
+      load_b(item);
+      load_c(item);
+      for (int n = 0; item < total; ++n) {
+        const uint32_t ph = n & 1, after = next(item + gridDim.x);
+        mbar_wait(la, ph, P.err);
+        if (n > 0) {
+          mbar_wait(e3, ph ^ 1, P.err);  // the last chunk's accumulators have been read
+          load_c(item);
+        }
+        tmem_fence_after_sync();
+#pragma unroll
+        for (int p = 0; p < DVB; ++p)  // dR = T^T dU
+          tc::mma_k<4>(tm + L::kDR + 64 * p, tc::desc(base + L::kT, 1024, 128, false), 2048,
+                       tc::desc(base + L::kDU + p * L::kT8, 1024, 128, false), 2048, tc::instr(64, true, true), false);
+        tc::commit(m1);
+        mbar_wait(lb, ph, P.err);
+        mbar_wait(lc, ph, P.err);
+#pragma unroll
+        for (int j = 0; j < DK / 64; ++j)  // [Q; K] K^T
+          tc::mma_k<4>(tm + L::kQKK, tc::desc(base + 2 * j * L::kT8, 16, 1024, true), 32,
+                       tc::desc(base + (2 * j + 1) * L::kT8, 16, 1024, true), 32, tc::instr(64, false, false), j > 0);
+        mbar_wait(e1, ph, P.err);
+        tmem_fence_after_sync();
+#pragma unroll
+        for (int p = 0; p < DVB; ++p) {
+          const uint32_t at = base + L::kPart0 + p * L::kPart;
+          const uint64_t od = tc::desc(at, 16, 1024, true);  // [dO; dR]
+          tc::mma_k<4>(tm + L::kDPA, od, 32, tc::desc(at + 2 * L::kT8, 128, 1024, false), 256,
+                       tc::instr(64, false, false), p > 0);
+          tc::mma_k<4>(tm + L::kX13, od, 32, tc::desc(at + 3 * L::kT8, DK * 16, 128, false), 2 * DK * 16,
+                       tc::instr(DK, false, true), p > 0);
+          tc::mma_k<4>(tm + L::kX2, tc::desc(at + L::kT8, 128, 1024, false), 256,  // rows 64..: U
+                       tc::desc(at + 3 * L::kT8 + L::kS, DK * 16, 128, false), 2 * DK * 16,
+                       tc::instr(DK, false, true), p > 0);
+        }
+        tc::commit(m2);
+        mbar_wait(e2, ph, P.err);
+        tmem_fence_after_sync();
+        const uint64_t kb = tc::desc(base + L::kT8, 2 * L::kT8, 1024, true);  // K, Q as right operands
+        const uint64_t qb = tc::desc(base, 2 * L::kT8, 1024, true);
+        tc::mma_k<4>(tm + L::kY1, tc::desc(base + L::kP, 16, 1024, true), 32, kb, 2048, tc::instr(DK, false, true),
+                     false);
+        tc::mma_k<4>(tm + L::kY2, tc::desc(base + L::kP - L::kT8, L::kT8, 1024, true), 2048, qb, 2048,
+                     tc::instr(DK, true, true), false);
+        tc::mma_k<4>(tm + L::kY2, tc::desc(base + L::kP, L::kT8, 1024, true), 2048, kb, 2048,
+                     tc::instr(DK, true, true), true);
+        tc::commit(m3);
+        // all warps have passed their waits for these loads and read what came with them (e2), the products too (m2)
+        load_a(after, n + 1);
+        load_b(after);
+        item = after;
+      }
+    }
+    __syncwarp();
+  } else {
+    const int quad = warp & 3, hf = warp >> 2, side = quad >> 1;  // side 0: dQ's terms, 1: dK's
+    const int row = 32 * (quad & 1) + l;
+    const uint32_t lane = tm + ((uint32_t)(32 * quad) << 16);
+    const int64_t ldo = (int64_t)P.Hv * P.Dv;
+    int n = 0;
+    for (uint32_t item = blockIdx.x; item < total; item += gridDim.x) {
+      const Where w = where(item);
+      const int hq = heads == P.Hk ? w.hk : w.h;
+      if (w.rows < kC && w.len < P.L) {
+        for (int i = 0; i < kC; ++i) {
+          const int64_t t = padding_step(P, w, i);
+          if (t < 0) continue;
+          const int64_t at = w.b * P.L + t;
+          for (int j = threadIdx.x; j < DK / 2; j += 256) {
+            store_pair(dq + (at * heads + hq) * DK + 2 * j, 0.0f, 0.0f);
+            store_pair(dk + (at * heads + hq) * DK + 2 * j, 0.0f, 0.0f);
+          }
+          for (int j = threadIdx.x; j < P.Dv / 2; j += 256)
+            store_pair(dv + (at * P.Hv + w.h) * P.Dv + 2 * j, 0.0f, 0.0f);
+          if (threadIdx.x == 0) {
+            store_one(dg + at * P.Hv + w.h, 0.0f);
+            store_one(dbeta + at * P.Hv + w.h, 0.0f);
+          }
+        }
+      }
+      if (w.rows <= 0) continue;
+      const uint32_t ph = n & 1;
+      const float* G = reinterpret_cast<const float*>(smem + L::kGates0 + (n & 1) * L::kGateStage);
+      float* rows = reinterpret_cast<float*>(smem + L::kSums0) + (n & 1) * L::kSums;  // [half][5][64]
+      float* cols = rows + 2 * 5 * 64;                                              // [quad][64]
+      float* dots = cols + 4 * 64;
+      const bool real = row < w.rows;
+      float bsum = 0.0f;  // dbeta's part without S
+      if (side == 0) {  // dR, dV
+        uint4 vr[DVB][4];
+#pragma unroll
+        for (int p = 0; p < DVB; ++p)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            vr[p][i] = real ? __ldg(reinterpret_cast<const uint4*>(v + (w.step + row) * P.ldv + w.h * P.Dv + 64 * p +
+                                                                   32 * hf) + i)
+                            : make_uint4(0, 0, 0, 0);
+        mbar_wait(la, ph, P.err);
+        mbar_wait(m1, ph, P.err);
+        tmem_fence_after_sync();
+        const float bt = G[kBeta + row];
+#pragma unroll
+        for (int p = 0; p < DVB; ++p) {
+          float r[32];
+          tc::load32(lane + L::kDR + 64 * p + 32 * hf, r);
+          tc::put32(base + L::kPart0 + p * L::kPart + L::kT8, row, 4 * hf, r);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t x[4] = {vr[p][i].x, vr[p][i].y, vr[p][i].z, vr[p][i].w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              bsum = fmaf(r[8 * i + 2 * j], lo_f(x[j]), bsum);
+              bsum = fmaf(r[8 * i + 2 * j + 1], hi_f(x[j]), bsum);
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < 32; ++i) r[i] *= bt;
+          if (real) tc::store32(dv + (w.step + row) * ldo + w.h * P.Dv + 64 * p + 32 * hf, r);
+        }
+        fence_proxy_async_smem();
+        tmem_fence_before_sync();
+        __syncwarp();
+        if (l == 0) mbar_arrive(e1);
+      } else {  // <S, dS'>
+        mbar_wait(la, ph, P.err);
+        mbar_wait(lb, ph, P.err);
+        float s = 0.0f;
+        const int t = 64 * hf + 32 * (quad & 1) + l;
+#pragma unroll
+        for (int p = 0; p < DVB; ++p) {
+          const uint32_t at = base + L::kPart0 + p * L::kPart + 3 * L::kT8;
+#pragma unroll 4
+          for (int i = 16 * t; i < L::kS; i += 128 * 16) s += dot16<1, 0>(at + i, at + L::kS + i);
+        }
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+        if (l == 0) dots[2 * hf + (quad & 1)] = s;
+      }
+      mbar_wait(m2, ph, P.err);
+      tmem_fence_after_sync();
+      float rsum = 0.0f;
+      {  // scores: this thread's row, 32 columns
+        const uint32_t tile = base + L::kP + side * L::kT8;
+        float x[32], y[32];
+        if ((quad & 1) == 0 && hf == 1) {  // all above the diagonal
+#pragma unroll
+          for (int i = 0; i < 32; ++i) x[i] = 0.0f;
+          tc::put32(tile, row, 4, x);
+          cols[quad * 64 + 32 + l] = 0.0f;
+        } else {
+          tc::load32(lane + L::kDPA + 32 * hf, x);
+          tc::load32(lane + L::kQKK + 32 * hf, y);
+          const float gi = G[row], bt = G[kBeta + row];
+          float4 gj = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            const int j = 32 * hf + i;
+            if ((i & 3) == 0) gj = *reinterpret_cast<const float4*>(&G[j]);
+            const float g = (i & 3) == 0 ? gj.x : (i & 3) == 1 ? gj.y : (i & 3) == 2 ? gj.z : gj.w;
+            const float d = __expf(fminf(gi - g, 0.0f));
+            if (side == 0) {
+              x[i] = j <= row ? P.scale * x[i] * d : 0.0f;
+              y[i] *= x[i];
+              rsum += y[i];
+            } else {
+              const float m0 = j < row ? -x[i] * d : 0.0f, mk = m0 * y[i];
+              bsum += mk;
+              x[i] = bt * m0;
+              y[i] = bt * mk;
+              rsum += y[i];
+            }
+          }
+          tc::put32(tile, row, 4 * hf, x);
+          cols[quad * 64 + 32 * hf + l] = tc::column_sums(y);
+        }
+      }
+      fence_proxy_async_smem();
+      tmem_fence_before_sync();
+      __syncwarp();
+      if (l == 0) mbar_arrive(e2);
+      // row products, and this thread's half of a row of dQ or dK without the scores' part
+      float acc[DK / 64][32], y1 = 0.0f, y2 = 0.0f;
+      {
+        const float up = G[kUp + row], fa = side == 0 ? P.scale * up : -G[kBeta + row] * up, fb = G[kDown + row];
+#pragma unroll
+        for (int c = 0; c < DK / 64; ++c) {
+          const int col = hf * (DK / 2) + 32 * c;  // of Dk
+          const uint32_t tile = base + (2 * (col >> 6) + side) * L::kT8;  // Q's rows, or K's
+          float x[32];
+          tc::load32(lane + L::kX13 + col, x);
+          y1 += tc::dot32(tile, row, (col & 63) >> 3, x);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) acc[c][i] = fa * x[i];
+          if (side == 1) {
+            tc::load32(lane + L::kX2 + col, x);
+            y2 += tc::dot32(tile, row, (col & 63) >> 3, x);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) acc[c][i] = fmaf(fb, x[i], acc[c][i]);
+          }
+        }
+      }
+      // by half: [0] dR.v and the scores' part of dbeta, [1] x1.q, [2] x2.k, [3] x3.k, [4] row sums
+      if (side == 0) {
+        rows[(hf * 5 + 0) * 64 + row] = bsum;
+        rows[(hf * 5 + 1) * 64 + row] = y1;
+        rows[(hf * 5 + 4) * 64 + row] = rsum;
+      } else {
+        rows[(hf * 5 + 2) * 64 + row] = y2;
+        rows[(hf * 5 + 3) * 64 + row] = y1;
+      }
+      asm volatile("bar.sync 1, 256;" ::: "memory");
+      if (side == 1) {  // the other side's entries are complete: add this side's
+        rows[(hf * 5 + 0) * 64 + row] += bsum;
+        rows[(hf * 5 + 4) * 64 + row] += rsum;
+      }
+      asm volatile("bar.sync 1, 256;" ::: "memory");
+      mbar_wait(m3, ph, P.err);
+      tmem_fence_after_sync();
+#pragma unroll
+      for (int c = 0; c < DK / 64; ++c) {
+        const int col = hf * (DK / 2) + 32 * c;
+        float x[32];
+        tc::load32(lane + L::kY1 + col, x);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) acc[c][i] += x[i];
+        if (side == 1) {
+          tc::load32(lane + L::kY2 + col, x);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) acc[c][i] += x[i];
+        }
+      }
+      tmem_fence_before_sync();
+      __syncwarp();
+      if (l == 0) mbar_arrive(e3);
+      if (real) {
+        TG* out = (side == 0 ? dq : dk) + ((w.step + row) * heads + hq) * DK + hf * (DK / 2);
+#pragma unroll
+        for (int c = 0; c < DK / 64; ++c) tc::store32(out + 32 * c, acc[c]);
+      }
+      if (warp == 0) {  // dbeta, and dg: the cumulative decay's gradient summed from the end
+        float dG[2], add = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int i = 2 * l + e;
+          float a[5];
+#pragma unroll
+          for (int x = 0; x < 5; ++x) a[x] = rows[x * 64 + i] + rows[(5 + x) * 64 + i];
+          const float up = G[kUp + i], down = G[kDown + i];
+          const float col = (cols[i] + cols[64 + i]) + (cols[128 + i] + cols[192 + i]);
+          dG[e] = P.scale * up * a[1] - G[kBeta + i] * up * a[3] - down * a[2] + a[4] - col;
+          add += down * a[2];
+          if (i < w.rows) store_one(dbeta + (w.step + i) * P.Hv + w.h, a[0] - up * a[3]);
+        }
+        const float all = (dots[0] + dots[1]) + (dots[2] + dots[3]);
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) add += __shfl_xor_sync(0xffffffffu, add, d);
+        if (l == 31) dG[1] += add + G[kUp + 63] * all;
+        float s = dG[0] + dG[1];
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+          const float o = __shfl_down_sync(0xffffffffu, s, d);
+          if (l + d < 32) s += o;
+        }
+        if (2 * l < w.rows) store_one(dg + (w.step + 2 * l) * P.Hv + w.h, s);
+        if (2 * l + 1 < w.rows) store_one(dg + (w.step + 2 * l + 1) * P.Hv + w.h, s - dG[0]);
+      }
+      ++n;
+    }
+  }
+  tmem_fence_before_sync();
+  __syncthreads();
+  tmem_fence_after_sync();
+  if (warp == 8) tmem_dealloc(tm, L::kColumns);
+}
+
+}  // namespace gdr
+}  // namespace blr

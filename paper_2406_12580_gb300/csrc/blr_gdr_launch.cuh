@@ -2,6 +2,7 @@
 #pragma once
 
 #include "blr_gdr_bwd.cuh"
+#include "blr_gdr_grad.cuh"
 #include "blr_gdr_fwd.cuh"
 #include "blr_gdr_launch.h"
 
@@ -47,13 +48,33 @@ blr_status fwd_dk(const Problem& p, const FwdCall& c) {
                static_cast<TI*>(c.o));
 }
 
+template <typename TI, typename TG, int DK, int DVB>
+blr_status grad_tc(const Problem& p, const BwdCall& c, TG* dq, TG* dk, int heads) {
+  const int64_t chunks = p.B * p.Hv * p.n, most = 152 * (DK == 64 && DVB == 1 ? 2 : 1);
+  return start("grad", grad_tc_kernel<TG, DK, DVB>, chunks < most ? chunks : most, 288, TcSmem<DK, DVB>::kBytes,
+               c.stream, p, c.maps, static_cast<const TI*>(c.v), dq, dk, heads, static_cast<TI*>(c.dv),
+               static_cast<TI*>(c.dg), static_cast<TI*>(c.dbeta), (uint32_t)chunks);
+}
+
+template <typename TI, typename TG, int DK, int NI, int NM>
+blr_status grad(const Problem& p, const BwdCall& c, TG* dq, TG* dk, int heads) {
+  if constexpr (NM == 1) {  // wider values do not fit beside each other in shared memory
+    if (p.Dv == 64) return grad_tc<TI, TG, DK, 1>(p, c, dq, dk, heads);
+    if (p.Dv == 128) return grad_tc<TI, TG, DK, 2>(p, c, dq, dk, heads);
+  }
+  // 16 warps an SM hide each other's latencies; float32's operands take the registers of 8
+  constexpr int kParts = NM == 3 || DK == 64 ? 2 : 4, bytes = GradSmem<DK, NI, NM, kParts>::kBytes;
+  return start("grad", grad_kernel<TI, TG, DK, NI, NM, kParts>, p.B * p.Hv * p.n, 128 * kParts, bytes, c.stream, p,
+               c.maps, static_cast<const TI*>(c.q), static_cast<const TI*>(c.k), static_cast<const TI*>(c.v),
+               static_cast<const TI*>(c.d_o), dq, dk, heads, static_cast<TI*>(c.dv), static_cast<TI*>(c.dg),
+               static_cast<TI*>(c.dbeta));
+}
+
 template <typename TI, int DK, int NI, int NM>
 blr_status bwd_dk(const Problem& p, const BwdCall& c) {
   const int64_t chunks = p.B * p.Hv * p.n;
-  const TI *q = static_cast<const TI*>(c.q), *k = static_cast<const TI*>(c.k), *v = static_cast<const TI*>(c.v),
-           *d_o = static_cast<const TI*>(c.d_o);
-  TI *dq = static_cast<TI*>(c.dq), *dk = static_cast<TI*>(c.dk_out), *dv = static_cast<TI*>(c.dv),
-     *dg = static_cast<TI*>(c.dg), *dbeta = static_cast<TI*>(c.dbeta);
+  const TI *q = static_cast<const TI*>(c.q), *k = static_cast<const TI*>(c.k), *d_o = static_cast<const TI*>(c.d_o);
+  TI *dq = static_cast<TI*>(c.dq), *dk = static_cast<TI*>(c.dk_out);
   BLR_TRY(start("du", du_kernel<TI, DK, NI, NM>, chunks, 128, DuSmem<DK, NI>::kBytes, c.stream, p, c.maps, q, k, d_o));
   // two stages of float32 tiles and 64 columns do not fit beside each other
   constexpr int kWide = 2 * BackSmem<DK, NI, NM, 4>::kStage <= 227 * 1024 ? 4 : 2;
@@ -71,13 +92,11 @@ blr_status bwd_dk(const Problem& p, const BwdCall& c) {
   else
     BLR_TRY(start("back", back_kernel<TI, DK, NI, NM, 2, false>, heads * p.nseg * (p.Dv / 32),
                   32 * (2 + kLoadWarps<NI>), narrow, c.stream, p, c.maps, q, k, d_o, c.ds_last, c.ds0));
-  // 16 warps an SM hide each other's latencies; float32's operands take the registers of 8
-  constexpr int kParts = NM == 3 || DK == 64 ? 2 : 4, bytes = GradSmem<DK, NI, NM, kParts>::kBytes;
   if (p.Hk == p.Hv)
-    return start("grad", grad_kernel<TI, TI, DK, NI, NM, kParts>, chunks, 128 * kParts, bytes, c.stream, p, c.maps, q, k, v,
-                 d_o, dq, dk, p.Hk, dv, dg, dbeta);
-  BLR_TRY(start("grad", grad_kernel<TI, float, DK, NI, NM, kParts>, chunks, 128 * kParts, bytes, c.stream, p, c.maps, q, k, v,
-                d_o, p.pq, p.pk, p.Hv, dv, dg, dbeta));
+    BLR_TRY((grad<TI, TI, DK, NI, NM>(p, c, dq, dk, p.Hk)));
+  else
+    BLR_TRY((grad<TI, float, DK, NI, NM>(p, c, p.pq, p.pk, p.Hv)));
+  if (p.Hk == p.Hv) return BLR_OK;
   const int64_t pairs = p.B * p.L * p.Hk * (DK / 2), blocks = (pairs + 255) / 256;
   return start("share", share_kernel<TI>, blocks < 152 * 16 ? blocks : 152 * 16, 256, 0, c.stream,
                (const float*)p.pq, (const float*)p.pk, dq, dk, pairs, p.Hv / p.Hk, DK / 2);
