@@ -36,6 +36,7 @@ has its autograd operator and a layer), and the AdamW step of a whole model
 from __future__ import annotations
 
 import ctypes
+import operator
 
 from ._lib import (BLR_BF16, BLR_ERR_CUDA, BLR_ERR_INVALID_ARG, BLR_ERR_TIMEOUT,  # noqa: F401
                    BLR_ERR_UNSUPPORTED, BLR_ERR_WORKSPACE, BLR_F32, BLR_OK, blr_desc, blr_gdr_desc,
@@ -323,19 +324,18 @@ def blr_adamw_step(params, grads, m, v, *, lr: float, step: int, beta1: float = 
         raise TypeError("moments are float32 or float8_e4m3fn")
     device = torch._C._cuda_getDevice()
     table = np.zeros((n, 8), dtype=np.int64)
-    sizes = [t.numel() for t in params]
+    T, dtype_of = torch.Tensor, operator.attrgetter("dtype")  # C-level loops: a model has hundreds of tensors
+    sizes = [*map(T.numel, params)]
     blocks = [-(-x // 256) for x in sizes] if eight else None
     for column, (name, ts) in enumerate(lists.items()):
         if ts is None:
             continue
         dtype, want = dtypes.get(name, torch.float32), blocks if "scales" in name else sizes
-        if len(ts) == n:
-            fit = [t.dtype is dtype and t.get_device() == device and t.is_contiguous() and t.numel() == x
-                   for t, x in zip(ts, want)]
-        if len(ts) != n or not all(fit):
+        if (len(ts) != n or {*map(dtype_of, ts)} != {dtype} or {*map(T.get_device, ts)} != {device}
+                or not all(map(T.is_contiguous, ts)) or [*map(T.numel, ts)] != want):
             raise ValueError(f"{name}: {n} contiguous {dtype} tensors of the parameters' sizes on the current CUDA "
                              "device are wanted")
-        table[:, column] = [t.data_ptr() for t in ts]
+        table[:, column] = [*map(T.data_ptr, ts)]
     table[:, 7] = sizes
     _check(load().blr_adamw_step(n, table.ctypes.data, io, 8 if eight else 32, lr, beta1, beta2, eps,
                                  weight_decay, step, _ptr(grad_scale, "grad_scale"), _stream(stream)),

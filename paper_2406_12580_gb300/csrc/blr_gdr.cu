@@ -211,8 +211,13 @@ blr_status blr_gdr_bwd(const blr_gdr_desc* desc, int flags, const int32_t* lengt
   BLR_TRY(blr::need(dg, "dg", e));
   BLR_TRY(blr::need(dbeta, "dbeta", e));
   const Problem p = make_problem(desc, s, l, lengths, ws);
-  blr::gdr::BwdCall c{(int)s.Dk, d_o, ds_last, q, k, v, dq, dk, dv, dg, dbeta, ds0, stream, {}};
+  blr::gdr::BwdCall c{(int)s.Dk, d_o, ds_last, q, k, v, dq, dk, dv, dg, dbeta, ds0, stream, {}, {}};
   BLR_TRY(make_maps(desc, s, q, k, v, d_o, &c.maps));
+  if (desc->io == BLR_BF16) {
+    BLR_TRY(make_map(s, dq, s.Hk * s.Dk, s.Hk * s.Dk, &c.grads.dq));
+    BLR_TRY(make_map(s, dk, s.Hk * s.Dk, s.Hk * s.Dk, &c.grads.dk));
+    BLR_TRY(make_map(s, dv, s.Hv * s.Dv, s.Hv * s.Dv, &c.grads.dv));
+  }
   if (desc->io == BLR_F32) return blr::gdr::bwd_f32(p, c);
   return l.np == 2 ? blr::gdr::bwd_bf16_state(p, c) : blr::gdr::bwd_bf16(p, c);
 }

@@ -357,6 +357,21 @@ __device__ __forceinline__ float dot16(uint32_t a, uint32_t b) {
   return s;
 }
 
+// The gradients of the padding that the chunk's free slots stand for.
+template <int DK, typename TI, typename TG>
+__device__ __forceinline__ void zero_gradients(const Problem& P, const Where& w, TG* dq, TG* dk, int heads, int hq, TI* dv,
+                                               TI* dg, TI* dbeta, int tid, int threads) {
+  const Padding pad = padding(P, w);
+  const int64_t at = w.b * P.L + pad.first;
+  zero_rows(dq + (at * heads + hq) * DK, (int64_t)heads * DK, pad.count, DK, tid, threads);
+  zero_rows(dk + (at * heads + hq) * DK, (int64_t)heads * DK, pad.count, DK, tid, threads);
+  zero_rows(dv + (at * P.Hv + w.h) * P.Dv, (int64_t)P.Hv * P.Dv, pad.count, P.Dv, tid, threads);
+  if (tid < pad.count) {
+    store_one(dg + (at + tid) * P.Hv + w.h, 0.0f);
+    store_one(dbeta + (at + tid) * P.Hv + w.h, 0.0f);
+  }
+}
+
 // Everything else, for all chunks at once. Warp (rg, pt) holds rows 16 rg .. of the chunk and one of
 // PARTS parts of the columns of each product.
 template <typename TI, typename TG, int DK, int NI, int NM, int PARTS>
@@ -372,22 +387,7 @@ grad_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restric
   const Where w = locate(P);
   const int tid = threadIdx.x, warp = tid >> 5, l = tid & 31, rg = warp & 3, pt = warp >> 2;
   const int hq = heads == P.Hk ? w.hk : w.h;
-  if (w.rows < kC && w.len < P.L) {
-    for (int i = 0; i < kC; ++i) {
-      const int64_t t = padding_step(P, w, i);
-      if (t < 0) continue;
-      const int64_t at = w.b * P.L + t;
-      for (int j = tid; j < DK / 2; j += THREADS) {
-        store_pair(dq + (at * heads + hq) * DK + 2 * j, 0.0f, 0.0f);
-        store_pair(dk + (at * heads + hq) * DK + 2 * j, 0.0f, 0.0f);
-      }
-      for (int j = tid; j < P.Dv / 2; j += THREADS) store_pair(dv + (at * P.Hv + w.h) * P.Dv + 2 * j, 0.0f, 0.0f);
-      if (tid == 0) {
-        store_one(dg + at * P.Hv + w.h, 0.0f);
-        store_one(dbeta + at * P.Hv + w.h, 0.0f);
-      }
-    }
-  }
+  if (w.rows < kC && w.len < P.L) zero_gradients<DK>(P, w, dq, dk, heads, hq, dv, dg, dbeta, tid, THREADS);
   if (w.rows <= 0) return;
   const uint32_t base = smem_addr(smem);
   const InTile<DK / 8, NI> tq{base}, tk{base + L::kQ};

@@ -608,10 +608,8 @@ output_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restr
   const Where w = locate(P);
   const int tid = threadIdx.x, warp = tid >> 5, l = tid & 31;
   if (w.rows < kC && w.len < P.L) {
-    for (int i = tid; i < kC * (P.Dv / 2); i += 128) {
-      const int64_t t = padding_step(P, w, i / (P.Dv / 2));
-      if (t >= 0) store_pair(o + ((w.b * P.L + t) * P.Hv + w.h) * P.Dv + 2 * (i % (P.Dv / 2)), 0.0f, 0.0f);
-    }
+    const Padding pad = padding(P, w);
+    zero_rows(o + ((w.b * P.L + pad.first) * P.Hv + w.h) * P.Dv, (int64_t)P.Hv * P.Dv, pad.count, P.Dv, tid, 128);
   }
   if (w.rows <= 0) return;
   const uint32_t base = smem_addr(smem);

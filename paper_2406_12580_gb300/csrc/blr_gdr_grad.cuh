@@ -13,8 +13,10 @@
 //
 // Bound by memory at Dk = Dv = 128: 216 KB a chunk, 0.52 ms of 16384 chunks. A persistent block an SM
 // works on one chunk at a time; each of its buffers is refilled for the next chunk as soon as its last
-// product is done, so the loads run beside the arithmetic on the scores and gradients (8 warps) and one
-// thread issues loads and products.
+// reader is done, so the loads run beside the arithmetic on the scores and gradients (8 warps). One
+// thread issues loads, products and the gradients' stores, whose tiles are staged in buffers that are
+// idle then (16-byte stores of a row a thread had taken 3600 of a chunk's 17000 cycles); a tenth warp
+// sums the gates' gradients behind the others.
 #pragma once
 
 #include "blr_gdr_bwd.cuh"
@@ -73,6 +75,13 @@ __device__ __forceinline__ void load32(uint32_t taddr, float (&v)[32]) {
   for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
 }
 
+// A staged 64 x 64 tile to steps step .. of batch row b, columns col ..; steps past the row's end are not written.
+__device__ __forceinline__ void store_tile(const CUtensorMap* map, uint32_t tile, int col, int64_t step, int b) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map), "r"(tile),
+               "r"(col), "r"((int)step), "r"(b)
+               : "memory");
+}
+
 __device__ __forceinline__ void st_shared16(uint32_t addr, const uint32_t (&w)[4]) {
   asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3])
                : "memory");
@@ -110,15 +119,6 @@ __device__ __forceinline__ float dot32(uint32_t tile, int row, int c, const floa
   }
   return s;
 }
-__device__ __forceinline__ void store32(__nv_bfloat16* p, const float (&x)[32]) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    uint32_t w[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) w[j] = pack2(x[8 * i + 2 * j], x[8 * i + 2 * j + 1]);
-    *reinterpret_cast<uint4*>(p + 8 * i) = make_uint4(w[0], w[1], w[2], w[3]);
-  }
-}
 __device__ __forceinline__ void store32(float* p, const float (&x)[32]) {
 #pragma unroll
   for (int i = 0; i < 8; ++i)
@@ -146,40 +146,52 @@ template <int DK, int DVB>
 struct TcSmem {
   static constexpr int kT8 = 8192;  // a 64 x 64 tile
   static constexpr int kS = DK * 128;
-  // offsets: [Q K] per 64 columns; per part of Dv [dO dR U S dS]; P' M; dU per part; T
+  // offsets: [Q K] per 64 columns; per part of Dv [dO dR U S dS]; P' M; dU, V per part; T
   static constexpr int kQK = 0, kPart0 = DK / 64 * 2 * kT8, kPart = 3 * kT8 + 2 * kS;
-  static constexpr int kP = kPart0 + DVB * kPart, kDU = kP + 2 * kT8, kT = kDU + DVB * kT8;
-  static constexpr int kGates0 = kT + kT8 + 1024;  // the product with T^T reads 1 KB past T
+  static constexpr int kP = kPart0 + DVB * kPart, kDU = kP + 2 * kT8, kV = kDU + DVB * kT8, kT = kV + DVB * kT8;
+  static constexpr int kMore = kT + kT8;  // the product with T^T reads 1 KB past T
+  static constexpr int kGates0 = kMore + (DK == 128 && DVB == 1 ? kT8 : 1024);
   static constexpr int kGateStage = kGateFloats<1> * 4;
-  // row sums by column half, column sums by warp, <S, dS'> by warp: two sets in turn
-  static constexpr int kSums = 2 * 5 * 64 + 4 * 64 + 8;
-  static constexpr int kSums0 = kGates0 + 2 * kGateStage, kBars0 = kSums0 + 2 * 4 * kSums;
-  static constexpr int kBytes = kBars0 + 10 * 8 + 16;
+  // row sums by column half, column sums by warp; <S, dS'> by warp, two sets in turn
+  static constexpr int kSums0 = kGates0 + 2 * kGateStage, kSums = 2 * 5 * 64 + 4 * 64 + 2 * 4;
+  static constexpr int kBars0 = kSums0 + 4 * kSums;
+  static constexpr int kBytes = kBars0 + 12 * 8;
   static constexpr int kColumns = DK == 128 ? 512 : 256;
-  static constexpr int kX13 = 0, kX2 = DK, kDPA = 2 * DK, kQKK = 2 * DK + 64, kDR = DK /* X2's, and for Dk 64 DPA's */,
-                       kY1 = 2 * DK, kY2 = DK == 128 ? 384 : 192;
+  static constexpr int kX13 = 0, kX2 = DK, kDPA = 2 * DK, kQKK = 2 * DK + 64, kY1 = 2 * DK,
+                       kY2 = DK == 128 ? 384 : 192;
+  // dR's columns: of sums that begin only after it has been read
+  static __device__ constexpr int dr(int p) { return DK == 128 ? kY2 + 64 * p : p == 0 ? kDPA : kX13; }
+  // Where 64 columns of dQ and dK are staged: in P', M, then in the tiles of dR
+  static __device__ constexpr int stage_q(int j) { return kP + j * kT8; }
+  static __device__ constexpr int stage_k(int j) {
+    return DK == 64 ? kP + kT8 : j < DVB ? kPart0 + j * kPart + kT8 : kMore;
+  }
 };
 
 template <typename TG, int DK, int DVB>
-__global__ void __launch_bounds__(288, DK == 64 && DVB == 1 ? 2 : 1)
-grad_tc_kernel(const Problem P, const __grid_constant__ Maps M, const __nv_bfloat16* __restrict__ v,
+__global__ void __launch_bounds__(320, DK == 64 && DVB == 1 ? 2 : 1)
+grad_tc_kernel(const Problem P, const __grid_constant__ Maps M, const __grid_constant__ GradMaps O,
                TG* __restrict__ dq, TG* __restrict__ dk, int heads, __nv_bfloat16* __restrict__ dv,
                __nv_bfloat16* __restrict__ dg, __nv_bfloat16* __restrict__ dbeta, uint32_t total) {
+  // dq, dk: `heads` heads a step. Float gradients (of value heads that share a key head) are stored directly.
+  constexpr bool kStaged = sizeof(TG) == 2;
   extern __shared__ __align__(1024) unsigned char smem[];
   using L = TcSmem<DK, DVB>;
   const uint32_t base = smem_addr(smem);
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::kBars0);
-  // arrivals: loads of (T, dU, gates), (dO, U, S, dS), (Q, K); products dR, X and scores, Y; warps: dR is
-  // written, the scores' matrices are, everything has been read
+  // arrivals: loads of (T, dU, V, gates), (dO, U, S, dS), (Q, K); products dR, X and scores, Y; warps: dR is
+  // written, the scores' matrices are, all sums have been read, the row sums are written, and are read
   uint64_t *la = bars, *lb = bars + 1, *lc = bars + 2, *m1 = bars + 3, *m2 = bars + 4, *m3 = bars + 5, *e1 = bars + 6,
-           *e2 = bars + 7, *e3 = bars + 8;
-  uint32_t* tmem_at = reinterpret_cast<uint32_t*>(bars + 10);
+           *e2 = bars + 7, *e3 = bars + 8, *e4 = bars + 9, *r4 = bars + 10;
+  uint32_t* tmem_at = reinterpret_cast<uint32_t*>(bars + 11);
   const int warp = threadIdx.x >> 5, l = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int i = 0; i < 6; ++i) mbar_init(&bars[i], 1);
     mbar_init(e1, 4);
     mbar_init(e2, 8);
     mbar_init(e3, 8);
+    mbar_init(e4, 8);
+    mbar_init(r4, 1);
     fence_mbar_init();
   }
   if (warp == 8) tmem_alloc(tmem_at, L::kColumns);
@@ -196,15 +208,23 @@ grad_tc_kernel(const Problem P, const __grid_constant__ Maps M, const __nv_bfloa
     while (item < total && where(item).rows <= 0) item += gridDim.x;
     return item;
   };
+  float* rows = reinterpret_cast<float*>(smem + L::kSums0);  // [half][5][64]
+  float* cols = rows + 2 * 5 * 64;                           // [quad][64]
+  float* dots = cols + 4 * 64;
   if (warp == 8) {
     if (l == 0) {
+      const __nv_bfloat16* none = nullptr;
       const auto load_a = [&](uint32_t item, int n) {
         if (item >= total) return;
         const Where w = where(item);
-        mbar_arrive_expect_tx(la, L::kT8 + DVB * L::kT8 + L::kGateStage);
+        mbar_arrive_expect_tx(la, L::kT8 + 2 * DVB * L::kT8 + L::kGateStage);
         bulk_load(base + L::kT, P.T + w.nc * L::kT8, L::kT8, la);
         bulk_load(base + L::kDU, P.dU + w.nc * DVB * L::kT8, DVB * L::kT8, la);
         bulk_load(base + L::kGates0 + (n & 1) * L::kGateStage, P.gates + w.nc * kGates, L::kGateStage, la);
+#pragma unroll
+        for (int p = 0; p < DVB; ++p)
+          load_rows<1>(Tile<8, 1, true>{base + L::kV + p * L::kT8}, &M.v, la, none, 0, w.h * P.Dv + 64 * p, w.t, w.b,
+                       P.L, 0, 0);
       };
       const auto load_b = [&](uint32_t item) {
         if (item >= total) return;
@@ -214,7 +234,7 @@ grad_tc_kernel(const Problem P, const __grid_constant__ Maps M, const __nv_bfloa
         for (int p = 0; p < DVB; ++p) {
           const uint32_t at = base + L::kPart0 + p * L::kPart;
           const int64_t tile = w.nc * DVB + p;
-          load_rows<1>(Tile<8, 1, true>{at}, &M.d_o, lb, v, 0, w.h * P.Dv + 64 * p, w.t, w.b, P.L, 0, 0);
+          load_rows<1>(Tile<8, 1, true>{at}, &M.d_o, lb, none, 0, w.h * P.Dv + 64 * p, w.t, w.b, P.L, 0, 0);
           bulk_load(at + 2 * L::kT8, P.U + tile * L::kT8, L::kT8, lb);
           bulk_load(at + 3 * L::kT8, P.S + tile * L::kS, L::kS, lb);
           bulk_load(at + 3 * L::kT8 + L::kS, P.dS + tile * L::kS, L::kS, lb);
@@ -226,9 +246,10 @@ grad_tc_kernel(const Problem P, const __grid_constant__ Maps M, const __nv_bfloa
         mbar_arrive_expect_tx(lc, DK / 64 * 2 * L::kT8);
 #pragma unroll
         for (int j = 0; j < DK / 64; ++j) {
-          load_rows<1>(Tile<8, 1, true>{base + 2 * j * L::kT8}, &M.q, lc, v, 0, w.hk * DK + 64 * j, w.t, w.b, P.L, 0, 0);
-          load_rows<1>(Tile<8, 1, true>{base + (2 * j + 1) * L::kT8}, &M.k, lc, v, 0, w.hk * DK + 64 * j, w.t, w.b, P.L,
-                       0, 0);
+          load_rows<1>(Tile<8, 1, true>{base + 2 * j * L::kT8}, &M.q, lc, none, 0, w.hk * DK + 64 * j, w.t, w.b, P.L, 0,
+                       0);
+          load_rows<1>(Tile<8, 1, true>{base + (2 * j + 1) * L::kT8}, &M.k, lc, none, 0, w.hk * DK + 64 * j, w.t, w.b,
+                       P.L, 0, 0);
         }
       };
       uint32_t item = next(blockIdx.x);
@@ -237,18 +258,23 @@ grad_tc_kernel(const Problem P, const __grid_constant__ Maps M, const __nv_bfloa
       load_c(item);
       for (int n = 0; item < total; ++n) {
         const uint32_t ph = n & 1, after = next(item + gridDim.x);
+        const Where w = where(item);
         mbar_wait(la, ph, P.err);
-        if (n > 0) {
-          mbar_wait(e3, ph ^ 1, P.err);  // the last chunk's accumulators have been read
-          load_c(item);
-        }
+        bulk_wait_read<0>();  // the last chunk's gradients have left the tiles that dR goes to
         tmem_fence_after_sync();
 #pragma unroll
         for (int p = 0; p < DVB; ++p)  // dR = T^T dU
-          tc::mma_k<4>(tm + L::kDR + 64 * p, tc::desc(base + L::kT, 1024, 128, false), 2048,
+          tc::mma_k<4>(tm + L::dr(p), tc::desc(base + L::kT, 1024, 128, false), 2048,
                        tc::desc(base + L::kDU + p * L::kT8, 1024, 128, false), 2048, tc::instr(64, true, true), false);
         tc::commit(m1);
         mbar_wait(lb, ph, P.err);
+#pragma unroll
+        for (int p = 0; p < DVB; ++p) {  // rows 64..: U dS'^T
+          const uint32_t at = base + L::kPart0 + p * L::kPart;
+          tc::mma_k<4>(tm + L::kX2, tc::desc(at + L::kT8, 128, 1024, false), 256,
+                       tc::desc(at + 3 * L::kT8 + L::kS, DK * 16, 128, false), 2 * DK * 16,
+                       tc::instr(DK, false, true), p > 0);
+        }
         mbar_wait(lc, ph, P.err);
 #pragma unroll
         for (int j = 0; j < DK / 64; ++j)  // [Q; K] K^T
@@ -264,11 +290,12 @@ grad_tc_kernel(const Problem P, const __grid_constant__ Maps M, const __nv_bfloa
                        tc::instr(64, false, false), p > 0);
           tc::mma_k<4>(tm + L::kX13, od, 32, tc::desc(at + 3 * L::kT8, DK * 16, 128, false), 2 * DK * 16,
                        tc::instr(DK, false, true), p > 0);
-          tc::mma_k<4>(tm + L::kX2, tc::desc(at + L::kT8, 128, 1024, false), 256,  // rows 64..: U
-                       tc::desc(at + 3 * L::kT8 + L::kS, DK * 16, 128, false), 2 * DK * 16,
-                       tc::instr(DK, false, true), p > 0);
         }
         tc::commit(m2);
+#pragma unroll
+        for (int p = 0; p < DVB; ++p)  // dV has been staged where dU was
+          tc::store_tile(&O.dv, base + L::kDU + p * L::kT8, w.h * P.Dv + 64 * p, w.t, w.b);
+        bulk_commit();
         mbar_wait(e2, ph, P.err);
         tmem_fence_after_sync();
         const uint64_t kb = tc::desc(base + L::kT8, 2 * L::kT8, 1024, true);  // K, Q as right operands
@@ -281,55 +308,75 @@ grad_tc_kernel(const Problem P, const __grid_constant__ Maps M, const __nv_bfloa
                      tc::instr(DK, true, true), true);
         tc::commit(m3);
         // all warps have passed their waits for these loads and read what came with them (e2), the products too (m2)
-        load_a(after, n + 1);
         load_b(after);
+        bulk_wait_read<0>();
+        load_a(after, n + 1);
+        mbar_wait(e3, ph, P.err);
+        load_c(after);
+        if constexpr (kStaged) {
+          const int hq = heads == P.Hk ? w.hk : w.h;
+#pragma unroll
+          for (int j = 0; j < DK / 64; ++j) {
+            tc::store_tile(&O.dq, base + L::stage_q(j), hq * DK + 64 * j, w.t, w.b);
+            tc::store_tile(&O.dk, base + L::stage_k(j), hq * DK + 64 * j, w.t, w.b);
+          }
+          bulk_commit();
+        }
         item = after;
       }
+      bulk_wait_all();
     }
     __syncwarp();
+  } else if (warp == 9) {  // dbeta, and dg: the cumulative decay's gradient summed from the end
+    int n = 0;
+    for (uint32_t item = next(blockIdx.x); item < total; item = next(item + gridDim.x), ++n) {
+      const Where w = where(item);
+      const float* G = reinterpret_cast<const float*>(smem + L::kGates0 + (n & 1) * L::kGateStage);
+      mbar_wait(e4, n & 1, P.err);
+      float dG[2], add = 0.0f;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int i = 2 * l + e;
+        float a[5];
+#pragma unroll
+        for (int x = 0; x < 5; ++x) a[x] = rows[x * 64 + i] + rows[(5 + x) * 64 + i];
+        const float up = G[kUp + i], down = G[kDown + i];
+        const float col = (cols[i] + cols[64 + i]) + (cols[128 + i] + cols[192 + i]);
+        dG[e] = P.scale * up * a[1] - G[kBeta + i] * up * a[3] - down * a[2] + a[4] - col;
+        add += down * a[2];
+        if (i < w.rows) store_one(dbeta + (w.step + i) * P.Hv + w.h, a[0] - up * a[3]);
+      }
+      const float* dot = dots + 4 * (n & 1);
+      const float all = (dot[0] + dot[1]) + (dot[2] + dot[3]);
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) add += __shfl_xor_sync(0xffffffffu, add, d);
+      if (l == 31) dG[1] += add + G[kUp + 63] * all;
+      __syncwarp();
+      if (l == 0) mbar_arrive(r4);
+      float s = dG[0] + dG[1];
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const float o = __shfl_down_sync(0xffffffffu, s, d);
+        if (l + d < 32) s += o;
+      }
+      if (2 * l < w.rows) store_one(dg + (w.step + 2 * l) * P.Hv + w.h, s);
+      if (2 * l + 1 < w.rows) store_one(dg + (w.step + 2 * l + 1) * P.Hv + w.h, s - dG[0]);
+    }
   } else {
     const int quad = warp & 3, hf = warp >> 2, side = quad >> 1;  // side 0: dQ's terms, 1: dK's
     const int row = 32 * (quad & 1) + l;
     const uint32_t lane = tm + ((uint32_t)(32 * quad) << 16);
-    const int64_t ldo = (int64_t)P.Hv * P.Dv;
     int n = 0;
     for (uint32_t item = blockIdx.x; item < total; item += gridDim.x) {
       const Where w = where(item);
       const int hq = heads == P.Hk ? w.hk : w.h;
-      if (w.rows < kC && w.len < P.L) {
-        for (int i = 0; i < kC; ++i) {
-          const int64_t t = padding_step(P, w, i);
-          if (t < 0) continue;
-          const int64_t at = w.b * P.L + t;
-          for (int j = threadIdx.x; j < DK / 2; j += 256) {
-            store_pair(dq + (at * heads + hq) * DK + 2 * j, 0.0f, 0.0f);
-            store_pair(dk + (at * heads + hq) * DK + 2 * j, 0.0f, 0.0f);
-          }
-          for (int j = threadIdx.x; j < P.Dv / 2; j += 256)
-            store_pair(dv + (at * P.Hv + w.h) * P.Dv + 2 * j, 0.0f, 0.0f);
-          if (threadIdx.x == 0) {
-            store_one(dg + at * P.Hv + w.h, 0.0f);
-            store_one(dbeta + at * P.Hv + w.h, 0.0f);
-          }
-        }
-      }
+      if (w.rows < kC && w.len < P.L)
+        zero_gradients<DK>(P, w, dq, dk, heads, hq, dv, dg, dbeta, (int)threadIdx.x, 256);
       if (w.rows <= 0) continue;
       const uint32_t ph = n & 1;
       const float* G = reinterpret_cast<const float*>(smem + L::kGates0 + (n & 1) * L::kGateStage);
-      float* rows = reinterpret_cast<float*>(smem + L::kSums0) + (n & 1) * L::kSums;  // [half][5][64]
-      float* cols = rows + 2 * 5 * 64;                                              // [quad][64]
-      float* dots = cols + 4 * 64;
-      const bool real = row < w.rows;
       float bsum = 0.0f;  // dbeta's part without S
-      if (side == 0) {  // dR, dV
-        uint4 vr[DVB][4];
-#pragma unroll
-        for (int p = 0; p < DVB; ++p)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            vr[p][i] = real ? __ldg(reinterpret_cast<const uint4*>(v + (w.step + row) * P.ldv + w.h * P.Dv + 64 * p +
-                                                                   32 * hf) + i)
-                            : make_uint4(0, 0, 0, 0);
+      if (side == 0) {    // dR, dV
         mbar_wait(la, ph, P.err);
         mbar_wait(m1, ph, P.err);
         tmem_fence_after_sync();
@@ -337,20 +384,12 @@ grad_tc_kernel(const Problem P, const __grid_constant__ Maps M, const __nv_bfloa
 #pragma unroll
         for (int p = 0; p < DVB; ++p) {
           float r[32];
-          tc::load32(lane + L::kDR + 64 * p + 32 * hf, r);
+          tc::load32(lane + L::dr(p) + 32 * hf, r);
           tc::put32(base + L::kPart0 + p * L::kPart + L::kT8, row, 4 * hf, r);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t x[4] = {vr[p][i].x, vr[p][i].y, vr[p][i].z, vr[p][i].w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              bsum = fmaf(r[8 * i + 2 * j], lo_f(x[j]), bsum);
-              bsum = fmaf(r[8 * i + 2 * j + 1], hi_f(x[j]), bsum);
-            }
-          }
+          bsum += tc::dot32(base + L::kV + p * L::kT8, row, 4 * hf, r);
 #pragma unroll
           for (int i = 0; i < 32; ++i) r[i] *= bt;
-          if (real) tc::store32(dv + (w.step + row) * ldo + w.h * P.Dv + 64 * p + 32 * hf, r);
+          tc::put32(base + L::kDU + p * L::kT8, row, 4 * hf, r);
         }
         fence_proxy_async_smem();
         tmem_fence_before_sync();
@@ -369,10 +408,11 @@ grad_tc_kernel(const Problem P, const __grid_constant__ Maps M, const __nv_bfloa
         }
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
-        if (l == 0) dots[2 * hf + (quad & 1)] = s;
+        if (l == 0) dots[4 * (n & 1) + 2 * hf + (quad & 1)] = s;
       }
       mbar_wait(m2, ph, P.err);
       tmem_fence_after_sync();
+      if (n > 0) mbar_wait(r4, ph ^ 1, P.err);  // the last chunk's row and column sums have been read
       float rsum = 0.0f;
       {  // scores: this thread's row, 32 columns
         const uint32_t tile = base + L::kP + side * L::kT8;
@@ -448,7 +488,8 @@ grad_tc_kernel(const Problem P, const __grid_constant__ Maps M, const __nv_bfloa
         rows[(hf * 5 + 0) * 64 + row] += bsum;
         rows[(hf * 5 + 4) * 64 + row] += rsum;
       }
-      asm volatile("bar.sync 1, 256;" ::: "memory");
+      __syncwarp();
+      if (l == 0) mbar_arrive(e4);
       mbar_wait(m3, ph, P.err);
       tmem_fence_after_sync();
 #pragma unroll
@@ -463,41 +504,21 @@ grad_tc_kernel(const Problem P, const __grid_constant__ Maps M, const __nv_bfloa
 #pragma unroll
           for (int i = 0; i < 32; ++i) acc[c][i] += x[i];
         }
+        if constexpr (kStaged) {
+          const int j = col >> 6;
+          tc::put32(base + (side == 0 ? L::stage_q(j) : L::stage_k(j)), row, (col & 63) >> 3, acc[c]);
+        }
       }
+      fence_proxy_async_smem();
       tmem_fence_before_sync();
       __syncwarp();
       if (l == 0) mbar_arrive(e3);
-      if (real) {
-        TG* out = (side == 0 ? dq : dk) + ((w.step + row) * heads + hq) * DK + hf * (DK / 2);
+      if constexpr (!kStaged) {
+        if (row < w.rows) {
+          TG* out = (side == 0 ? dq : dk) + ((w.step + row) * heads + hq) * DK + hf * (DK / 2);
 #pragma unroll
-        for (int c = 0; c < DK / 64; ++c) tc::store32(out + 32 * c, acc[c]);
-      }
-      if (warp == 0) {  // dbeta, and dg: the cumulative decay's gradient summed from the end
-        float dG[2], add = 0.0f;
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int i = 2 * l + e;
-          float a[5];
-#pragma unroll
-          for (int x = 0; x < 5; ++x) a[x] = rows[x * 64 + i] + rows[(5 + x) * 64 + i];
-          const float up = G[kUp + i], down = G[kDown + i];
-          const float col = (cols[i] + cols[64 + i]) + (cols[128 + i] + cols[192 + i]);
-          dG[e] = P.scale * up * a[1] - G[kBeta + i] * up * a[3] - down * a[2] + a[4] - col;
-          add += down * a[2];
-          if (i < w.rows) store_one(dbeta + (w.step + i) * P.Hv + w.h, a[0] - up * a[3]);
+          for (int c = 0; c < DK / 64; ++c) tc::store32(out + 32 * c, acc[c]);
         }
-        const float all = (dots[0] + dots[1]) + (dots[2] + dots[3]);
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) add += __shfl_xor_sync(0xffffffffu, add, d);
-        if (l == 31) dG[1] += add + G[kUp + 63] * all;
-        float s = dG[0] + dG[1];
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-          const float o = __shfl_down_sync(0xffffffffu, s, d);
-          if (l + d < 32) s += o;
-        }
-        if (2 * l < w.rows) store_one(dg + (w.step + 2 * l) * P.Hv + w.h, s);
-        if (2 * l + 1 < w.rows) store_one(dg + (w.step + 2 * l + 1) * P.Hv + w.h, s - dG[0]);
       }
       ++n;
     }

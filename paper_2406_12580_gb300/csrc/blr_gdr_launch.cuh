@@ -51,9 +51,9 @@ blr_status fwd_dk(const Problem& p, const FwdCall& c) {
 template <typename TI, typename TG, int DK, int DVB>
 blr_status grad_tc(const Problem& p, const BwdCall& c, TG* dq, TG* dk, int heads) {
   const int64_t chunks = p.B * p.Hv * p.n, most = 152 * (DK == 64 && DVB == 1 ? 2 : 1);
-  return start("grad", grad_tc_kernel<TG, DK, DVB>, chunks < most ? chunks : most, 288, TcSmem<DK, DVB>::kBytes,
-               c.stream, p, c.maps, static_cast<const TI*>(c.v), dq, dk, heads, static_cast<TI*>(c.dv),
-               static_cast<TI*>(c.dg), static_cast<TI*>(c.dbeta), (uint32_t)chunks);
+  return start("grad", grad_tc_kernel<TG, DK, DVB>, chunks < most ? chunks : most, 320, TcSmem<DK, DVB>::kBytes,
+               c.stream, p, c.maps, c.grads, dq, dk, heads, static_cast<TI*>(c.dv), static_cast<TI*>(c.dg),
+               static_cast<TI*>(c.dbeta), (uint32_t)chunks);
 }
 
 template <typename TI, typename TG, int DK, int NI, int NM>

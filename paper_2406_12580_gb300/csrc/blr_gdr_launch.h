@@ -27,6 +27,7 @@ struct BwdCall {
   float* ds0;
   cudaStream_t stream;
   Maps maps;
+  GradMaps grads;
 };
 
 blr_status fwd_f32(const Problem& p, const FwdCall& c);

@@ -253,6 +253,10 @@ __host__ __device__ constexpr uint32_t tma_bytes(int bytes) { return P == 1 ? by
 struct Maps {
   CUtensorMap q, k, v, d_o;
 };
+// The gradients, as TMA stores them.
+struct GradMaps {
+  CUtensorMap dq, dk, dv;
+};
 
 // Calls f(piece, row, column block) for a thread's 16-byte pieces of a 64 x 8 C8 tile: piece i is row
 // 8 (i / (8 C8)) + i % 8, column block (i / 8) % C8, so that a warp reads at least 64 bytes of 8 rows.
@@ -435,10 +439,23 @@ __device__ __forceinline__ Segment segment(const Problem& P, const Where& w0, in
   s.last = max(0, (s.chunks - 1) / P.seg_chunks);
   return s;
 }
-// The padding step that slot i of the chunk stands for, or -1.
-__device__ __forceinline__ int64_t padding_step(const Problem& P, const Where& w, int i) {
-  const int64_t s = (int64_t)w.c * kC + i;
-  return s >= w.len && s < P.L ? s - w.len : -1;
+// The padding steps that the chunk's slots past the row's end stand for: [first, first + count).
+struct Padding {
+  int64_t first;
+  int count;
+};
+__device__ __forceinline__ Padding padding(const Problem& P, const Where& w) {
+  const int64_t s0 = (int64_t)w.c * kC, from = w.len > s0 ? w.len : s0, to = s0 + kC < P.L ? s0 + kC : P.L;
+  return {from - w.len, from < to ? (int)(to - from) : 0};
+}
+// Zeroes `cols` values (a multiple of 8) of each of `count` rows at distance `ld`.
+template <typename T>
+__device__ __forceinline__ void zero_rows(T* p, int64_t ld, int count, int cols, int tid, int threads) {
+  const int pieces = cols * (int)sizeof(T) / 16;
+  for (int i = tid; i < count * pieces; i += threads) {
+    const int r = i / pieces;
+    *reinterpret_cast<uint4*>(reinterpret_cast<char*>(p + r * ld) + 16 * (i - r * pieces)) = make_uint4(0, 0, 0, 0);
+  }
 }
 
 }  // namespace gdr
