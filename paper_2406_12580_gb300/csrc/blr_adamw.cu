@@ -1,11 +1,15 @@
 // One AdamW step over many tensors (blr_adamw_step in blr.h).
 //
-// Per value, float32, each operation rounded on its own (no contraction, so
-// that 8-bit codes do not hang on how the compiler fuses a sum):
+// Per value, in float32:
 //     m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2,  r = sqrt(v)
 //     w = w (1 - lr wd) - m / (r / sqrt(1 - b2^t) + eps) * lr / (1 - b1^t)
-// Bound by memory: 28 bytes a value with float32 everywhere, 30 with bfloat16
-// parameters and float32 masters, about 10 with bfloat16 and 8-bit moments.
+// What the moments take is rounded operation by operation (no contraction): an
+// 8-bit code must not hang on how the compiler fuses a sum, or two builds would
+// drift apart by whole codes. Bound by memory with float32 moments: 28 bytes a
+// value with float32 everywhere, 28 with bfloat16 parameters and float32 masters
+// (190 M values: 771 us, 6.9 TB/s). With 8-bit moments about 10 bytes a value
+// are left and the instructions bound the kernel; the quotient, a thousandth of
+// w, is then approximate to two units in the last place.
 //
 // Layout: the tensors' records travel in the kernel's parameters (nothing is
 // copied to the device, nothing is kept between calls), up to kMaxTensors a
@@ -26,7 +30,11 @@ using blr::fail;
 
 constexpr int kThreads = 256;
 constexpr int kGroup = 256;   // values a warp takes at a time, one scale of the 8-bit moments
-constexpr int kChunk = 4096;  // values a block takes: two groups a warp
+// Values a block takes. A block first finds its tensor; with 8-bit moments, where that counts, 16384 values
+// spread it over eight groups a warp (285 -> 259 us of 95 M values; with float32 moments, which wait for
+// memory alone, 771 -> 794). A small model (under 4 M values) keeps its blocks many.
+constexpr int kChunk = 4096, kCodesChunk = 16384;
+constexpr int64_t kSmallModel = (int64_t)4 << 20;
 constexpr int kMaxTensors = 448;
 constexpr int kFewTensors = 32;
 constexpr float kE4m3Max = 448.0f;
@@ -37,7 +45,7 @@ struct Table {
   blr_adamw_tensor t[CAP];
   uint32_t first[CAP];  // first chunk of each tensor
   uint32_t wide[(CAP + 31) / 32];  // whether its pointers allow wide accesses
-  int count;
+  int count, chunk;
 };
 static_assert(sizeof(Table<kMaxTensors>) < 32000, "kernel parameters hold 32764 bytes");
 
@@ -90,12 +98,6 @@ template <> struct Eight<__nv_bfloat16> {
   static __device__ __forceinline__ void put(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
 };
 
-__device__ __forceinline__ float fast_sqrt(float x) {
-  float y;
-  asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-
 // e4m3 codes (two at a time) to and from floats, by the conversion instructions.
 __device__ __forceinline__ float2 from_e4m3x2(uint16_t c) {
   const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)c, __NV_E4M3);
@@ -113,36 +115,40 @@ __device__ __forceinline__ uint2 load_codes(const uint8_t* p, int n, bool wide) 
     if (i < n) w[i >> 2] |= (uint32_t)p[i] << (8 * (i & 3));
   return make_uint2(w[0], w[1]);
 }
-__device__ __forceinline__ void decode(uint2 c, float scale, float (&x)[8]) {
+__device__ __forceinline__ void decode(uint2 c, float (&x)[8]) {
   const uint32_t w[2] = {c.x, c.y};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const float2 f = from_e4m3x2((uint16_t)(w[i >> 1] >> (16 * (i & 1))));
-    x[2 * i] = __fmul_rn(f.x, scale);
-    x[2 * i + 1] = __fmul_rn(f.y, scale);
+    x[2 * i] = f.x;
+    x[2 * i + 1] = f.y;
   }
 }
 
-// Writes the codes and the scale of a warp's group; `tiny`: the least code of a positive value.
-__device__ __forceinline__ void store_codes(uint8_t* p, float* scale, int n, bool wide, float tiny,
-                                            const float (&x)[8]) {
-  // magnitudes order as their bits do, and a NaN's are above all others
-  uint32_t bits = 0;
+// Writes the codes and the scale of a warp's group. A NaN stays with its own value; ROOT: values are not
+// negative, and a positive one is stored as no less than the smallest code.
+template <bool ROOT>
+__device__ __forceinline__ void store_codes(uint8_t* p, float* scale, int n, bool wide, const float (&x)[8]) {
+  float top = 0.0f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) bits = max(bits, __float_as_uint(x[i]) & 0x7fffffffu);
-  const float top = __uint_as_float(__reduce_max_sync(0xffffffffu, bits));
+  for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[i]));
+  top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));  // magnitudes order as their bits
   const float inverse = top > 0.0f ? fminf(__fmul_rn(__fdiv_rn(1.0f, top), kE4m3Max), 3.402823466e38f) : 0.0f;
-  uint32_t w[2] = {0u, 0u};
+  uint32_t w[2];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    float y[2];
+  for (int h = 0; h < 2; ++h) {
+    uint16_t c[2];
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const float v = x[2 * i + j];
-      y[j] = __fmul_rn(v, inverse);
-      if (tiny > 0.0f && v > 0.0f) y[j] = fmaxf(y[j], tiny);
+    for (int i = 0; i < 2; ++i) {
+      float y[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        y[j] = __fmul_rn(x[4 * h + 2 * i + j], inverse);
+        if (ROOT) y[j] = y[j] > 0.0f ? fmaxf(y[j], kE4m3Tiny) : y[j];
+      }
+      c[i] = to_e4m3x2(y[0], y[1]);
     }
-    w[i >> 1] |= (uint32_t)to_e4m3x2(y[0], y[1]) << (16 * (i & 1));
+    w[h] = (uint32_t)c[0] | (uint32_t)c[1] << 16;
   }
   if (wide) {
     __stcs(reinterpret_cast<uint2*>(p), make_uint2(w[0], w[1]));
@@ -174,7 +180,7 @@ __device__ __forceinline__ void store8(T* p, int n, bool wide, const float (&x)[
 }
 
 template <typename T, int BITS, bool MASTER, int CAP>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, BITS == 8 ? 5 : 1)
 adamw_kernel(const __grid_constant__ Table<CAP> table, const __grid_constant__ Hyper h) {
   // the last tensor whose first chunk is not after this block
   int lo = 0, hi = table.count - 1;
@@ -183,97 +189,70 @@ adamw_kernel(const __grid_constant__ Table<CAP> table, const __grid_constant__ H
     if (table.first[mid] <= blockIdx.x) lo = mid; else hi = mid - 1;
   }
   const blr_adamw_tensor& t = table.t[lo];
-  const int64_t n = t.n, begin = (int64_t)(blockIdx.x - table.first[lo]) * kChunk;
+  const int64_t n = t.n, begin = (int64_t)(blockIdx.x - table.first[lo]) * table.chunk;
   const bool aligned = (table.wide[lo >> 5] >> (lo & 31)) & 1u;
   const float gs = h.grad_scale == nullptr ? 1.0f : __ldg(h.grad_scale);
+  const bool scaled = h.grad_scale != nullptr;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   constexpr int kStride = (kThreads / 32) * kGroup;
-  constexpr int kHeld = BITS == 8 ? kChunk / kStride : 1;  // groups whose loads are in flight together
-#pragma unroll
-  for (int it0 = 0; it0 < kChunk / kStride; it0 += kHeld) {
-    float w[kHeld][8], g[kHeld][8], m[kHeld][8], v[kHeld][8];
-    uint2 mc[kHeld], vc[kHeld];
-    float ms[kHeld], vs[kHeld];
-#pragma unroll
-    for (int k = 0; k < kHeld; ++k) {
-      const int64_t at = begin + (it0 + k) * kStride + warp * kGroup;
-      if (at >= n) break;  // by whole warps
-      const bool wide = aligned && at + kGroup <= n;
-      const int64_t i0 = at + lane * 8;
-      const int left = wide ? 8 : (int)max((int64_t)0, min((int64_t)8, n - i0));
-      if constexpr (MASTER) {
-        load8<float>(t.w + i0, left, wide, w[k]);
-      } else {
-        load8<T>(static_cast<const T*>(t.p) + i0, left, wide, w[k]);
-      }
-      load8<T>(static_cast<const T*>(t.g) + i0, left, wide, g[k]);
-      if constexpr (BITS == 32) {
-        load8<float>(static_cast<const float*>(t.m) + i0, left, wide, m[k]);
-        load8<float>(static_cast<const float*>(t.v) + i0, left, wide, v[k]);
-      } else {
-        const int64_t block = at / kGroup;
-        mc[k] = load_codes(static_cast<const uint8_t*>(t.m) + i0, left, wide);
-        vc[k] = load_codes(static_cast<const uint8_t*>(t.v) + i0, left, wide);
-        ms[k] = t.m_scale[block];
-        vs[k] = t.v_scale[block];
-      }
+  for (int64_t at = begin + warp * kGroup; at < min(n, begin + table.chunk); at += kStride) {  // by whole warps
+    float w[8], g[8], m[8], v[8];
+    const bool wide = aligned && at + kGroup <= n;
+    const int64_t i0 = at + lane * 8, block = at / kGroup;
+    const int left = wide ? 8 : (int)max((int64_t)0, min((int64_t)8, n - i0));
+    if constexpr (MASTER) {
+      load8<float>(t.w + i0, left, wide, w);
+    } else {
+      load8<T>(static_cast<const T*>(t.p) + i0, left, wide, w);
     }
-#pragma unroll
-    for (int k = 0; k < kHeld; ++k) {
-      const int64_t at = begin + (it0 + k) * kStride + warp * kGroup;
-      if (at >= n) break;
-      const bool wide = aligned && at + kGroup <= n;
-      const int64_t i0 = at + lane * 8;
-      const int left = wide ? 8 : (int)max((int64_t)0, min((int64_t)8, n - i0));
-      if constexpr (BITS == 8) {
-        decode(mc[k], ms[k], m[k]);
-        decode(vc[k], vs[k], v[k]);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[k][i] = __fmul_rn(v[k][i], v[k][i]);
-      }
+    load8<T>(static_cast<const T*>(t.g) + i0, left, wide, g);
+    if constexpr (BITS == 32) {
+      load8<float>(static_cast<const float*>(t.m) + i0, left, wide, m);
+      load8<float>(static_cast<const float*>(t.v) + i0, left, wide, v);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float gi = __fmul_rn(g[k][i], gs);
-        m[k][i] = __fadd_rn(__fmul_rn(m[k][i], h.b1), __fmul_rn(gi, h.c1));
-        v[k][i] = __fadd_rn(__fmul_rn(v[k][i], h.b2), __fmul_rn(__fmul_rn(gi, gi), h.c2));
-        // With 8-bit moments the instructions bound the kernel: root and quotient to two units in the
-        // last place there (a root is stored in 4 bits of precision, the quotient is a thousandth of w).
-        const float r = BITS == 8 ? fast_sqrt(v[k][i]) : __fsqrt_rn(v[k][i]);
-        const float d = __fadd_rn(__fmul_rn(r, h.root_scale), h.eps);
-        const float u = BITS == 8 ? __fdividef(m[k][i], d) : __fdiv_rn(m[k][i], d);
-        w[k][i] = __fsub_rn(__fmul_rn(w[k][i], h.keep), __fmul_rn(u, h.rate));
-        if constexpr (BITS == 8) v[k][i] = r;
+        const float gi = __fmul_rn(g[i], gs);
+        m[i] = __fadd_rn(__fmul_rn(m[i], h.b1), __fmul_rn(gi, h.c1));
+        v[i] = __fadd_rn(__fmul_rn(v[i], h.b2), __fmul_rn(__fmul_rn(gi, gi), h.c2));
+        const float d = __fadd_rn(__fmul_rn(__fsqrt_rn(v[i]), h.root_scale), h.eps);
+        w[i] = __fsub_rn(__fmul_rn(w[i], h.keep), __fmul_rn(__fdiv_rn(m[i], d), h.rate));
       }
-      if constexpr (BITS == 32) {
-        store8<float>(static_cast<float*>(t.m) + i0, left, wide, m[k]);
-        store8<float>(static_cast<float*>(t.v) + i0, left, wide, v[k]);
-      } else {
-        const int64_t block = at / kGroup;
-        if (!wide) {  // values past the end have no part in the scale
+      store8<float>(static_cast<float*>(t.m) + i0, left, wide, m);
+      store8<float>(static_cast<float*>(t.v) + i0, left, wide, v);
+    } else {
+      const uint2 mc = load_codes(static_cast<const uint8_t*>(t.m) + i0, left, wide);
+      const uint2 vc = load_codes(static_cast<const uint8_t*>(t.v) + i0, left, wide);
+      const float ms = t.m_scale[block], vs = t.v_scale[block];
+      decode(mc, m);
+      decode(vc, v);
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (i >= left) m[k][i] = v[k][i] = 0.0f;
-        }
-        store_codes(static_cast<uint8_t*>(t.m) + i0, t.m_scale + block, left, wide, 0.0f, m[k]);
-        store_codes(static_cast<uint8_t*>(t.v) + i0, t.v_scale + block, left, wide, kE4m3Tiny, v[k]);
+      for (int i = 0; i < 8; ++i) {
+        const float gi = scaled ? __fmul_rn(g[i], gs) : g[i], r0 = __fmul_rn(v[i], vs);
+        m[i] = __fadd_rn(__fmul_rn(__fmul_rn(m[i], ms), h.b1), __fmul_rn(gi, h.c1));
+        v[i] = __fsqrt_rn(__fadd_rn(__fmul_rn(__fmul_rn(r0, r0), h.b2), __fmul_rn(__fmul_rn(gi, gi), h.c2)));
+        w[i] = w[i] * h.keep - __fdividef(m[i], v[i] * h.root_scale + h.eps) * h.rate;
+        if (!wide && i >= left) m[i] = v[i] = 0.0f;  // values past the end have no part in the scale
       }
-      if constexpr (MASTER) store8<float>(t.w + i0, left, wide, w[k]);
-      store8<T>(static_cast<T*>(t.p) + i0, left, wide, w[k]);
+      store_codes<false>(static_cast<uint8_t*>(t.m) + i0, t.m_scale + block, left, wide, m);
+      store_codes<true>(static_cast<uint8_t*>(t.v) + i0, t.v_scale + block, left, wide, v);
     }
+    if constexpr (MASTER) store8<float>(t.w + i0, left, wide, w);
+    store8<T>(static_cast<T*>(t.p) + i0, left, wide, w);
   }
 }
 
 template <typename T, int BITS, bool MASTER, int CAP>
-blr_status launch(const blr_adamw_tensor* tensors, int64_t& at, int64_t count, const Hyper& h,
+blr_status launch(const blr_adamw_tensor* tensors, int64_t& at, int64_t count, int chunk, const Hyper& h,
                   cudaStream_t stream) {
   Table<CAP> table;
   table.count = 0;
+  table.chunk = chunk;
   for (uint32_t& w : table.wide) w = 0;
   int64_t chunks = 0;
   for (; at < count && table.count < CAP; ++at) {
     const blr_adamw_tensor& t = tensors[at];
     if (t.n == 0) continue;
-    const int64_t more = (t.n + kChunk - 1) / kChunk;
+    const int64_t more = (t.n + chunk - 1) / chunk;
     if (chunks + more > 0x7fffffff) {
       if (table.count == 0) return fail(BLR_ERR_UNSUPPORTED, "tensor %lld is too large", (long long)at);
       break;
@@ -293,13 +272,15 @@ blr_status launch(const blr_adamw_tensor* tensors, int64_t& at, int64_t count, c
 
 template <typename T, int BITS, bool MASTER>
 blr_status step_all(const blr_adamw_tensor* tensors, int64_t count, const Hyper& h, cudaStream_t stream) {
-  int64_t at = 0;
+  int64_t at = 0, values = 0;
+  for (int64_t i = 0; i < count; ++i) values += tensors[i].n;
+  const int chunk = BITS == 8 && values >= kSmallModel ? kCodesChunk : kChunk;
   while (at < count) {
     // a small table keeps the launch of a small model short
     if (count - at <= kFewTensors)
-      BLR_TRY((launch<T, BITS, MASTER, kFewTensors>(tensors, at, count, h, stream)));
+      BLR_TRY((launch<T, BITS, MASTER, kFewTensors>(tensors, at, count, chunk, h, stream)));
     else
-      BLR_TRY((launch<T, BITS, MASTER, kMaxTensors>(tensors, at, count, h, stream)));
+      BLR_TRY((launch<T, BITS, MASTER, kMaxTensors>(tensors, at, count, chunk, h, stream)));
   }
   return BLR_OK;
 }
