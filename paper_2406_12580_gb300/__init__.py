@@ -36,11 +36,10 @@ has its autograd operator and a layer), and the AdamW step of a whole model
 from __future__ import annotations
 
 import ctypes
-import operator
 
 from ._lib import (BLR_BF16, BLR_ERR_CUDA, BLR_ERR_INVALID_ARG, BLR_ERR_TIMEOUT,  # noqa: F401
                    BLR_ERR_UNSUPPORTED, BLR_ERR_WORKSPACE, BLR_F32, BLR_OK, blr_desc, blr_gdr_desc,
-                   load)
+                   extension, load)
 
 __all__ = [
     "BLR_F32", "BLR_BF16", "Desc", "BLRError", "blr_workspace_bytes", "blr_scan_fwd",
@@ -103,7 +102,7 @@ def _ptr(t, name: str):
 def _stream(stream):
     if stream is None:
         import torch
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        return torch.cuda.current_stream().cuda_stream
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -241,24 +240,8 @@ def GDRDesc(B: int, L: int, Hk: int, Hv: int, Dk: int, Dv: int, ldq: int = 0, ld
     return blr_gdr_desc(B, L, Hk, Hv, Dk, Dv, ldq, ldk, ldv, io, scale)
 
 
-def _pointers(names: str, *tensors) -> list:
-    """_ptr of many tensors at once; a name with a star may be a slice of wider rows (its strides are
-    the descriptor's)."""
-    import torch
-    device = torch._C._cuda_getDevice()
-    out = []
-    for name, t in zip(names.split(), tensors):
-        if t is None or isinstance(t, int):
-            out.append(t)
-            continue
-        if not isinstance(t, torch.Tensor):
-            raise TypeError(f"{name}: expected a CUDA tensor, an int pointer or None")
-        if t.get_device() != device and t.numel() > 0:
-            raise ValueError(f"{name}: tensor must be on the current CUDA device")
-        if not t.is_contiguous() and not (name[0] == "*" and t.stride(-1) == 1):
-            raise ValueError(f"{name}: tensor must be contiguous")
-        out.append(t.data_ptr() or None)
-    return out
+def _raw_stream(stream):
+    return stream if stream is None or isinstance(stream, int) else stream.cuda_stream
 
 
 def _ws_bytes(ws) -> int:
@@ -271,19 +254,15 @@ def blr_gdr_workspace_bytes(desc: blr_gdr_desc, flags: int) -> int:
 
 def blr_gdr_fwd(desc, flags, lengths, q, k, v, g, beta, s0, o, s_last, ws, stream=None):
     """Gated delta rule over whole sequences (see include/blr.h)."""
-    _check(load().blr_gdr_fwd(ctypes.byref(desc), flags,
-                              *_pointers("lengths *q *k *v g beta s0 o s_last ws", lengths, q, k, v, g, beta, s0,
-                                         o, s_last, ws),
-                              _ws_bytes(ws), _stream(stream)),
+    _check(extension().gdr_fwd(ctypes.addressof(desc), flags, lengths, q, k, v, g, beta, s0, o, s_last, ws,
+                               _raw_stream(stream)),
            "blr_gdr_fwd")
 
 
 def blr_gdr_bwd(desc, flags, lengths, d_o, ds_last, q, k, v, g, beta, s0, dq, dk, dv, dg, dbeta, ds0, ws,
                 stream=None):
-    _check(load().blr_gdr_bwd(ctypes.byref(desc), flags,
-                              *_pointers("lengths d_o ds_last *q *k *v g beta s0 dq dk dv dg dbeta ds0 ws", lengths,
-                                         d_o, ds_last, q, k, v, g, beta, s0, dq, dk, dv, dg, dbeta, ds0, ws),
-                              _ws_bytes(ws), _stream(stream)),
+    _check(extension().gdr_bwd(ctypes.addressof(desc), flags, lengths, d_o, ds_last, q, k, v, g, beta, s0, dq, dk,
+                               dv, dg, dbeta, ds0, ws, _raw_stream(stream)),
            "blr_gdr_bwd")
 
 
@@ -294,9 +273,8 @@ def blr_gdr_status(ws, stream=None) -> int:
 
 def blr_gdr_steps(desc, state, s_prev, q, k, v, g, beta, s_out, o=None, stream=None):
     """desc.L recurrent steps per row (state dtype `state`, BLR_F32 or BLR_BF16); s_out may be s_prev."""
-    _check(load().blr_gdr_steps(ctypes.byref(desc), state,
-                                *_pointers("s_prev *q *k *v g beta s_out o", s_prev, q, k, v, g, beta, s_out, o),
-                                _stream(stream)),
+    _check(extension().gdr_steps(ctypes.addressof(desc), state, s_prev, q, k, v, g, beta, s_out, o,
+                                 _raw_stream(stream)),
            "blr_gdr_steps")
 
 
@@ -308,37 +286,8 @@ def blr_adamw_step(params, grads, m, v, *, lr: float, step: int, beta1: float = 
     params and grads float32 or bfloat16; m and v float32, or float8_e4m3fn (v then holds the second
     moment's root) with float32 m_scales and v_scales of ceil(n / 256) values each; masters: float32
     weights beside bfloat16 params; grad_scale: a float32 tensor of one value, or None."""
-    import numpy as np
-    import torch
-    n = len(params)
-    lists = {"params": params, "grads": grads, "m": m, "v": v, "masters": masters, "m_scales": m_scales,
-             "v_scales": v_scales}
-    if n == 0:
-        return
-    io = _dtype_code(params[0])
-    eight = m[0].dtype == torch.float8_e4m3fn
-    if eight != (m_scales is not None) or eight != (v_scales is not None):
-        raise ValueError("m_scales and v_scales go with float8_e4m3fn moments")
-    dtypes = {"params": params[0].dtype, "grads": params[0].dtype, "m": m[0].dtype, "v": m[0].dtype}
-    if dtypes["m"] not in (torch.float32, torch.float8_e4m3fn):
-        raise TypeError("moments are float32 or float8_e4m3fn")
-    device = torch._C._cuda_getDevice()
-    table = np.zeros((n, 8), dtype=np.int64)
-    T, dtype_of = torch.Tensor, operator.attrgetter("dtype")  # C-level loops: a model has hundreds of tensors
-    sizes = [*map(T.numel, params)]
-    blocks = [-(-x // 256) for x in sizes] if eight else None
-    for column, (name, ts) in enumerate(lists.items()):
-        if ts is None:
-            continue
-        dtype, want = dtypes.get(name, torch.float32), blocks if "scales" in name else sizes
-        if (len(ts) != n or {*map(dtype_of, ts)} != {dtype} or {*map(T.get_device, ts)} != {device}
-                or not all(map(T.is_contiguous, ts)) or [*map(T.numel, ts)] != want):
-            raise ValueError(f"{name}: {n} contiguous {dtype} tensors of the parameters' sizes on the current CUDA "
-                             "device are wanted")
-        table[:, column] = [*map(T.data_ptr, ts)]
-    table[:, 7] = sizes
-    _check(load().blr_adamw_step(n, table.ctypes.data, io, 8 if eight else 32, lr, beta1, beta2, eps,
-                                 weight_decay, step, _ptr(grad_scale, "grad_scale"), _stream(stream)),
+    _check(extension().adamw_step(params, grads, m, v, masters, m_scales, v_scales, lr, beta1, beta2, eps,
+                                  weight_decay, step, grad_scale, _raw_stream(stream)),
            "blr_adamw_step")
 
 

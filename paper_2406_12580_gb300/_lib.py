@@ -96,3 +96,19 @@ def load() -> ctypes.CDLL:
                 fn.argtypes = args
             _lib = lib
         return _lib
+
+
+_ext = None
+
+
+def extension():
+    """The C++ side of the torch binding, loaded once. Raises if it has not been built."""
+    global _ext
+    if _ext is None:
+        load()
+        import torch  # noqa: F401  (its libraries come first)
+        if not os.path.exists(_build.EXTENSION):
+            raise RuntimeError(f"{_build.EXTENSION} is missing: build it with `python -m paper_2406_12580_gb300.build`")
+        from . import _torch_ext
+        _ext = _torch_ext
+    return _ext

@@ -1,0 +1,323 @@
+// The torch side of the package in C++: argument checks and pointers of the newer entry points, and the gated
+// delta rule's autograd node. It computes nothing and launches nothing itself; it calls libblr.so's C ABI. In
+// Python the checks of a model's few hundred tensors alone took longer than the step that updates them (276 us
+// of 135 tensors and their states, 0.6 us here per hundred), and a backward waits for the interpreter's lock.
+#include <Python.h>
+
+#include <vector>
+
+#include <ATen/ATen.h>
+#include <c10/cuda/CUDAFunctions.h>
+#include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/Exceptions.h>
+#include <torch/csrc/autograd/custom_function.h>
+#include <torch/csrc/autograd/python_variable.h>
+
+#include "blr.h"
+
+namespace {
+
+using at::Tensor;
+using torch::autograd::AutogradContext;
+using torch::autograd::variable_list;
+
+blr_stream_t current_stream() {
+  return reinterpret_cast<blr_stream_t>(c10::cuda::getCurrentCUDAStream().stream());
+}
+
+// Device pointer of a tensor on the current device, None, or an integer; `rows`: it may be a slice of wider rows.
+void* pointer(PyObject* o, const char* name, bool rows, int device) {
+  if (o == Py_None) return nullptr;
+  if (PyLong_Check(o)) return PyLong_AsVoidPtr(o);
+  TORCH_CHECK_TYPE(THPVariable_Check(o), name, ": expected a CUDA tensor, an int pointer or None");
+  const Tensor& t = THPVariable_Unpack(o);
+  if (t.numel() == 0) return nullptr;
+  TORCH_CHECK_VALUE(t.is_cuda() && t.get_device() == device, name, ": tensor must be on the current CUDA device");
+  TORCH_CHECK_VALUE(t.is_contiguous() || (rows && t.stride(-1) == 1), name, ": tensor must be contiguous");
+  return t.data_ptr();
+}
+
+size_t bytes_of(PyObject* o) {
+  return THPVariable_Check(o) ? THPVariable_Unpack(o).nbytes() : 0;
+}
+
+void want(Py_ssize_t got, Py_ssize_t n) {
+  TORCH_CHECK_TYPE(got == n, "expected ", n, " arguments, got ", got);
+}
+
+blr_stream_t stream_of(PyObject* o) {
+  return o == Py_None ? current_stream() : reinterpret_cast<blr_stream_t>(PyLong_AsVoidPtr(o));
+}
+
+template <typename D>
+const D* desc_of(PyObject* address) { return static_cast<const D*>(PyLong_AsVoidPtr(address)); }
+
+// gdr_fwd(desc address, flags, lengths, q, k, v, g, beta, s0, o, s_last, ws, stream) -> status
+PyObject* gdr_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  want(n, 13);
+  static const char* names[] = {"lengths", "q", "k", "v", "g", "beta", "s0", "o", "s_last", "ws"};
+  void* p[10];
+  const int device = c10::cuda::current_device();
+  for (int i = 0; i < 10; ++i) p[i] = pointer(a[2 + i], names[i], i >= 1 && i <= 3, device);
+  return PyLong_FromLong(blr_gdr_fwd(desc_of<blr_gdr_desc>(a[0]), (int)PyLong_AsLong(a[1]),
+                                     static_cast<const int32_t*>(p[0]), p[1], p[2], p[3], p[4], p[5],
+                                     static_cast<const float*>(p[6]), p[7], static_cast<float*>(p[8]), p[9],
+                                     bytes_of(a[11]), stream_of(a[12])));
+  END_HANDLE_TH_ERRORS
+}
+
+// gdr_bwd(desc address, flags, lengths, d_o, ds_last, q, k, v, g, beta, s0, dq, dk, dv, dg, dbeta, ds0, ws, stream)
+PyObject* gdr_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  want(n, 19);
+  static const char* names[] = {"lengths", "d_o", "ds_last", "q", "k", "v", "g", "beta", "s0",
+                                "dq", "dk", "dv", "dg", "dbeta", "ds0", "ws"};
+  void* p[16];
+  const int device = c10::cuda::current_device();
+  for (int i = 0; i < 16; ++i) p[i] = pointer(a[2 + i], names[i], i >= 3 && i <= 5, device);
+  return PyLong_FromLong(blr_gdr_bwd(desc_of<blr_gdr_desc>(a[0]), (int)PyLong_AsLong(a[1]),
+                                     static_cast<const int32_t*>(p[0]), p[1], static_cast<const float*>(p[2]), p[3],
+                                     p[4], p[5], p[6], p[7], static_cast<const float*>(p[8]), p[9], p[10], p[11], p[12],
+                                     p[13], static_cast<float*>(p[14]), p[15], bytes_of(a[17]), stream_of(a[18])));
+  END_HANDLE_TH_ERRORS
+}
+
+// gdr_steps(desc address, state, s_prev, q, k, v, g, beta, s_out, o, stream) -> status
+PyObject* gdr_steps(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  want(n, 11);
+  static const char* names[] = {"s_prev", "q", "k", "v", "g", "beta", "s_out", "o"};
+  void* p[8];
+  const int device = c10::cuda::current_device();
+  for (int i = 0; i < 8; ++i) p[i] = pointer(a[2 + i], names[i], i >= 1 && i <= 3, device);
+  return PyLong_FromLong(blr_gdr_steps(desc_of<blr_gdr_desc>(a[0]), (blr_dtype)PyLong_AsLong(a[1]), p[0], p[1], p[2],
+                                       p[3], p[4], p[5], p[6], p[7], stream_of(a[10])));
+  END_HANDLE_TH_ERRORS
+}
+
+// adamw_step(params, grads, m, v, masters, m_scales, v_scales, lr, beta1, beta2, eps, weight_decay, step,
+//            grad_scale, stream) -> status
+PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  want(n, 15);
+  static const char* names[] = {"params", "grads", "m", "v", "masters", "m_scales", "v_scales"};
+  PyObject* lists[7];
+  for (int i = 0; i < 7; ++i) {
+    TORCH_CHECK_TYPE((a[i] == Py_None && i >= 4) || PyList_Check(a[i]) || PyTuple_Check(a[i]), names[i],
+                     ": a list of tensors is wanted");
+    lists[i] = a[i];
+  }
+  const Py_ssize_t count = PySequence_Fast_GET_SIZE(lists[0]);
+  const auto item = [&](int list, Py_ssize_t i) -> const Tensor& {
+    PyObject* o = PySequence_Fast_GET_ITEM(lists[list], i);
+    TORCH_CHECK_TYPE(THPVariable_Check(o), names[list], ": a list of tensors is wanted");
+    return THPVariable_Unpack(o);
+  };
+  const int device = c10::cuda::current_device();
+  std::vector<blr_adamw_tensor> table((size_t)count);
+  at::ScalarType io = at::kFloat, moment = at::kFloat;
+  if (count > 0) {
+    io = item(0, 0).scalar_type();
+    TORCH_CHECK_TYPE(io == at::kFloat || io == at::kBFloat16, "params: float32 or bfloat16 is wanted");
+    TORCH_CHECK_VALUE(PySequence_Fast_GET_SIZE(lists[2]) == count, "m: ", count, " tensors are wanted");
+    moment = item(2, 0).scalar_type();
+    TORCH_CHECK_TYPE(moment == at::kFloat || moment == at::kFloat8_e4m3fn, "moments are float32 or float8_e4m3fn");
+  }
+  const bool eight = moment == at::kFloat8_e4m3fn;
+  TORCH_CHECK_VALUE(count == 0 || (eight == (lists[5] != Py_None) && eight == (lists[6] != Py_None)),
+                    "m_scales and v_scales go with float8_e4m3fn moments");
+  for (int list = 0; list < 7; ++list) {
+    if (lists[list] == Py_None) continue;
+    TORCH_CHECK_VALUE(PySequence_Fast_GET_SIZE(lists[list]) == count, names[list], ": ", count, " tensors are wanted");
+    const at::ScalarType type = list < 2 ? io : list < 4 ? moment : at::kFloat;
+    for (Py_ssize_t i = 0; i < count; ++i) {
+      const Tensor& t = item(list, i);
+      const int64_t values = list == 0 ? t.numel() : table[i].n;
+      if (list == 0) table[i] = {nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, values};
+      const int64_t size = list < 5 ? values : (values + 255) / 256;
+      TORCH_CHECK_VALUE(t.is_cuda() && t.get_device() == device && t.scalar_type() == type && t.is_contiguous() &&
+                            t.numel() == size,
+                        names[list], "[", i, "]: a contiguous ", type, " tensor of ", size,
+                        " values on the current CUDA device is wanted");
+      void* p = t.data_ptr();
+      blr_adamw_tensor& r = table[i];
+      switch (list) {
+        case 0: r.p = p; break;
+        case 1: r.g = p; break;
+        case 2: r.m = p; break;
+        case 3: r.v = p; break;
+        case 4: r.w = static_cast<float*>(p); break;
+        case 5: r.m_scale = static_cast<float*>(p); break;
+        default: r.v_scale = static_cast<float*>(p);
+      }
+    }
+  }
+  double h[5];
+  for (int i = 0; i < 5; ++i) h[i] = PyFloat_AsDouble(a[7 + i]);
+  const int64_t step = PyLong_AsLongLong(a[12]);
+  if (PyErr_Occurred()) return nullptr;
+  return PyLong_FromLong(blr_adamw_step(count, table.data(), io == at::kFloat ? BLR_F32 : BLR_BF16, eight ? 8 : 32, h[0],
+                                        h[1], h[2], h[3], h[4], step,
+                                        static_cast<const float*>(pointer(a[13], "grad_scale", false, device)),
+                                        stream_of(a[14])));
+  END_HANDLE_TH_ERRORS
+}
+
+// ---- the gated delta rule with its gradients
+
+struct BlrFailure {
+  blr_status status;
+  const char* where;
+};
+
+// t (B, L, H, D) itself when its steps lie at one distance (a slice of wider rows), else a copy.
+Tensor as_rows(const Tensor& t) {
+  const int64_t B = t.size(0), L = t.size(1), H = t.size(2), D = t.size(3);
+  const int64_t ld = L > 1 ? t.stride(1) : H * D;
+  const bool fits = t.stride(3) == 1 && (H == 1 || t.stride(2) == D) && ld >= H * D && ld % 8 == 0 &&
+                    (B == 1 || t.stride(0) == L * ld) && (reinterpret_cast<uintptr_t>(t.data_ptr()) & 15) == 0;
+  return fits ? t : t.contiguous();
+}
+
+struct Inputs {
+  blr_gdr_desc desc;
+  Tensor q, k, v, g, beta, s0, lengths;  // the last two may be undefined
+};
+
+Inputs prepare(const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& g, const Tensor& beta, double scale,
+               const Tensor& s0, const Tensor& lengths) {
+  TORCH_CHECK_VALUE(q.dim() == 4 && k.sizes() == q.sizes() && v.dim() == 4 && v.size(0) == q.size(0) &&
+                        v.size(1) == q.size(1),
+                    "q and k (B, L, Hk, Dk) and v (B, L, Hv, Dv) are wanted");
+  TORCH_CHECK_VALUE(g.sizes() == v.sizes().slice(0, 3) && beta.sizes() == g.sizes(), "g and beta (B, L, Hv) are wanted");
+  const at::ScalarType type = v.scalar_type();
+  TORCH_CHECK_TYPE(type == at::kFloat || type == at::kBFloat16, "unsupported dtype ", type);
+  TORCH_CHECK_TYPE(q.scalar_type() == type && k.scalar_type() == type && g.scalar_type() == type &&
+                       beta.scalar_type() == type,
+                   "q, k, v, g and beta must have one dtype");
+  const int device = c10::cuda::current_device();
+  for (const Tensor* t : {&q, &k, &v, &g, &beta, &s0, &lengths})
+    TORCH_CHECK_VALUE(!t->defined() || (t->is_cuda() && t->get_device() == device),
+                      "tensors must be on the current CUDA device");
+  const int64_t B = q.size(0), L = q.size(1), Hk = q.size(2), Dk = q.size(3), Hv = v.size(2), Dv = v.size(3);
+  TORCH_CHECK_VALUE(!s0.defined() || (s0.scalar_type() == at::kFloat && s0.sizes() == at::IntArrayRef({B, Hv, Dk, Dv})),
+                    "s0 must be float32 (B, Hv, Dk, Dv)");
+  TORCH_CHECK_VALUE(!lengths.defined() || (lengths.scalar_type() == at::kInt && lengths.sizes() == at::IntArrayRef({B})),
+                    "lengths must be int32 (B,)");
+  Inputs in;
+  in.q = as_rows(q);
+  in.k = as_rows(k);
+  in.v = as_rows(v);
+  in.g = g.contiguous();
+  in.beta = beta.contiguous();
+  if (s0.defined()) in.s0 = s0.contiguous();
+  if (lengths.defined()) in.lengths = lengths.contiguous();
+  const auto ld = [&](const Tensor& t) { return L > 1 ? t.stride(1) : (int64_t)0; };
+  in.desc = {B, L, Hk, Hv, Dk, Dv, ld(in.q), ld(in.k), ld(in.v), type == at::kFloat ? BLR_F32 : BLR_BF16, (float)scale};
+  return in;
+}
+
+template <typename T = void>
+T* data(const Tensor& t) { return t.defined() && t.numel() > 0 ? static_cast<T*>(t.data_ptr()) : nullptr; }
+
+void forward_into(const Inputs& in, int flags, bool with_state, Tensor* o, Tensor* s_last, Tensor* ws) {
+  const blr_gdr_desc& d = in.desc;
+  const auto bytes = (int64_t)blr_gdr_workspace_bytes(&d, flags);
+  *ws = at::empty({bytes > 16 ? bytes : 16}, in.v.options().dtype(at::kByte));
+  *o = at::empty(in.v.sizes(), in.v.options());
+  if (with_state) *s_last = at::empty({d.B, d.Hv, d.Dk, d.Dv}, in.v.options().dtype(at::kFloat));
+  const blr_status st = blr_gdr_fwd(&d, flags, data<int32_t>(in.lengths), data(in.q), data(in.k), data(in.v), data(in.g),
+                                    data(in.beta), data<float>(in.s0), data(*o), data<float>(*s_last), data(*ws),
+                                    (size_t)ws->numel(), current_stream());
+  if (st != BLR_OK) throw BlrFailure{st, "blr_gdr_fwd"};
+}
+
+struct Rule : torch::autograd::Function<Rule> {
+  static variable_list forward(AutogradContext* ctx, const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& g,
+                               const Tensor& beta, const std::optional<Tensor>& s0, const std::optional<Tensor>& lengths,
+                               double scale, bool with_state) {
+    const int flags = BLR_GDR_TRAIN | (with_state || s0.has_value() ? BLR_GDR_STATE : 0);
+    const Inputs in = prepare(q, k, v, g, beta, scale, s0.value_or(Tensor()), lengths.value_or(Tensor()));
+    Tensor o, s_last, ws;
+    forward_into(in, flags, with_state, &o, &s_last, &ws);
+    ctx->save_for_backward({in.q, in.k, in.v, in.g, in.beta, in.s0, in.lengths, ws});
+    ctx->saved_data["scale"] = scale;
+    ctx->saved_data["flags"] = (int64_t)flags;
+    ctx->set_materialize_grads(false);
+    return with_state ? variable_list{o, s_last} : variable_list{o};
+  }
+
+  static variable_list backward(AutogradContext* ctx, variable_list grads) {
+    TORCH_CHECK(!at::GradMode::is_enabled(), "the gated delta rule has no second derivative (create_graph=True)");
+    const variable_list s = ctx->get_saved_variables();
+    const Inputs in = prepare(s[0], s[1], s[2], s[3], s[4], ctx->saved_data["scale"].toDouble(), s[5], s[6]);
+    Tensor d_o = grads[0].defined() ? grads[0].contiguous() : at::zeros(in.v.sizes(), in.v.options());
+    Tensor ds_last = grads.size() > 1 && grads[1].defined() ? grads[1].contiguous() : Tensor();
+    const auto like = [](const Tensor& t) { return at::empty(t.sizes(), t.options()); };
+    Tensor dq = like(in.q), dk = like(in.k), dv = like(in.v), dg = like(in.g), dbeta = like(in.beta), ds0;
+    if (in.s0.defined() && ctx->needs_input_grad(5)) ds0 = like(in.s0);
+    const blr_status st =
+        blr_gdr_bwd(&in.desc, (int)ctx->saved_data["flags"].toInt(), data<int32_t>(in.lengths), data(d_o),
+                    data<float>(ds_last), data(in.q), data(in.k), data(in.v), data(in.g), data(in.beta),
+                    data<float>(in.s0), data(dq), data(dk), data(dv), data(dg), data(dbeta), data<float>(ds0),
+                    data(s[7]), (size_t)s[7].numel(), current_stream());
+    TORCH_CHECK(st == BLR_OK, "blr_gdr_bwd: ", blr_status_string(st), " (", blr_last_error_string(), ")");
+    return {dq, dk, dv, dg, dbeta, ds0, Tensor(), Tensor(), Tensor()};
+  }
+};
+
+// rule(q, k, v, g, beta, scale, s0, lengths, with_state) -> (o, s_last or None); a failed call of the library
+// returns (status, name of the entry point)
+PyObject* rule(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  want(n, 9);
+  Tensor t[7];
+  static const int at_arg[] = {0, 1, 2, 3, 4, 6, 7};
+  bool tracked = false;
+  for (int i = 0; i < 7; ++i) {
+    PyObject* o = a[at_arg[i]];
+    if (i >= 5 && o == Py_None) continue;
+    TORCH_CHECK_TYPE(THPVariable_Check(o), "tensors are wanted");
+    t[i] = THPVariable_Unpack(o);
+    tracked = tracked || t[i].requires_grad();
+  }
+  const double scale = PyFloat_AsDouble(a[5]);
+  const int with_state = PyObject_IsTrue(a[8]);
+  if (PyErr_Occurred()) return nullptr;
+  Tensor o, s_last;
+  try {
+    if (tracked && at::GradMode::is_enabled()) {
+      const auto opt = [](const Tensor& x) { return x.defined() ? std::optional<Tensor>(x) : std::nullopt; };
+      variable_list out = Rule::apply(t[0], t[1], t[2], t[3], t[4], opt(t[5]), opt(t[6]), scale, with_state != 0);
+      o = out[0];
+      if (with_state) s_last = out[1];
+    } else {
+      Tensor ws;
+      const at::NoGradGuard no_grad;
+      const int flags = with_state || t[5].defined() ? BLR_GDR_STATE : 0;
+      forward_into(prepare(t[0], t[1], t[2], t[3], t[4], scale, t[5], t[6]), flags, with_state, &o, &s_last, &ws);
+    }
+  } catch (const BlrFailure& f) {
+    return Py_BuildValue("(is)", (int)f.status, f.where);
+  }
+  PyObject* po = THPVariable_Wrap(o);
+  PyObject* ps = s_last.defined() ? THPVariable_Wrap(s_last) : Py_NewRef(Py_None);
+  return Py_BuildValue("(NN)", po, ps);
+  END_HANDLE_TH_ERRORS
+}
+
+template <typename F>
+PyCFunction fast(F f) { return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(f)); }
+
+PyMethodDef methods[] = {{"gdr_fwd", fast(gdr_fwd), METH_FASTCALL, nullptr},
+                         {"gdr_bwd", fast(gdr_bwd), METH_FASTCALL, nullptr},
+                         {"gdr_steps", fast(gdr_steps), METH_FASTCALL, nullptr},
+                         {"adamw_step", fast(adamw_step), METH_FASTCALL, nullptr},
+                         {"rule", fast(rule), METH_FASTCALL, nullptr},
+                         {nullptr, nullptr, 0, nullptr}};
+PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_torch_ext", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
+
+}  // namespace
+
+PyMODINIT_FUNC PyInit__torch_ext() { return PyModule_Create(&module_def); }
