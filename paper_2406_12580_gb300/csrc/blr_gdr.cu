@@ -98,6 +98,7 @@ Problem make_problem(const blr_gdr_desc* d, const GdrSizes& s, const Layout& l, 
   p.dS = w + l.dS;
   p.nseg = (int)l.nseg;
   p.seg_chunks = (int)l.seg_chunks;
+  p.single = l.n == 1 && l.np == 1 && s.Dv <= 128;  // one plane: neither s0 nor a state's gradient is given
   p.phi = w + l.phi;
   p.carry = reinterpret_cast<float*>(w + l.carry);
   p.back_carry = reinterpret_cast<float*>(w + l.back_carry);

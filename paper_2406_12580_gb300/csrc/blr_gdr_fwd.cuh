@@ -620,8 +620,8 @@ output_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restr
   uint64_t* bars = reinterpret_cast<uint64_t*>(G + kGates);
   const int dvb = P.Dv / 64;
   const auto load = [&](int part) {
-    mbar_arrive_expect_tx(&bars[1], L::kU + L::kS);
-    bulk_load(ts.base, P.S + (w.nc * dvb + part) * L::kS, L::kS, &bars[1]);
+    mbar_arrive_expect_tx(&bars[1], L::kU + (P.single ? 0 : L::kS));
+    if (!P.single) bulk_load(ts.base, P.S + (w.nc * dvb + part) * L::kS, L::kS, &bars[1]);
     bulk_load(tu.base, P.U + (w.nc * dvb + part) * L::kU, L::kU, &bars[1]);
   };
   if (tid == 0) {
@@ -671,6 +671,7 @@ output_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restr
     }
     mbar_wait(&bars[1], part & 1, P.err);
     float acc[8][4] = {};
+    if (!P.single) {
 #pragma unroll
     for (int kk = 0; kk < DK / 16; ++kk) {
       uint32_t a[kPl<NI>][4];
@@ -682,6 +683,7 @@ output_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restr
         mma_p<NI, NM>(acc[2 * nn], a, b[0]);
         mma_p<NI, NM>(acc[2 * nn + 1], a, b[1]);
       }
+    }
     }
 #pragma unroll
     for (int nb = 0; nb < 8; ++nb) {

@@ -229,13 +229,14 @@ grad_tc_kernel(const Problem P, const __grid_constant__ Maps M, const __grid_con
       const auto load_b = [&](uint32_t item) {
         if (item >= total) return;
         const Where w = where(item);
-        mbar_arrive_expect_tx(lb, DVB * (2 * L::kT8 + 2 * L::kS));
+        mbar_arrive_expect_tx(lb, DVB * (2 * L::kT8 + (P.single ? 0 : 2 * L::kS)));
 #pragma unroll
         for (int p = 0; p < DVB; ++p) {
           const uint32_t at = base + L::kPart0 + p * L::kPart;
           const int64_t tile = w.nc * DVB + p;
           load_rows<1>(Tile<8, 1, true>{at}, &M.d_o, lb, none, 0, w.h * P.Dv + 64 * p, w.t, w.b, P.L, 0, 0);
           bulk_load(at + 2 * L::kT8, P.U + tile * L::kT8, L::kT8, lb);
+          if (P.single) continue;
           bulk_load(at + 3 * L::kT8, P.S + tile * L::kS, L::kS, lb);
           bulk_load(at + 3 * L::kT8 + L::kS, P.dS + tile * L::kS, L::kS, lb);
         }
@@ -269,7 +270,7 @@ grad_tc_kernel(const Problem P, const __grid_constant__ Maps M, const __grid_con
         tc::commit(m1);
         mbar_wait(lb, ph, P.err);
 #pragma unroll
-        for (int p = 0; p < DVB; ++p) {  // rows 64..: U dS'^T
+        for (int p = 0; p < (P.single ? 0 : DVB); ++p) {  // rows 64..: U dS'^T
           const uint32_t at = base + L::kPart0 + p * L::kPart;
           tc::mma_k<4>(tm + L::kX2, tc::desc(at + L::kT8, 128, 1024, false), 256,
                        tc::desc(at + 3 * L::kT8 + L::kS, DK * 16, 128, false), 2 * DK * 16,
@@ -288,8 +289,9 @@ grad_tc_kernel(const Problem P, const __grid_constant__ Maps M, const __grid_con
           const uint64_t od = tc::desc(at, 16, 1024, true);  // [dO; dR]
           tc::mma_k<4>(tm + L::kDPA, od, 32, tc::desc(at + 2 * L::kT8, 128, 1024, false), 256,
                        tc::instr(64, false, false), p > 0);
-          tc::mma_k<4>(tm + L::kX13, od, 32, tc::desc(at + 3 * L::kT8, DK * 16, 128, false), 2 * DK * 16,
-                       tc::instr(DK, false, true), p > 0);
+          if (!P.single)
+            tc::mma_k<4>(tm + L::kX13, od, 32, tc::desc(at + 3 * L::kT8, DK * 16, 128, false), 2 * DK * 16,
+                         tc::instr(DK, false, true), p > 0);
         }
         tc::commit(m2);
 #pragma unroll
@@ -400,8 +402,7 @@ grad_tc_kernel(const Problem P, const __grid_constant__ Maps M, const __grid_con
         mbar_wait(lb, ph, P.err);
         float s = 0.0f;
         const int t = 64 * hf + 32 * (quad & 1) + l;
-#pragma unroll
-        for (int p = 0; p < DVB; ++p) {
+        for (int p = 0; p < (P.single ? 0 : DVB); ++p) {
           const uint32_t at = base + L::kPart0 + p * L::kPart + 3 * L::kT8;
 #pragma unroll 4
           for (int i = 16 * t; i < L::kS; i += 128 * 16) s += dot16<1, 0>(at + i, at + L::kS + i);
@@ -462,6 +463,11 @@ grad_tc_kernel(const Problem P, const __grid_constant__ Maps M, const __grid_con
           const int col = hf * (DK / 2) + 32 * c;  // of Dk
           const uint32_t tile = base + (2 * (col >> 6) + side) * L::kT8;  // Q's rows, or K's
           float x[32];
+          if (P.single) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) acc[c][i] = 0.0f;
+            continue;
+          }
           tc::load32(lane + L::kX13 + col, x);
           y1 += tc::dot32(tile, row, (col & 63) >> 3, x);
 #pragma unroll

@@ -38,7 +38,8 @@ blr_status fwd_dk(const Problem& p, const FwdCall& c) {
     BLR_TRY(start("combine", combine_kernel<DK, NM, false>, heads * (p.Dv / 64), 128, CombineSmem<DK, NM>::kBytes,
                   c.stream, p, p.carry, c.s0));
   }
-  if (wide_chains(p))
+  if (p.single) {
+  } else if (wide_chains(p))
     BLR_TRY(start("chain", chain_kernel<TI, DK, NI, NM, 4, false>, heads * p.nseg * (p.Dv / 64),
                   32 * (4 + kLoadWarps<NI>), wide, c.stream, p, c.maps, k, c.s0, c.s_last));
   else
@@ -86,7 +87,8 @@ blr_status bwd_dk(const Problem& p, const BwdCall& c) {
     BLR_TRY(start("combine", combine_kernel<DK, NM, true>, heads * (p.Dv / 64), 128, CombineSmem<DK, NM>::kBytes,
                   c.stream, p, p.back_carry, c.ds_last));
   }
-  if (wide_chains(p))
+  if (p.single) {
+  } else if (wide_chains(p))
     BLR_TRY(start("back", back_kernel<TI, DK, NI, NM, kWide, false>, heads * p.nseg * (p.Dv / (16 * kWide)),
                   32 * (kWide + kLoadWarps<NI>), wide, c.stream, p, c.maps, q, k, d_o, c.ds_last, c.ds0));
   else

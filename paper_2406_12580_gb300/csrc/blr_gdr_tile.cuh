@@ -391,6 +391,9 @@ struct Problem {
   // state before it affinely, S -> phi S + N: `phi` holds phi^T of every segment as Dk / 64 tiles, `carry`
   // N^T and later the state before the segment, `back_carry` the same of the states' gradients (Dv x Dk each).
   int nseg, seg_chunks;
+  // Rows of one chunk without carried states: every state and state's gradient is zero, the chain kernels
+  // do not run and S, dS are not there to be read (bfloat16 operands, Dv 64 or 128).
+  int single;
   char* phi;
   float *carry, *back_carry;
   float *pq, *pk;  // per value head gradients of q and k, when heads are shared

@@ -32,6 +32,9 @@ SHAPES = [  # B, L, Hk, Hv, Dk, Dv, lengths
     (1, 70, 1, 3, 128, 256, None),
     (5, 131, 1, 2, 64, 64, [0, 131, 1, 64, 77]),
     (3, 257, 2, 2, 128, 128, [300, -5, 65]),
+    # one chunk a row: no states without BLR_GDR_STATE
+    (7, 50, 2, 2, 64, 64, [50, 0, 1, 49, 17, 33, 50]),
+    (3, 64, 1, 2, 128, 128, [64, 20, 0]),
     # few heads and long rows: cut into segments
     (1, 2700, 1, 1, 64, 64, None),
     (3, 2600, 1, 1, 64, 128, [0, 2600, 130]),
@@ -69,7 +72,11 @@ def test_forward_and_gradients(shape, kind):
     for n, x in got.items():
         if x is None:
             continue
-        bound = EXACT if x.dtype == torch.float32 else ROUNDED if state else COARSE
+        bound = EXACT if x.dtype == torch.float32 else COARSE
+        if state and x.dtype == torch.bfloat16:
+            # a few large values can round worse than the mean: the reference's own rounding, and what the
+            # 2e-5 before it turns into where a value lies that near a boundary, sqrt(2e-5 2^-8)
+            bound = off(want[n].bfloat16(), want[n]) + 3e-4
         assert off(x, want[n]) <= bound, (n, off(x, want[n]))
         if lengths is not None and n not in ("s", "ds0"):
             assert not x.detach()[pad].any(), n
