@@ -86,15 +86,23 @@ gdr_steps_kernel(int64_t K, int Hk, int Hv, int Dv, int64_t ldq, int64_t ldk, in
 #pragma unroll
     for (int i = 0; i < R; ++i) S[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
   }
+  // a step's inputs are loaded while the one before it is computed
+  float kk[R], qq[R], ga, bt;
+  float4 vv;
+  const auto load = [&](int64_t t) {
+    const int64_t at = b * K + t;
+    ga = to_f(g[at * Hv + h]);
+    bt = to_f(beta[at * Hv + h]);
+    vv = load4(v + at * ldv + (int64_t)h * Dv + col);
+#pragma unroll
+    for (int i = 0; i < R; i += 8) {
+      load8(k + at * ldk + hk * DK + rg * R + i, *reinterpret_cast<float(*)[8]>(&kk[i]));
+      load8(q + at * ldq + hk * DK + rg * R + i, *reinterpret_cast<float(*)[8]>(&qq[i]));
+    }
+  };
+  if (K > 0) load(0);
   for (int64_t t = 0; t < K; ++t) {
     const int64_t at = b * K + t;
-    const float a = expf(fmaxf(to_f(g[at * Hv + h]), -120.0f)), bt = to_f(beta[at * Hv + h]);
-    const T* kp = k + at * ldk + hk * DK + rg * R;
-    const T* qp = q + at * ldq + hk * DK + rg * R;
-    const T* vp = v + at * ldv + (int64_t)h * Dv + col;
-    float kk[R];
-#pragma unroll
-    for (int i = 0; i < R; i += 8) load8(kp + i, *reinterpret_cast<float(*)[8]>(&kk[i]));
     float4 r = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
     for (int i = 0; i < R; ++i) {
@@ -104,26 +112,23 @@ gdr_steps_kernel(int64_t K, int Hk, int Hv, int Dv, int64_t ldq, int64_t ldk, in
       r.w = fmaf(kk[i], S[i].w, r.w);
     }
     r = sum_rows(r);
-    const float4 u = make_float4(bt * (to_f(vp[0]) - a * r.x), bt * (to_f(vp[1]) - a * r.y),
-                                 bt * (to_f(vp[2]) - a * r.z), bt * (to_f(vp[3]) - a * r.w));
+    const float a = expf(fmaxf(ga, -120.0f));
+    const float4 u = make_float4(bt * (vv.x - a * r.x), bt * (vv.y - a * r.y), bt * (vv.z - a * r.z),
+                                 bt * (vv.w - a * r.w));
     float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-    for (int i = 0; i < R; i += 8) {
-      float qq[8];
-      load8(qp + i, qq);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        float4& s = S[i + j];
-        s.x = fmaf(kk[i + j], u.x, a * s.x);
-        s.y = fmaf(kk[i + j], u.y, a * s.y);
-        s.z = fmaf(kk[i + j], u.z, a * s.z);
-        s.w = fmaf(kk[i + j], u.w, a * s.w);
-        y.x = fmaf(qq[j], s.x, y.x);
-        y.y = fmaf(qq[j], s.y, y.y);
-        y.z = fmaf(qq[j], s.z, y.z);
-        y.w = fmaf(qq[j], s.w, y.w);
-      }
+    for (int i = 0; i < R; ++i) {
+      float4& s = S[i];
+      s.x = fmaf(kk[i], u.x, a * s.x);
+      s.y = fmaf(kk[i], u.y, a * s.y);
+      s.z = fmaf(kk[i], u.z, a * s.z);
+      s.w = fmaf(kk[i], u.w, a * s.w);
+      y.x = fmaf(qq[i], s.x, y.x);
+      y.y = fmaf(qq[i], s.y, y.y);
+      y.z = fmaf(qq[i], s.z, y.z);
+      y.w = fmaf(qq[i], s.w, y.w);
     }
+    if (t + 1 < K) load(t + 1);
     if (o != nullptr) {
       y = sum_rows(y);
       if (rg == 0) store4(o + at * Hv * Dv + (int64_t)h * Dv + col,
