@@ -99,8 +99,8 @@ du_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restrict_
     char* out = P.dU + (w.nc * dvb + part) * Tile<8, NM>::kBytes;
 #pragma unroll
     for (int nb = 0; nb < 8; ++nb) {
-      store_block<8, NM>(out, 2 * warp, nb, acc[nb][0], acc[nb][1]);
-      store_block<8, NM>(out, 2 * warp + 1, nb, acc[nb][2], acc[nb][3]);
+      store_u<NM>(out, 2 * warp, nb, acc[nb][0], acc[nb][1]);
+      store_u<NM>(out, 2 * warp + 1, nb, acc[nb][2], acc[nb][3]);
     }
   }
 }
@@ -112,8 +112,14 @@ struct BackSmem {
   static constexpr int kW = Tile<DK / 8, NM>::kBytes, kK = Tile<DK / 8, NI>::kBytes, kO = Tile<kO8, NI>::kBytes,
                        kU = Tile<2 * WARPS, NM>::kBytes;
   static constexpr int kStage = 2 * kK + kO + kW + kU + kGateBytes<NI>;
-  static constexpr int kStages = WARPS == 2 && 3 * kStage <= 227 * 1024 ? 3 : 2;
-  static constexpr int kBytes = kStages * kStage + 16 * kStages;
+  // Staged stores take a sixth off a wide block's chunk; in a narrow one, where a chunk waits for its one
+  // warp a scheduler, the staging warp's fence and issue cost more than they save (446 -> 573 us).
+  static constexpr bool kStaged = WARPS == 4 && 2 * kStage + WARPS * ChainOut<DK, NM, true>::kBytes + 48 <= 227 * 1024;
+  using Out = ChainOut<DK, NM, kStaged>;
+  static constexpr int kOut = WARPS * Out::kBytes;
+  static constexpr int kStages = WARPS == 2 && 3 * kStage + kOut + 48 <= 227 * 1024 ? 3 : 2;
+  static constexpr int kBytes = kStages * kStage + kOut + 16 * kStages;
+  static_assert(kBytes <= 227 * 1024 || kStage > 113 * 1024, "shared memory of a block");
 };
 
 // The states' gradients from chunk to chunk, last to first: as chain_kernel, a warp holds dS^T of 16
@@ -133,7 +139,7 @@ back_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restric
   if (P.nseg > 1 && sg.count <= 0 && seg > 0) return;
   if (MAPS && (seg == 0 || sg.chunks == 0)) return;
   const int block = part * WARPS / 4, c8 = 2 * ((part * WARPS) & 3);
-  uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kStages * L::kStage);
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kStages * L::kStage + L::kOut);
   uint64_t* empty = full + L::kStages;
   init_ring(full, empty, L::kStages, NI == 1 ? 1 : 1 + 32 * kLoadWarps<NI>, WARPS);
   if (warp >= WARPS) {  // loads
@@ -150,7 +156,7 @@ back_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restric
       if (tid == 0) {
         mbar_arrive_expect_tx(&full[s], tma_bytes<NI>(kIn) + L::kW + L::kU + 4 * kGateFloats<NM>);
         bulk_load(st + kIn, P.W + nc * L::kW, L::kW, &full[s]);
-        bulk_columns(Tile<2 * WARPS, NM>{st + kIn + L::kW}, P.dU + (nc * dvb + block) * Tile<8, NM>::kBytes, c8,
+        bulk_columns(UTile<2 * WARPS, NM>{st + kIn + L::kW}, P.dU + (nc * dvb + block) * Tile<8, NM>::kBytes, c8,
                      &full[s]);
         bulk_load(st + kIn + L::kW + L::kU, P.gates + nc * kGates, 4 * kGateFloats<NM>, &full[s]);
       }
@@ -188,13 +194,15 @@ back_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restric
     const InTile<DK / 8, NI> tk{st}, tq{st + L::kK};
     const InTile<L::kO8, NI> to{st + 2 * L::kK};
     const Tile<DK / 8, NM> tw{st + 2 * L::kK + L::kO};
-    const Tile<2 * WARPS, NM> tu{st + 2 * L::kK + L::kO + L::kW};
+    const UTile<2 * WARPS, NM> tu{st + 2 * L::kK + L::kO + L::kW};
     const float* G = reinterpret_cast<const float*>(smem + s * L::kStage + 2 * L::kK + L::kO + L::kW + L::kU);
     const int o8 = (NI == 1 ? c8 : 0) + 2 * warp;  // this warp's columns of dO
     const int64_t tile = (w0.nc + c) * dvb + block;
     // K dS': columns are the chunk's steps
     float u[8][4] = {};
-    char* so = P.dS + tile * Tile<DK / 8, NM>::kBytes + (c8 + 2 * warp) * (DK / 8) * 128 + l * 4;
+    const typename L::Out out{smem_addr(smem) + L::kStages * L::kStage + warp * L::Out::kBytes,
+                              P.dS + tile * Tile<DK / 8, NM>::kBytes, P.dU + tile * UTile<8, NM>::kBytes, c8 + 2 * warp};
+    if (!MAPS) out.begin();
     pipelined<DK / 16, 4, NI>(
         [&](int kk, auto& b) {
 #pragma unroll
@@ -203,13 +211,7 @@ back_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restric
         [&](int kk, auto& b) {
           uint32_t a[kPl<NM>][4];
           to_a<NM>(S[2 * kk], S[2 * kk + 1], a);
-          if (!MAPS)
-#pragma unroll
-          for (int p = 0; p < kPl<NM>; ++p)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              *reinterpret_cast<uint32_t*>(so + p * Tile<DK / 8, NM>::kPlane +
-                                           ((e & 1) * (DK / 8) + 2 * kk + (e >> 1)) * 128) = a[p][e];
+          if (!MAPS) out.state(kk, a);
 #pragma unroll
           for (int nn = 0; nn < 4; ++nn) {
             mma_p<NM, NI>(u[2 * nn], a, b[nn][0]);
@@ -253,7 +255,6 @@ back_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restric
           }
         });
     // this chunk's dU^T: the decayed sum and the part computed before; then -W^T dU
-    char* uo = P.dU + tile * Tile<8, NM>::kBytes;
     uint32_t a[kPl<NM>][4];
     pipelined<4 * (DK / 64), 4, NM>(
         [&](int s, auto& b) {
@@ -282,9 +283,9 @@ back_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restric
                 const float2 v = join2<NM>(x);
                 y[2 * e] = fmaf(y[2 * e], down.x, v.x);
                 y[2 * e + 1] = fmaf(y[2 * e + 1], down.y, v.y);
-                if (!MAPS) store_block_t<8, NM>(uo, 2 * kk + h, c8 + 2 * warp + e, y[2 * e], y[2 * e + 1]);
               }
             }
+            if (!MAPS) out.values(kk, u[2 * kk], u[2 * kk + 1]);
             to_a<NM>(u[2 * kk], u[2 * kk + 1], a);
           }
 #pragma unroll
@@ -293,9 +294,11 @@ back_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restric
             mma_p<NM, NM>(S[n0 + 2 * nn + 1], a, b[nn][1]);
           }
         });
+    if (!MAPS) out.end();
     __syncwarp();
     if (l == 0) mbar_arrive(&empty[s]);
   }
+  if (!MAPS && L::Out::kBytes > 0 && l == 0) bulk_wait_all();  // before the block's shared memory goes
   if constexpr (MAPS) {
 #pragma unroll
     for (int nb = 0; nb < DK / 8; ++nb) {
@@ -440,7 +443,7 @@ grad_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restric
     mbar_wait(&bars[part % L::kStages], (part / L::kStages) & 1, P.err);
     const uint32_t st = base + L::kFixed + (part % L::kStages) * L::kStage;
     const InTile<8, NI> tv{st}, to{st + L::kI};
-    const Tile<8, NM> tu{st + 2 * L::kI}, tdu{st + 2 * L::kI + L::kM};
+    const UTile<8, NM> tu{st + 2 * L::kI}, tdu{st + 2 * L::kI + L::kM};
     const Tile<DK / 8, NM> ts{st + 2 * L::kI + 2 * L::kM}, tds{st + 2 * L::kI + 2 * L::kM + L::kS};
     {  // dR, dV
       float r[VB][4] = {};

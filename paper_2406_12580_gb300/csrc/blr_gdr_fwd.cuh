@@ -283,8 +283,8 @@ prepare_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __rest
       char* u = P.U + (w.nc * dvb + first + i) * Tile<8, NM>::kBytes;
 #pragma unroll
       for (int nb = 0; nb < 8; ++nb) {
-        store_block<8, NM>(u, 2 * warp, nb, acc[nb][0], acc[nb][1]);
-        store_block<8, NM>(u, 2 * warp + 1, nb, acc[nb][2], acc[nb][3]);
+        store_u<NM>(u, 2 * warp, nb, acc[nb][0], acc[nb][1]);
+        store_u<NM>(u, 2 * warp + 1, nb, acc[nb][2], acc[nb][3]);
       }
     }
   }
@@ -317,8 +317,14 @@ template <int DK, int NI, int NM, int WARPS>
 struct ChainSmem {
   static constexpr int kW = Tile<DK / 8, NM>::kBytes, kK = Tile<DK / 8, NI>::kBytes, kU = Tile<2 * WARPS, NM>::kBytes;
   static constexpr int kStage = kK + kW + kU + kGateBytes<NI>;
-  static constexpr int kStages = WARPS == 2 && 3 * kStage <= 227 * 1024 ? 3 : 2;
-  static constexpr int kBytes = kStages * kStage + 16 * kStages;
+  // Staged stores take a sixth off a wide block's chunk; in a narrow one, where a chunk waits for its one
+  // warp a scheduler, the staging warp's fence and issue cost more than they save (446 -> 573 us).
+  static constexpr bool kStaged = WARPS == 4 && 2 * kStage + WARPS * ChainOut<DK, NM, true>::kBytes + 48 <= 227 * 1024;
+  using Out = ChainOut<DK, NM, kStaged>;
+  static constexpr int kOut = WARPS * Out::kBytes;
+  static constexpr int kStages = WARPS == 2 && 3 * kStage + kOut + 48 <= 227 * 1024 ? 3 : 2;
+  static constexpr int kBytes = kStages * kStage + kOut + 16 * kStages;
+  static_assert(kBytes <= 227 * 1024 || kStage > 113 * 1024, "shared memory of a block");
 };
 
 // The states from chunk to chunk. A block takes 16 WARPS columns of a head's state, a warp 16 of them, as
@@ -346,7 +352,7 @@ chain_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restri
   if (P.nseg > 1 && sg.count <= 0 && seg > 0) return;
   if (MAPS && seg == sg.last && (!ident || P.T == nullptr)) return;  // only the backward takes its phi
   const int block = part * WARPS / 4, c8 = 2 * ((part * WARPS) & 3);  // this part's 64 columns, and where in them
-  uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kStages * L::kStage);
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kStages * L::kStage + L::kOut);
   uint64_t* empty = full + L::kStages;
   init_ring(full, empty, L::kStages, NI == 1 ? 1 : 1 + 32 * kLoadWarps<NI>, WARPS);
   if (warp >= WARPS) {  // loads
@@ -361,7 +367,7 @@ chain_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restri
         mbar_arrive_expect_tx(&full[s], tma_bytes<NI>(L::kK) + L::kW + (ident ? 0 : L::kU) + 4 * kGateFloats<NM>);
         bulk_load(st + L::kK, P.W + nc * L::kW, L::kW, &full[s]);
         if (!ident)
-          bulk_columns(Tile<2 * WARPS, NM>{st + L::kK + L::kW}, P.U + (nc * dvb + block) * Tile<8, NM>::kBytes, c8,
+          bulk_columns(UTile<2 * WARPS, NM>{st + L::kK + L::kW}, P.U + (nc * dvb + block) * Tile<8, NM>::kBytes, c8,
                        &full[s]);
         bulk_load(st + L::kK + L::kW + L::kU, P.gates + nc * kGates, 4 * kGateFloats<NM>, &full[s]);
       }
@@ -393,36 +399,14 @@ chain_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restri
     const uint32_t st = smem_addr(smem) + s * L::kStage;
     const InTile<DK / 8, NI> tk{st};
     const Tile<DK / 8, NM> tw{st + L::kK};
-    const Tile<2 * WARPS, NM> tu{st + L::kK + L::kW};
+    const UTile<2 * WARPS, NM> tu{st + L::kK + L::kW};
     const float* G = reinterpret_cast<const float*>(smem + s * L::kStage + L::kK + L::kW + L::kU);
     const int64_t tile = (w0.nc + c) * dvb + block;
-    float u[8][4];
-#pragma unroll
-    for (int nb = 0; nb < 8; ++nb)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) u[nb][e] = 0.0f;
-    if (!ident)
-#pragma unroll
-    for (int nb = 0; nb < 8; nb += 2) {  // U0^T: blocks (tokens 8 nb, columns 16 warp), transposed
-      uint32_t f[2][kPl<NM>][2];
-      const int i = l >> 3;
-#pragma unroll
-      for (int p = 0; p < kPl<NM>; ++p)
-        ldsm_t(tu.at(p, nb + (i >> 1), 2 * warp + (i & 1), l & 7), f[0][p][0], f[0][p][1], f[1][p][0], f[1][p][1]);
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          uint32_t x[kPl<NM>];
-#pragma unroll
-          for (int p = 0; p < kPl<NM>; ++p) x[p] = f[h][p][e];
-          const float2 v = join2<NM>(x);
-          u[nb + h][2 * e] = v.x;
-          u[nb + h][2 * e + 1] = v.y;
-        }
-    }
+    float u[8][4] = {};
     // the state before the chunk goes out as it becomes an operand: blocks (columns 16 warp.., rows 16 kk..)
-    char* so = P.S + tile * Tile<DK / 8, NM>::kBytes + (c8 + 2 * warp) * (DK / 8) * 128 + l * 4;
+    const typename L::Out out{smem_addr(smem) + L::kStages * L::kStage + warp * L::Out::kBytes,
+                              P.S + tile * Tile<DK / 8, NM>::kBytes, P.U + tile * UTile<8, NM>::kBytes, c8 + 2 * warp};
+    if (!MAPS) out.begin();
     pipelined<DK / 16, 4, NM>(
         [&](int kk, auto& b) {
 #pragma unroll
@@ -431,25 +415,38 @@ chain_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restri
         [&](int kk, auto& b) {
           uint32_t a[kPl<NM>][4];
           to_a<NM>(S[2 * kk], S[2 * kk + 1], a);
-          if (!MAPS)
-#pragma unroll
-          for (int p = 0; p < kPl<NM>; ++p)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              *reinterpret_cast<uint32_t*>(so + p * Tile<DK / 8, NM>::kPlane +
-                                           ((e & 1) * (DK / 8) + 2 * kk + (e >> 1)) * 128) = a[p][e];
+          if (!MAPS) out.state(kk, a);
 #pragma unroll
           for (int nn = 0; nn < 4; ++nn) {
             mma_p<NM, NM>(u[2 * nn], a, b[nn][0]);
             mma_p<NM, NM>(u[2 * nn + 1], a, b[nn][1]);
           }
         });
+    if (!ident)
+#pragma unroll
+      for (int nb = 0; nb < 8; nb += 2) {  // U0^T: blocks (tokens 8 nb, columns 16 warp), transposed
+        uint32_t f[2][kPl<NM>][2];
+        const int i = l >> 3;
+#pragma unroll
+        for (int p = 0; p < kPl<NM>; ++p)
+          ldsm_t(tu.at(p, nb + (i >> 1), 2 * warp + (i & 1), l & 7), f[0][p][0], f[0][p][1], f[1][p][0], f[1][p][1]);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            uint32_t x[kPl<NM>];
+#pragma unroll
+            for (int p = 0; p < kPl<NM>; ++p) x[p] = f[h][p][e];
+            const float2 v = join2<NM>(x);
+            u[nb + h][2 * e] += v.x;
+            u[nb + h][2 * e + 1] += v.y;
+          }
+      }
     const float decay = G[kUp + 63];
 #pragma unroll
     for (int nb = 0; nb < DK / 8; ++nb)
 #pragma unroll
       for (int e = 0; e < 4; ++e) S[nb][e] *= decay;
-    char* uo = P.U + tile * Tile<8, NM>::kBytes;
     uint32_t a[kPl<NM>][4];
     pipelined<4 * (DK / 64), 4, NI>(
         [&](int s, auto& b) {
@@ -460,13 +457,10 @@ chain_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restri
         [&](int s, auto& b) {
           const int kk = s / (DK / 64), n0 = 8 * (s % (DK / 64));
           if (n0 == 0) {
+            if (!MAPS) out.values(kk, u[2 * kk], u[2 * kk + 1]);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               float(&x)[4] = u[2 * kk + h];
-              if (!MAPS) {
-                store_block_t<8, NM>(uo, 2 * kk + h, c8 + 2 * warp, x[0], x[1]);
-                store_block_t<8, NM>(uo, 2 * kk + h, c8 + 2 * warp + 1, x[2], x[3]);
-              }
               const float2 down = *reinterpret_cast<const float2*>(&G[kDown + 16 * kk + 8 * h + row]);
               x[0] *= down.x;
               x[1] *= down.y;
@@ -481,9 +475,11 @@ chain_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restri
             mma_p<NM, NI>(S[n0 + 2 * nn + 1], a, b[nn][1]);
           }
         });
+    if (!MAPS) out.end();
     __syncwarp();
     if (l == 0) mbar_arrive(&empty[s]);
   }
+  if (!MAPS && L::Out::kBytes > 0 && l == 0) bulk_wait_all();  // before the block's shared memory goes
   if constexpr (MAPS) {
     if (ident) {
       constexpr int kTile = Tile<DK / 8, kMapForm<NM>>::kBytes;
@@ -595,7 +591,9 @@ combine_kernel(const Problem P, float* __restrict__ carry, const float* __restri
 template <int DK, int NI, int NM>
 struct OutputSmem {
   static constexpr int kQ = Tile<DK / 8, NI>::kBytes, kU = Tile<8, NM>::kBytes, kS = Tile<DK / 8, NM>::kBytes;
-  static constexpr int kBytes = 2 * kQ + kU + kS + kGates * 4 + 16;
+  // Two slots of (U, S): the second's S takes K's place once P is done, where the two are of one size
+  static constexpr int kSlots = kQ == kS ? 2 : 1;
+  static constexpr int kBytes = 2 * kQ + kSlots * kU + kS + kGates * 4 + 24;
 };
 
 // O = scale (diag(gamma) Q S + P U) of one chunk of one head; zero on the row's padding.
@@ -614,26 +612,32 @@ output_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restr
   if (w.rows <= 0) return;
   const uint32_t base = smem_addr(smem);
   const InTile<DK / 8, NI> tq{base}, tk{base + L::kQ};
-  const Tile<8, NM> tu{base + 2 * L::kQ};
-  const Tile<DK / 8, NM> ts{base + 2 * L::kQ + L::kU};
-  float* G = reinterpret_cast<float*>(smem + 2 * L::kQ + L::kU + L::kS);
-  uint64_t* bars = reinterpret_cast<uint64_t*>(G + kGates);
+  constexpr int kMid = 2 * L::kQ + L::kSlots * L::kU;
+  const auto tu_of = [&](int part) { return UTile<8, NM>{base + 2 * L::kQ + (part % L::kSlots) * L::kU}; };
+  const auto ts_of = [&](int part) {
+    return Tile<DK / 8, NM>{part % L::kSlots == 0 ? base + kMid : base + L::kQ};
+  };
+  float* G = reinterpret_cast<float*>(smem + kMid + L::kS);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(G + kGates);  // of Q, K, gates; of the slots
   const int dvb = P.Dv / 64;
   const auto load = [&](int part) {
-    mbar_arrive_expect_tx(&bars[1], L::kU + (P.single ? 0 : L::kS));
-    if (!P.single) bulk_load(ts.base, P.S + (w.nc * dvb + part) * L::kS, L::kS, &bars[1]);
-    bulk_load(tu.base, P.U + (w.nc * dvb + part) * L::kU, L::kU, &bars[1]);
+    if (tid != 0 || part >= dvb) return;
+    uint64_t* bar = &bars[1 + part % L::kSlots];
+    mbar_arrive_expect_tx(bar, L::kU + (P.single ? 0 : L::kS));
+    if (!P.single) bulk_load(ts_of(part).base, P.S + (w.nc * dvb + part) * L::kS, L::kS, bar);
+    bulk_load(tu_of(part).base, P.U + (w.nc * dvb + part) * L::kU, L::kU, bar);
   };
   if (tid == 0) {
     mbar_init(&bars[0], 1);
     mbar_init(&bars[1], 1);
+    mbar_init(&bars[2], 1);
     fence_mbar_init();
     mbar_arrive_expect_tx(&bars[0], 2 * tma_bytes<NI>(L::kQ) + 4 * kGateFloats<NM>);
     bulk_load(smem_addr(G), P.gates + w.nc * kGates, 4 * kGateFloats<NM>, &bars[0]);
   }
   load_rows<128>(tq, &M.q, &bars[0], q, P.ldq, w.hk * DK, w.t, w.b, P.L, w.rows, tid);
   load_rows<128>(tk, &M.k, &bars[0], k, P.ldk, w.hk * DK, w.t, w.b, P.L, w.rows, tid);
-  if (tid == 0) load(0);
+  load(0);
   __syncthreads();
   mbar_wait(&bars[0], 0, P.err);
   const int r = l >> 2, c0 = 2 * (l & 3), r0 = 16 * warp + r;
@@ -665,11 +669,14 @@ output_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restr
   }
   const float up0 = G[kUp + r0], up1 = G[kUp + r0 + 8];
   for (int part = 0; part < dvb; ++part) {
-    if (part > 0) {
-      __syncthreads();
-      if (tid == 0) load(part);
+    if (part + L::kSlots - 1 < dvb && (part > 0 || L::kSlots > 1)) {
+      if (NI == 3) fence_proxy_async_smem();  // K was written by these threads
+      __syncthreads();  // K, or the part before, has been read
+      load(part + L::kSlots - 1);
     }
-    mbar_wait(&bars[1], part & 1, P.err);
+    const UTile<8, NM> tu = tu_of(part);
+    const Tile<DK / 8, NM> ts = ts_of(part);
+    mbar_wait(&bars[1 + part % L::kSlots], (part / L::kSlots) & 1, P.err);
     float acc[8][4] = {};
     if (!P.single) {
 #pragma unroll

@@ -75,13 +75,6 @@ __device__ __forceinline__ void load32(uint32_t taddr, float (&v)[32]) {
   for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
 }
 
-// A staged 64 x 64 tile to steps step .. of batch row b, columns col ..; steps past the row's end are not written.
-__device__ __forceinline__ void store_tile(const CUtensorMap* map, uint32_t tile, int col, int64_t step, int b) {
-  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map), "r"(tile),
-               "r"(col), "r"((int)step), "r"(b)
-               : "memory");
-}
-
 __device__ __forceinline__ void st_shared16(uint32_t addr, const uint32_t (&w)[4]) {
   asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3])
                : "memory");
@@ -223,7 +216,7 @@ grad_tc_kernel(const Problem P, const __grid_constant__ Maps M, const __grid_con
         bulk_load(base + L::kGates0 + (n & 1) * L::kGateStage, P.gates + w.nc * kGates, L::kGateStage, la);
 #pragma unroll
         for (int p = 0; p < DVB; ++p)
-          load_rows<1>(Tile<8, 1, true>{base + L::kV + p * L::kT8}, &M.v, la, none, 0, w.h * P.Dv + 64 * p, w.t, w.b,
+          load_rows<1>(Tile<8, 1, 1>{base + L::kV + p * L::kT8}, &M.v, la, none, 0, w.h * P.Dv + 64 * p, w.t, w.b,
                        P.L, 0, 0);
       };
       const auto load_b = [&](uint32_t item) {
@@ -234,7 +227,7 @@ grad_tc_kernel(const Problem P, const __grid_constant__ Maps M, const __grid_con
         for (int p = 0; p < DVB; ++p) {
           const uint32_t at = base + L::kPart0 + p * L::kPart;
           const int64_t tile = w.nc * DVB + p;
-          load_rows<1>(Tile<8, 1, true>{at}, &M.d_o, lb, none, 0, w.h * P.Dv + 64 * p, w.t, w.b, P.L, 0, 0);
+          load_rows<1>(Tile<8, 1, 1>{at}, &M.d_o, lb, none, 0, w.h * P.Dv + 64 * p, w.t, w.b, P.L, 0, 0);
           bulk_load(at + 2 * L::kT8, P.U + tile * L::kT8, L::kT8, lb);
           if (P.single) continue;
           bulk_load(at + 3 * L::kT8, P.S + tile * L::kS, L::kS, lb);
@@ -247,9 +240,9 @@ grad_tc_kernel(const Problem P, const __grid_constant__ Maps M, const __grid_con
         mbar_arrive_expect_tx(lc, DK / 64 * 2 * L::kT8);
 #pragma unroll
         for (int j = 0; j < DK / 64; ++j) {
-          load_rows<1>(Tile<8, 1, true>{base + 2 * j * L::kT8}, &M.q, lc, none, 0, w.hk * DK + 64 * j, w.t, w.b, P.L, 0,
+          load_rows<1>(Tile<8, 1, 1>{base + 2 * j * L::kT8}, &M.q, lc, none, 0, w.hk * DK + 64 * j, w.t, w.b, P.L, 0,
                        0);
-          load_rows<1>(Tile<8, 1, true>{base + (2 * j + 1) * L::kT8}, &M.k, lc, none, 0, w.hk * DK + 64 * j, w.t, w.b,
+          load_rows<1>(Tile<8, 1, 1>{base + (2 * j + 1) * L::kT8}, &M.k, lc, none, 0, w.hk * DK + 64 * j, w.t, w.b,
                        P.L, 0, 0);
         }
       };
@@ -266,13 +259,13 @@ grad_tc_kernel(const Problem P, const __grid_constant__ Maps M, const __grid_con
 #pragma unroll
         for (int p = 0; p < DVB; ++p)  // dR = T^T dU
           tc::mma_k<4>(tm + L::dr(p), tc::desc(base + L::kT, 1024, 128, false), 2048,
-                       tc::desc(base + L::kDU + p * L::kT8, 1024, 128, false), 2048, tc::instr(64, true, true), false);
+                       tc::desc(base + L::kDU + p * L::kT8, 128, 1024, false), 256, tc::instr(64, true, true), false);
         tc::commit(m1);
         mbar_wait(lb, ph, P.err);
 #pragma unroll
         for (int p = 0; p < (P.single ? 0 : DVB); ++p) {  // rows 64..: U dS'^T
           const uint32_t at = base + L::kPart0 + p * L::kPart;
-          tc::mma_k<4>(tm + L::kX2, tc::desc(at + L::kT8, 128, 1024, false), 256,
+          tc::mma_k<4>(tm + L::kX2, tc::desc(at + 2 * L::kT8 - 1024, 1024, 128, false), 2048,
                        tc::desc(at + 3 * L::kT8 + L::kS, DK * 16, 128, false), 2 * DK * 16,
                        tc::instr(DK, false, true), p > 0);
         }
@@ -287,7 +280,7 @@ grad_tc_kernel(const Problem P, const __grid_constant__ Maps M, const __grid_con
         for (int p = 0; p < DVB; ++p) {
           const uint32_t at = base + L::kPart0 + p * L::kPart;
           const uint64_t od = tc::desc(at, 16, 1024, true);  // [dO; dR]
-          tc::mma_k<4>(tm + L::kDPA, od, 32, tc::desc(at + 2 * L::kT8, 128, 1024, false), 256,
+          tc::mma_k<4>(tm + L::kDPA, od, 32, tc::desc(at + 2 * L::kT8, 1024, 128, false), 2048,
                        tc::instr(64, false, false), p > 0);
           if (!P.single)
             tc::mma_k<4>(tm + L::kX13, od, 32, tc::desc(at + 3 * L::kT8, DK * 16, 128, false), 2 * DK * 16,
@@ -296,7 +289,7 @@ grad_tc_kernel(const Problem P, const __grid_constant__ Maps M, const __grid_con
         tc::commit(m2);
 #pragma unroll
         for (int p = 0; p < DVB; ++p)  // dV has been staged where dU was
-          tc::store_tile(&O.dv, base + L::kDU + p * L::kT8, w.h * P.Dv + 64 * p, w.t, w.b);
+          store_tile(&O.dv, base + L::kDU + p * L::kT8, w.h * P.Dv + 64 * p, w.t, w.b);
         bulk_commit();
         mbar_wait(e2, ph, P.err);
         tmem_fence_after_sync();
@@ -319,8 +312,8 @@ grad_tc_kernel(const Problem P, const __grid_constant__ Maps M, const __grid_con
           const int hq = heads == P.Hk ? w.hk : w.h;
 #pragma unroll
           for (int j = 0; j < DK / 64; ++j) {
-            tc::store_tile(&O.dq, base + L::stage_q(j), hq * DK + 64 * j, w.t, w.b);
-            tc::store_tile(&O.dk, base + L::stage_k(j), hq * DK + 64 * j, w.t, w.b);
+            store_tile(&O.dq, base + L::stage_q(j), hq * DK + 64 * j, w.t, w.b);
+            store_tile(&O.dk, base + L::stage_k(j), hq * DK + 64 * j, w.t, w.b);
           }
           bulk_commit();
         }

@@ -64,8 +64,8 @@ blr_status grad(const Problem& p, const BwdCall& c, TG* dq, TG* dk, int heads) {
     if (p.Dv == 128) return grad_tc<TI, TG, DK, 2>(p, c, dq, dk, heads);
   }
   // 16 warps an SM hide each other's latencies; float32's operands take the registers of 8
-  constexpr int kParts = NM == 3 || DK == 64 ? 2 : 4, bytes = GradSmem<DK, NI, NM, kParts>::kBytes;
-  return start("grad", grad_kernel<TI, TG, DK, NI, NM, kParts>, p.B * p.Hv * p.n, 128 * kParts, bytes, c.stream, p,
+  constexpr int kColumns = NM == 3 || DK == 64 ? 2 : 4, bytes = GradSmem<DK, NI, NM, kColumns>::kBytes;
+  return start("grad", grad_kernel<TI, TG, DK, NI, NM, kColumns>, p.B * p.Hv * p.n, 128 * kColumns, bytes, c.stream, p,
                c.maps, static_cast<const TI*>(c.q), static_cast<const TI*>(c.k), static_cast<const TI*>(c.v),
                static_cast<const TI*>(c.d_o), dq, dk, heads, static_cast<TI*>(c.dv), static_cast<TI*>(c.dg),
                static_cast<TI*>(c.dbeta));
@@ -79,7 +79,8 @@ blr_status bwd_dk(const Problem& p, const BwdCall& c) {
   BLR_TRY(start("du", du_kernel<TI, DK, NI, NM>, chunks, 128, DuSmem<DK, NI>::kBytes, c.stream, p, c.maps, q, k, d_o));
   // two stages of float32 tiles and 64 columns do not fit beside each other
   constexpr int kWide = 2 * BackSmem<DK, NI, NM, 4>::kStage <= 227 * 1024 ? 4 : 2;
-  constexpr int wide = BackSmem<DK, NI, NM, kWide>::kBytes, narrow = BackSmem<DK, NI, NM, 2>::kBytes;
+  constexpr int wide = BackSmem<DK, NI, NM, kWide>::kBytes,
+                narrow = BackSmem<DK, NI, NM, 2>::kBytes;
   const int64_t heads = p.B * p.Hv;
   if (p.nseg > 1) {
     BLR_TRY(start("back maps", back_kernel<TI, DK, NI, NM, kWide, true>, heads * p.nseg * (p.Dv / (16 * kWide)),

@@ -158,17 +158,18 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
   return y;
 }
 
-// A tile of 64 rows x C8 * 8 columns in shared memory, in the planes of form P. SW: the layout that TMA
-// writes (1024-byte aligned, one plane).
-template <int C8, int P, bool SW = false>
+// A tile of 64 rows x C8 * 8 columns in shared memory, in the planes of form P. Its blocks follow one
+// another row by row (0), or column by column (2: U and dU, of which a warp of a chain kernel owns columns);
+// 1: the layout that TMA writes (1024-byte aligned, one plane).
+template <int C8, int P, int LAY = 0>
 struct Tile {
   static constexpr int kPlane = 8 * C8 * 128;  // bytes
   static constexpr int kBytes = kPl<P> * kPlane;
   uint32_t base;
   // Row i of block (r8, c8): 16 bytes.
   __device__ __forceinline__ uint32_t at(int p, int r8, int c8, int i) const {
-    if constexpr (SW) return base + (c8 >> 3) * 8192 + r8 * 1024 + i * 128 + (((c8 & 7) ^ i) << 4);
-    return base + p * kPlane + (r8 * C8 + c8) * 128 + i * 16;
+    if constexpr (LAY == 1) return base + (c8 >> 3) * 8192 + r8 * 1024 + i * 128 + (((c8 & 7) ^ i) << 4);
+    return base + p * kPlane + (LAY == 2 ? c8 * 8 + r8 : r8 * C8 + c8) * 128 + i * 16;
   }
   // Left operand, rows 8 m8 .. + 16, columns 8 k8 .. + 16, of the tile.
   __device__ __forceinline__ void a(int m8, int k8, uint32_t (&f)[kPl<P>][4]) const {
@@ -217,7 +218,9 @@ struct Tile {
   }
 };
 template <int C8, int P>
-using InTile = Tile<C8, P, P == 1>;  // of a caller's tensor
+using InTile = Tile<C8, P, P == 1 ? 1 : 0>;  // of a caller's tensor
+template <int C8, int P>
+using UTile = Tile<C8, P, 2>;
 
 // An accumulator tile (16 rows x 8 columns in d[0], d[1]: row lane / 4; d[2], d[3]: row + 8) as half
 // of a left operand: blocks (x, y) give its columns 0..7 and 8..15.
@@ -280,7 +283,7 @@ __device__ __forceinline__ void each_piece(int tid, F f) {
 // the row's end are zero. bfloat16: one thread, counted on `bar` (kBytes of it). float32: THREADS threads,
 // taken apart into its planes on the way (rows from `rows` on are not read); complete on return.
 template <int THREADS, int C8, typename TI>
-__device__ __forceinline__ void load_rows(const Tile<C8, 1, true>& t, const CUtensorMap* map, uint64_t* bar, const TI*,
+__device__ __forceinline__ void load_rows(const Tile<C8, 1, 1>& t, const CUtensorMap* map, uint64_t* bar, const TI*,
                                           int64_t, int col, int64_t step, int b, int64_t, int, int tid) {
   if (tid == 0) {
 #pragma unroll
@@ -314,20 +317,104 @@ __device__ __forceinline__ void load_rows(const Tile<C8, 3>& t, const CUtensorMa
   });
 }
 
-// Columns [8 c8, 8 c8 + 8 C) of a 64 x 64 tile of the workspace, by one thread.
+// Columns [8 c8, 8 c8 + 8 C) of a 64 x 64 tile of U or dU in the workspace, by one thread.
 template <int C, int P>
-__device__ __forceinline__ void bulk_columns(const Tile<C, P>& t, const char* src, int c8, uint64_t* bar) {
-  if constexpr (C == 8) {
-    bulk_load(t.base, src, Tile<C, P>::kBytes, bar);
-  } else {
+__device__ __forceinline__ void bulk_columns(const UTile<C, P>& t, const char* src, int c8, uint64_t* bar) {
 #pragma unroll
-    for (int p = 0; p < kPl<P>; ++p)
-#pragma unroll
-      for (int r8 = 0; r8 < 8; ++r8)
-        bulk_load(t.base + p * Tile<C, P>::kPlane + r8 * C * 128, src + p * Tile<8, P>::kPlane + (r8 * 8 + c8) * 128,
-                  C * 128, bar);
-  }
+  for (int p = 0; p < kPl<P>; ++p)
+    bulk_load(t.base + p * UTile<C, P>::kPlane, src + p * UTile<8, P>::kPlane + c8 * 1024, C * 1024, bar);
 }
+// A 64 x 64 tile under the 128-byte swizzle to steps step .. of batch row b, columns col ..; steps past the row's
+// end are not written.
+__device__ __forceinline__ void store_tile(const CUtensorMap* map, uint32_t tile, int col, int64_t step, int b) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map), "r"(tile),
+               "r"(col), "r"((int)step), "r"(b)
+               : "memory");
+}
+// A linear copy of `bytes` (a multiple of 16) to the workspace, in the thread's bulk group.
+__device__ __forceinline__ void bulk_store(void* dst, uint32_t src, uint32_t bytes) {
+  asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(src), "r"(bytes) : "memory");
+}
+// Four 8 x 8 blocks from a warp's registers; lane l gives the address of row l % 8 of block l / 8.
+__device__ __forceinline__ void stsm(uint32_t addr, uint32_t r0, uint32_t r1, uint32_t r2, uint32_t r3) {
+  asm volatile("stmatrix.sync.aligned.m8n8.x4.shared.b16 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(r0), "r"(r1), "r"(r2),
+               "r"(r3) : "memory");
+}
+__device__ __forceinline__ void stsm_t(uint32_t addr, uint32_t r0, uint32_t r1, uint32_t r2, uint32_t r3) {
+  asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(r0), "r"(r1),
+               "r"(r2), "r"(r3) : "memory");
+}
+
+// What a warp of a chain kernel writes for a chunk: its 16 columns of the state (S^T, as left operands) and of
+// U^T. Staged in shared memory and sent out linearly, or stored block by block.
+template <int DK, int P, bool STAGED>
+struct ChainOut {
+  static constexpr int kS = DK * 32, kU = 2048, kBytes = STAGED ? kPl<P> * (kS + kU) : 0;
+  uint32_t at;   // this warp's place
+  char *s, *u;   // this chunk's tiles in the workspace
+  int c8;        // the warp's first column block
+  __device__ __forceinline__ void begin() const {
+    if constexpr (STAGED) {
+      if ((threadIdx.x & 31) == 0) bulk_wait_read<0>();
+      __syncwarp();
+    }
+  }
+  // Left operand kk of S^T: blocks (columns c8, c8 + 1; rows of S 2 kk, 2 kk + 1).
+  __device__ __forceinline__ void state(int kk, const uint32_t (&a)[kPl<P>][4]) const {
+    const int l = threadIdx.x & 31, i = l >> 3;
+#pragma unroll
+    for (int p = 0; p < kPl<P>; ++p) {
+      if constexpr (STAGED) {
+        stsm(at + p * kS + ((i & 1) * (DK / 8) + 2 * kk + (i >> 1)) * 128 + (l & 7) * 16, a[p][0], a[p][1], a[p][2],
+             a[p][3]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          *reinterpret_cast<uint32_t*>(s + p * Tile<DK / 8, P>::kPlane + l * 4 +
+                                       ((c8 + (e & 1)) * (DK / 8) + 2 * kk + (e >> 1)) * 128) = a[p][e];
+      }
+    }
+  }
+  // Steps 16 kk .. of U^T, two accumulators of 8 steps.
+  __device__ __forceinline__ void values(int kk, const float (&x)[4], const float (&y)[4]) const {
+    const int l = threadIdx.x & 31, i = l >> 3;
+    uint32_t w[4][kPl<P>];
+    split2<P>(x[0], x[1], w[0]);
+    split2<P>(x[2], x[3], w[1]);
+    split2<P>(y[0], y[1], w[2]);
+    split2<P>(y[2], y[3], w[3]);
+#pragma unroll
+    for (int p = 0; p < kPl<P>; ++p) {
+      if constexpr (STAGED) {
+        stsm_t(at + kPl<P> * kS + p * kU + ((i & 1) * 8 + 2 * kk + (i >> 1)) * 128 + (l & 7) * 16, w[0][p], w[1][p],
+               w[2][p], w[3][p]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          *reinterpret_cast<uint32_t*>(u + p * UTile<8, P>::kPlane + ((c8 + (e & 1)) * 8 + 2 * kk + (e >> 1)) * 128 +
+                                       l * 4) = transpose8(w[e][p]);
+      }
+    }
+  }
+  __device__ __forceinline__ void end() const {
+    if constexpr (STAGED) {
+      fence_proxy_async_smem();
+      __syncwarp();
+      if ((threadIdx.x & 31) == 0) {
+#pragma unroll
+        for (int p = 0; p < kPl<P>; ++p)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            bulk_store(s + p * Tile<DK / 8, P>::kPlane + (c8 + i) * (DK / 8) * 128,
+                       at + p * kS + i * (kS / 2), kS / 2);
+            bulk_store(u + p * UTile<8, P>::kPlane + (c8 + i) * 1024,
+                       at + kPl<P> * kS + p * kU + i * 1024, 1024);
+          }
+        bulk_commit();
+      }
+    }
+  }
+};
 
 // N steps of which each loads right operands and multiplies by them: the next step's are on their way
 // while this one's are multiplied.
@@ -351,15 +438,14 @@ __device__ __forceinline__ void store_block(char* tile, int r8, int c8, float x,
   for (int p = 0; p < kPl<P>; ++p)
     *reinterpret_cast<uint32_t*>(tile + p * (8 * C8 * 128) + (r8 * C8 + c8) * 128 + (threadIdx.x & 31) * 4) = w[p];
 }
-// The same, transposed: the accumulator's rows become the tile's columns.
-template <int C8, int P>
-__device__ __forceinline__ void store_block_t(char* tile, int r8, int c8, float x, float y) {
+// The same in a tile of U or dU.
+template <int P>
+__device__ __forceinline__ void store_u(char* tile, int r8, int c8, float x, float y) {
   uint32_t w[kPl<P>];
   split2<P>(x, y, w);
 #pragma unroll
   for (int p = 0; p < kPl<P>; ++p)
-    *reinterpret_cast<uint32_t*>(tile + p * (8 * C8 * 128) + (r8 * C8 + c8) * 128 + (threadIdx.x & 31) * 4) =
-        transpose8(w[p]);
+    *reinterpret_cast<uint32_t*>(tile + p * UTile<8, P>::kPlane + (c8 * 8 + r8) * 128 + (threadIdx.x & 31) * 4) = w[p];
 }
 
 __device__ __forceinline__ void store_pair(__nv_bfloat16* p, float x, float y) {
