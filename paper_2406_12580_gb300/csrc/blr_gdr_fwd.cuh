@@ -20,8 +20,8 @@ __device__ __forceinline__ void load_gates(const T* g, const T* beta, int64_t st
                                            float* out) {  // by one warp; `out`: kGates floats
   using Sum = typename std::conditional<(P > 1), double, float>::type;
   const int l = threadIdx.x & 31;
-  const Sum x = 2 * l < rows ? fmaxf(to_float(g[2 * l * stride]), kMinDecay) : 0.0f;
-  const Sum y = 2 * l + 1 < rows ? fmaxf(to_float(g[(2 * l + 1) * stride]), kMinDecay) : 0.0f;
+  const Sum x = 2 * l < rows ? log_decay(to_float(g[2 * l * stride])) : 0.0f;
+  const Sum y = 2 * l + 1 < rows ? log_decay(to_float(g[(2 * l + 1) * stride])) : 0.0f;
   Sum s = x + y;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {

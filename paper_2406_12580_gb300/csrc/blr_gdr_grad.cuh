@@ -426,7 +426,7 @@ grad_tc_kernel(const Problem P, const __grid_constant__ Maps M, const __grid_con
             const int j = 32 * hf + i;
             if ((i & 3) == 0) gj = *reinterpret_cast<const float4*>(&G[j]);
             const float g = (i & 3) == 0 ? gj.x : (i & 3) == 1 ? gj.y : (i & 3) == 2 ? gj.z : gj.w;
-            const float d = __expf(fminf(gi - g, 0.0f));
+            const float d = __expf(gi - g);  // (above the diagonal not used)
             if (side == 0) {
               x[i] = j <= row ? P.scale * x[i] * d : 0.0f;
               y[i] *= x[i];

@@ -91,7 +91,8 @@ gdr_steps_kernel(int64_t K, int Hk, int Hv, int Dv, int64_t ldq, int64_t ldk, in
   float4 vv;
   const auto load = [&](int64_t t) {
     const int64_t at = b * K + t;
-    ga = to_f(g[at * Hv + h]);
+    const float gt = to_f(g[at * Hv + h]);
+    ga = gt < -120.0f ? -120.0f : gt;  // a decay of 0 in float32
     bt = to_f(beta[at * Hv + h]);
     vv = load4(v + at * ldv + (int64_t)h * Dv + col);
 #pragma unroll
@@ -112,7 +113,7 @@ gdr_steps_kernel(int64_t K, int Hk, int Hv, int Dv, int64_t ldq, int64_t ldk, in
       r.w = fmaf(kk[i], S[i].w, r.w);
     }
     r = sum_rows(r);
-    const float a = expf(fmaxf(ga, -120.0f));
+    const float a = expf(ga);
     const float4 u = make_float4(bt * (vv.x - a * r.x), bt * (vv.y - a * r.y), bt * (vv.z - a * r.z),
                                  bt * (vv.w - a * r.w));
     float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);

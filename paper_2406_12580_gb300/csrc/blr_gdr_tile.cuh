@@ -35,7 +35,8 @@ namespace blr {
 namespace gdr {
 
 constexpr int kC = 64;               // steps of a chunk
-constexpr float kMinDecay = -120.0f;  // exp(-120) is 0 in float32
+// A step's log decay: exp(-120) is 0 in float32, and sums of 64 stay finite (a NaN stays one).
+__device__ __forceinline__ float log_decay(float g) { return g < -120.0f ? -120.0f : g; }
 
 __device__ __forceinline__ uint32_t pack2(float a, float b) {  // a in the low half
   const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);

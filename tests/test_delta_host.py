@@ -143,3 +143,19 @@ def test_the_chunked_form_equals_the_recurrence():
         outs.append(d["scale"] * (G.exp()[:, None] * (q @ S) + (D * (q @ k.T)) @ U))
         S = G[-1].exp() * S + (k * (G[-1] - G).exp()[:, None]).T @ U
     assert off(torch.cat(outs)[None, :, None], want["o"]) <= 1e-6 and off(S[None, None], want["s"]) <= 1e-6
+
+
+def test_binding_loads_and_refuses_without_a_device(lib):
+    """The C++ binding imports on a machine without a GPU and raises, rather than falling back."""
+    torch = pytest.importorskip("torch")
+    ext = _lib.extension()
+    for name in ("gdr_fwd", "gdr_bwd", "gdr_steps", "adamw_step", "rule"):
+        assert callable(getattr(ext, name))
+    from paper_2406_12580_gb300.delta import gated_delta_rule
+    q, v, g = torch.zeros(1, 2, 1, 64), torch.zeros(1, 2, 1, 64), torch.zeros(1, 2, 1)
+    with pytest.raises((RuntimeError, ValueError)):
+        gated_delta_rule(q, q, v, g, g)
+    with pytest.raises(TypeError):
+        gated_delta_rule(q, None, v, g, g)
+    with pytest.raises(TypeError):
+        ext.rule(q)

@@ -279,3 +279,21 @@ def test_no_second_derivative():
     o, _ = gated_delta_rule(q, *(d[n] for n in ("k", "v", "g", "beta")))
     with pytest.raises(RuntimeError):
         torch.autograd.grad(o.sum(), q, create_graph=True)
+
+
+def test_not_a_number_is_not_hidden():
+    """A NaN among the gates or values shows in what comes after it in its row, and in no other row."""
+    for name in ("g", "beta", "v"):
+        d = make(2, 100, 1, 1, 64, 64, torch.bfloat16, seed=19, device="cuda")
+        d[name][1, 40] = float("nan")
+        o, _ = gated_delta_rule(*(d[n] for n in ("q", "k", "v", "g", "beta")))
+        assert torch.isfinite(o[0]).all() and torch.isnan(o[1, 40:]).any(-1).all()
+
+
+def test_status_of_a_workspace():
+    from paper_2406_12580_gb300 import BLR_OK, blr_gdr_status
+    d = make(1, 100, 1, 1, 64, 64, torch.bfloat16, seed=20, device="cuda")
+    desc = GDRDesc(1, 100, 1, 1, 64, 64, io=BLR_BF16)
+    ws = torch.full((blr_gdr_workspace_bytes(desc, 0),), 255, dtype=torch.uint8, device="cuda")
+    blr_gdr_fwd(desc, 0, None, *(d[n] for n in ("q", "k", "v", "g", "beta")), None, torch.empty_like(d["v"]), None, ws)
+    assert blr_gdr_status(ws) == BLR_OK
