@@ -7,17 +7,25 @@
 // 8-bit code must not hang on how the compiler fuses a sum, or two builds would
 // drift apart by whole codes. Bound by memory with float32 moments: 28 bytes a
 // value with float32 everywhere, 28 with bfloat16 parameters and float32 masters
-// (190 M values: 771 us, 6.9 TB/s). With 8-bit moments about 10 bytes a value
-// are left and the instructions bound the kernel; the quotient, a thousandth of
-// w, is then approximate to two units in the last place.
+// (190 M values: 763 us, 7.0 TB/s). With 8-bit moments about 10 bytes a value
+// are left (95 M values: 159 us, 6.0 TB/s) and the instructions count: values
+// are taken in pairs, and the quotient, a thousandth of w, is approximate to two
+// units in the last place (both: 227 -> 204 us).
 //
 // Layout: the tensors' records travel in the kernel's parameters (nothing is
 // copied to the device, nothing is kept between calls), up to kMaxTensors a
-// launch. A block takes one chunk of kChunk values of one tensor, found by a
-// binary search over the records' first chunks; a warp takes 256 consecutive
-// values at a time, 8 a lane, which is also the block that shares a scale of
-// the 8-bit moments: its maximum is one warp reduction, in registers.
+// launch. A block takes one chunk of values of one tensor, found by a binary
+// search over the records' first chunks; a warp takes 256 consecutive values at
+// a time, 8 a lane, which is also the block that shares a scale of the 8-bit
+// moments: its maximum is one warp reduction, in registers. With 8-bit moments,
+// where a warp computes for as long as it waits, it loads its next 256 values
+// meanwhile, and a block is one warp (blocks of 256, 128, 64 and 32 threads:
+// 211, 181, 167, 159 us); with float32 moments, which wait for memory alone,
+// blocks of 256 (128: 762 -> 770 us).
+#include <float.h>
 #include <math.h>
+
+#include <type_traits>
 
 #include <cuda_bf16.h>
 #include <cuda_fp8.h>
@@ -28,13 +36,13 @@ namespace {
 
 using blr::fail;
 
-constexpr int kThreads = 256;
+template <int BITS> constexpr int kThreads = BITS == 8 ? 32 : 256;
 constexpr int kGroup = 256;   // values a warp takes at a time, one scale of the 8-bit moments
-// Values a block takes. A block first finds its tensor; with 8-bit moments, where that counts, 16384 values
-// spread it over eight groups a warp (285 -> 259 us of 95 M values; with float32 moments, which wait for
-// memory alone, 771 -> 794). A small model (under 4 M values) keeps its blocks many.
-constexpr int kChunk = 4096, kCodesChunk = 16384;
-constexpr int64_t kSmallModel = (int64_t)4 << 20;
+// Values a block takes. A block first finds its tensor, which 4096 values pay for; with 8-bit moments a
+// block is a warp, and a smaller model is cut finer, into two chunks for every warp of the GPU at least
+// (5.7 M values: chunks of 8192, 4096 and 512 take 29, 19 and 13 us).
+constexpr int kChunk = 4096, kCodesMin = 512, kCodesMax = 4096;
+constexpr int64_t kWarps = 152 * 32;
 constexpr int kMaxTensors = 448;
 constexpr int kFewTensors = 32;
 constexpr float kE4m3Max = 448.0f;
@@ -58,32 +66,42 @@ struct Hyper {
   const float* grad_scale;
 };
 
-// 8 values of a tensor, as floats.
+// 8 values of a tensor: as they are loaded, as floats, and stored.
 template <typename T> struct Eight;
 template <> struct Eight<float> {
-  static __device__ __forceinline__ void load(const float* p, float (&x)[8]) {
+  float r[8];
+  __device__ __forceinline__ void load(const float* p) {
     asm volatile("ld.global.v8.f32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                 : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]),
-                   "=f"(x[7])
+                 : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]),
+                   "=f"(r[7])
                  : "l"(p));
   }
+  __device__ __forceinline__ void load(const float* p, int n) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = i < n ? p[i] : 0.0f;
+  }
+  __device__ __forceinline__ float get(int i) const { return r[i]; }
   static __device__ __forceinline__ void store(float* p, const float (&x)[8]) {
     asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "f"(x[0]), "f"(x[1]),
                  "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7])
                  : "memory");
   }
-  static __device__ __forceinline__ float one(const float* p) { return *p; }
   static __device__ __forceinline__ void put(float* p, float x) { *p = x; }
 };
 template <> struct Eight<__nv_bfloat16> {
-  static __device__ __forceinline__ void load(const __nv_bfloat16* p, float (&x)[8]) {
-    const uint4 r = __ldcs(reinterpret_cast<const uint4*>(p));
-    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+  uint32_t r[4];
+  __device__ __forceinline__ void load(const __nv_bfloat16* p) {
+    const uint4 x = __ldcs(reinterpret_cast<const uint4*>(p));
+    r[0] = x.x, r[1] = x.y, r[2] = x.z, r[3] = x.w;
+  }
+  __device__ __forceinline__ void load(const __nv_bfloat16* p, int n) {
+    const uint16_t* h = reinterpret_cast<const uint16_t*>(p);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = __uint_as_float(w[i] << 16);
-      x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
+    for (int i = 0; i < 4; ++i)
+      r[i] = (2 * i < n ? (uint32_t)h[2 * i] : 0u) | (2 * i + 1 < n ? (uint32_t)h[2 * i + 1] << 16 : 0u);
+  }
+  __device__ __forceinline__ float get(int i) const {
+    return __uint_as_float(i & 1 ? r[i >> 1] & 0xffff0000u : r[i >> 1] << 16);
   }
   static __device__ __forceinline__ void store(__nv_bfloat16* p, const float (&x)[8]) {
     uint32_t w[4];
@@ -94,7 +112,6 @@ template <> struct Eight<__nv_bfloat16> {
     }
     __stcs(reinterpret_cast<uint4*>(p), make_uint4(w[0], w[1], w[2], w[3]));
   }
-  static __device__ __forceinline__ float one(const __nv_bfloat16* p) { return __bfloat162float(*p); }
   static __device__ __forceinline__ void put(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
 };
 
@@ -115,23 +132,38 @@ __device__ __forceinline__ uint2 load_codes(const uint8_t* p, int n, bool wide) 
     if (i < n) w[i >> 2] |= (uint32_t)p[i] << (8 * (i & 3));
   return make_uint2(w[0], w[1]);
 }
-__device__ __forceinline__ void decode(uint2 c, float (&x)[8]) {
+__device__ __forceinline__ void decode(uint2 c, float2 (&x)[4]) {
   const uint32_t w[2] = {c.x, c.y};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float2 f = from_e4m3x2((uint16_t)(w[i >> 1] >> (16 * (i & 1))));
-    x[2 * i] = f.x;
-    x[2 * i + 1] = f.y;
-  }
+  for (int i = 0; i < 4; ++i) x[i] = from_e4m3x2((uint16_t)(w[i >> 1] >> (16 * (i & 1))));
+}
+
+// Arithmetic on pairs: one instruction for two values, each rounded as alone.
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float min_nan(float a, float b) {
+  float r;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+// 1 / x, to an ulp, of a normal x
+__device__ __forceinline__ float inverse_of(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
 }
 
 // Writes the codes and the scale of a warp's group. A NaN stays with its own value; ROOT: values are not
 // negative, and a positive one is stored as no less than the smallest code.
 template <bool ROOT>
-__device__ __forceinline__ void store_codes(uint8_t* p, float* scale, int n, bool wide, const float (&x)[8]) {
+__device__ __forceinline__ void store_codes(uint8_t* p, float* scale, int n, bool wide, const float2 (&x)[4]) {
   float top = 0.0f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[i]));
+  for (int i = 0; i < 4; ++i) top = fmaxf(fmaxf(top, fabsf(x[i].x)), fabsf(x[i].y));
   top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));  // magnitudes order as their bits
   const float inverse = top > 0.0f ? fminf(__fmul_rn(__fdiv_rn(1.0f, top), kE4m3Max), 3.402823466e38f) : 0.0f;
   uint32_t w[2];
@@ -140,13 +172,12 @@ __device__ __forceinline__ void store_codes(uint8_t* p, float* scale, int n, boo
     uint16_t c[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      float y[2];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        y[j] = __fmul_rn(x[4 * h + 2 * i + j], inverse);
-        if (ROOT) y[j] = y[j] > 0.0f ? fmaxf(y[j], kE4m3Tiny) : y[j];
+      float2 y = __fmul2_rn(x[2 * h + i], both(inverse));
+      if (ROOT) {  // at least the smallest code where positive: 0 stays 0, NaN stays NaN
+        const float2 z = __fmul2_rn(y, both(0x1p100f));
+        y = make_float2(max_nan(y.x, min_nan(z.x, kE4m3Tiny)), max_nan(y.y, min_nan(z.y, kE4m3Tiny)));
       }
-      c[i] = to_e4m3x2(y[0], y[1]);
+      c[i] = to_e4m3x2(y.x, y.y);
     }
     w[h] = (uint32_t)c[0] | (uint32_t)c[1] << 16;
   }
@@ -160,13 +191,8 @@ __device__ __forceinline__ void store_codes(uint8_t* p, float* scale, int n, boo
 }
 
 template <typename T>
-__device__ __forceinline__ void load8(const T* p, int n, bool wide, float (&x)[8]) {
-  if (wide) {
-    Eight<T>::load(p, x);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = i < n ? Eight<T>::one(p + i) : 0.0f;
-  }
+__device__ __forceinline__ void load8(Eight<T>& x, const T* p, int n, bool wide) {
+  if (wide) x.load(p); else x.load(p, n);
 }
 template <typename T>
 __device__ __forceinline__ void store8(T* p, int n, bool wide, const float (&x)[8]) {
@@ -179,8 +205,28 @@ __device__ __forceinline__ void store8(T* p, int n, bool wide, const float (&x)[
   }
 }
 
+// What a step reads of a lane's 8 values.
+template <typename T, bool MASTER>
+struct Input {
+  using W = typename std::conditional<MASTER, float, T>::type;
+  Eight<W> w;
+  Eight<T> g;
+  uint2 mc, vc;
+  float ms, vs;
+  __device__ __forceinline__ void load(const blr_adamw_tensor& t, int64_t i0, int n, bool wide) {
+    load8(w, static_cast<const W*>(MASTER ? t.w : t.p) + i0, n, wide);
+    load8(g, static_cast<const T*>(t.g) + i0, n, wide);
+  }
+  __device__ __forceinline__ void load_moments(const blr_adamw_tensor& t, int64_t i0, int n, bool wide) {
+    mc = load_codes(static_cast<const uint8_t*>(t.m) + i0, n, wide);
+    vc = load_codes(static_cast<const uint8_t*>(t.v) + i0, n, wide);
+    ms = t.m_scale[i0 / kGroup];
+    vs = t.v_scale[i0 / kGroup];
+  }
+};
+
 template <typename T, int BITS, bool MASTER, int CAP>
-__global__ void __launch_bounds__(kThreads, BITS == 8 ? 5 : 1)
+__global__ void __launch_bounds__(kThreads<BITS>, BITS == 8 ? (MASTER || sizeof(T) == 4 ? 28 : 32) : 1)
 adamw_kernel(const __grid_constant__ Table<CAP> table, const __grid_constant__ Hyper h) {
   // the last tensor whose first chunk is not after this block
   int lo = 0, hi = table.count - 1;
@@ -190,51 +236,74 @@ adamw_kernel(const __grid_constant__ Table<CAP> table, const __grid_constant__ H
   }
   const blr_adamw_tensor& t = table.t[lo];
   const int64_t n = t.n, begin = (int64_t)(blockIdx.x - table.first[lo]) * table.chunk;
+  const int64_t end = min(n, begin + table.chunk);
   const bool aligned = (table.wide[lo >> 5] >> (lo & 31)) & 1u;
   const float gs = h.grad_scale == nullptr ? 1.0f : __ldg(h.grad_scale);
   const bool scaled = h.grad_scale != nullptr;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  constexpr int kStride = (kThreads / 32) * kGroup;
-  for (int64_t at = begin + warp * kGroup; at < min(n, begin + table.chunk); at += kStride) {  // by whole warps
-    float w[8], g[8], m[8], v[8];
+  constexpr int kStride = (kThreads<BITS> / 32) * kGroup;
+  const auto left_of = [&](int64_t at, bool wide) {
+    return wide ? 8 : (int)max((int64_t)0, min((int64_t)8, n - at - lane * 8));
+  };
+  int64_t at = begin + warp * kGroup;
+  Input<T, MASTER> x;
+  const auto load = [&](int64_t from) {
+    const bool wide = aligned && from + kGroup <= n;
+    const int left = left_of(from, wide);
+    x.load(t, from + lane * 8, left, wide);
+    if constexpr (BITS == 8) x.load_moments(t, from + lane * 8, left, wide);
+  };
+  if (BITS == 8 && at < end) load(at);
+  for (; at < end; at += kStride) {  // by whole warps
     const bool wide = aligned && at + kGroup <= n;
     const int64_t i0 = at + lane * 8, block = at / kGroup;
-    const int left = wide ? 8 : (int)max((int64_t)0, min((int64_t)8, n - i0));
-    if constexpr (MASTER) {
-      load8<float>(t.w + i0, left, wide, w);
-    } else {
-      load8<T>(static_cast<const T*>(t.p) + i0, left, wide, w);
-    }
-    load8<T>(static_cast<const T*>(t.g) + i0, left, wide, g);
+    const int left = left_of(at, wide);
+    if (BITS == 32) load(at);
+    float w[8], g[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = x.w.get(i), g[i] = x.g.get(i);
     if constexpr (BITS == 32) {
-      load8<float>(static_cast<const float*>(t.m) + i0, left, wide, m);
-      load8<float>(static_cast<const float*>(t.v) + i0, left, wide, v);
+      Eight<float> m0, v0;
+      float m[8], v[8];
+      load8(m0, static_cast<const float*>(t.m) + i0, left, wide);
+      load8(v0, static_cast<const float*>(t.v) + i0, left, wide);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float gi = __fmul_rn(g[i], gs);
-        m[i] = __fadd_rn(__fmul_rn(m[i], h.b1), __fmul_rn(gi, h.c1));
-        v[i] = __fadd_rn(__fmul_rn(v[i], h.b2), __fmul_rn(__fmul_rn(gi, gi), h.c2));
+        m[i] = __fadd_rn(__fmul_rn(m0.r[i], h.b1), __fmul_rn(gi, h.c1));
+        v[i] = __fadd_rn(__fmul_rn(v0.r[i], h.b2), __fmul_rn(__fmul_rn(gi, gi), h.c2));
         const float d = __fadd_rn(__fmul_rn(__fsqrt_rn(v[i]), h.root_scale), h.eps);
         w[i] = __fsub_rn(__fmul_rn(w[i], h.keep), __fmul_rn(__fdiv_rn(m[i], d), h.rate));
       }
       store8<float>(static_cast<float*>(t.m) + i0, left, wide, m);
       store8<float>(static_cast<float*>(t.v) + i0, left, wide, v);
     } else {
-      const uint2 mc = load_codes(static_cast<const uint8_t*>(t.m) + i0, left, wide);
-      const uint2 vc = load_codes(static_cast<const uint8_t*>(t.v) + i0, left, wide);
-      const float ms = t.m_scale[block], vs = t.v_scale[block];
-      decode(mc, m);
-      decode(vc, v);
+      float2 m2[4], v2[4];
+      decode(x.mc, m2);
+      decode(x.vc, v2);
+      const float ms = x.ms, vs = x.vs;
+      if (at + kStride < end) load(at + kStride);  // on its way while this group is computed
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float gi = scaled ? __fmul_rn(g[i], gs) : g[i], r0 = __fmul_rn(v[i], vs);
-        m[i] = __fadd_rn(__fmul_rn(__fmul_rn(m[i], ms), h.b1), __fmul_rn(gi, h.c1));
-        v[i] = __fsqrt_rn(__fadd_rn(__fmul_rn(__fmul_rn(r0, r0), h.b2), __fmul_rn(__fmul_rn(gi, gi), h.c2)));
-        w[i] = w[i] * h.keep - __fdividef(m[i], v[i] * h.root_scale + h.eps) * h.rate;
-        if (!wide && i >= left) m[i] = v[i] = 0.0f;  // values past the end have no part in the scale
+      for (int i = 0; i < 4; ++i) {
+        float2 gi = make_float2(g[2 * i], g[2 * i + 1]);
+        if (scaled) gi = __fmul2_rn(gi, both(gs));
+        const float2 r0 = __fmul2_rn(v2[i], both(vs));
+        m2[i] = __fadd2_rn(__fmul2_rn(__fmul2_rn(m2[i], both(ms)), both(h.b1)), __fmul2_rn(gi, both(h.c1)));
+        const float2 sum = __fadd2_rn(__fmul2_rn(__fmul2_rn(r0, r0), both(h.b2)),
+                                      __fmul2_rn(__fmul2_rn(gi, gi), both(h.c2)));
+        v2[i] = make_float2(__fsqrt_rn(sum.x), __fsqrt_rn(sum.y));
+        const float2 d = __ffma2_rn(v2[i], both(h.root_scale), both(h.eps));
+        const float2 q = __fmul2_rn(m2[i], make_float2(inverse_of(d.x), inverse_of(d.y)));
+        const float2 y = __ffma2_rn(q, both(-h.rate), __fmul2_rn(make_float2(w[2 * i], w[2 * i + 1]), both(h.keep)));
+        w[2 * i] = y.x;
+        w[2 * i + 1] = y.y;
+        if (!wide) {  // values past the end have no part in the scale
+          if (2 * i >= left) m2[i].x = v2[i].x = 0.0f;
+          if (2 * i + 1 >= left) m2[i].y = v2[i].y = 0.0f;
+        }
       }
-      store_codes<false>(static_cast<uint8_t*>(t.m) + i0, t.m_scale + block, left, wide, m);
-      store_codes<true>(static_cast<uint8_t*>(t.v) + i0, t.v_scale + block, left, wide, v);
+      store_codes<false>(static_cast<uint8_t*>(t.m) + i0, t.m_scale + block, left, wide, m2);
+      store_codes<true>(static_cast<uint8_t*>(t.v) + i0, t.v_scale + block, left, wide, v2);
     }
     if constexpr (MASTER) store8<float>(t.w + i0, left, wide, w);
     store8<T>(static_cast<T*>(t.p) + i0, left, wide, w);
@@ -266,7 +335,7 @@ blr_status launch(const blr_adamw_tensor* tensors, int64_t& at, int64_t count, i
     chunks += more;
   }
   if (table.count == 0) return BLR_OK;
-  adamw_kernel<T, BITS, MASTER, CAP><<<(unsigned)chunks, kThreads, 0, stream>>>(table, h);
+  adamw_kernel<T, BITS, MASTER, CAP><<<(unsigned)chunks, kThreads<BITS>, 0, stream>>>(table, h);
   return blr::cuda_check(cudaGetLastError(), "blr_adamw_step");
 }
 
@@ -274,7 +343,8 @@ template <typename T, int BITS, bool MASTER>
 blr_status step_all(const blr_adamw_tensor* tensors, int64_t count, const Hyper& h, cudaStream_t stream) {
   int64_t at = 0, values = 0;
   for (int64_t i = 0; i < count; ++i) values += tensors[i].n;
-  const int chunk = BITS == 8 && values >= kSmallModel ? kCodesChunk : kChunk;
+  int chunk = BITS == 32 ? kChunk : kCodesMax;
+  while (BITS == 8 && chunk > kCodesMin && chunk * 2 * kWarps > values) chunk /= 2;
   while (at < count) {
     // a small table keeps the launch of a small model short
     if (count - at <= kFewTensors)
@@ -331,7 +401,7 @@ blr_status blr_adamw_step(int64_t count, const blr_adamw_tensor* tensors, blr_dt
   h.b2 = (float)beta2;
   h.c2 = (float)(1.0 - beta2);
   h.root_scale = (float)(1.0 / sqrt(1.0 - pow(beta2, (double)step)));
-  h.eps = (float)eps;
+  h.eps = fmaxf((float)eps, FLT_MIN);  // no divisor is 0 or subnormal
   h.keep = (float)(1.0 - lr * weight_decay);
   h.rate = (float)(lr / (1.0 - pow(beta1, (double)step)));
   h.grad_scale = grad_scale;
