@@ -138,8 +138,14 @@ __device__ __forceinline__ void decode(uint2 c, float2 (&x)[4]) {
   for (int i = 0; i < 4; ++i) x[i] = from_e4m3x2((uint16_t)(w[i >> 1] >> (16 * (i & 1))));
 }
 
-// Arithmetic on pairs: one instruction for two values, each rounded as alone.
+// Products of pairs: one instruction for two values, each rounded as alone. Their sums are taken one by
+// one: a sum of pairs is fused with its product, whatever rounding either names (a third of the scales then
+// differ in the last place).
 __device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) { return __fmul2_rn(a, b); }
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  return make_float2(__fadd_rn(a.x, b.x), __fadd_rn(a.y, b.y));
+}
 __device__ __forceinline__ float max_nan(float a, float b) {
   float r;
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
@@ -172,9 +178,9 @@ __device__ __forceinline__ void store_codes(uint8_t* p, float* scale, int n, boo
     uint16_t c[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      float2 y = __fmul2_rn(x[2 * h + i], both(inverse));
+      float2 y = mul2(x[2 * h + i], both(inverse));
       if (ROOT) {  // at least the smallest code where positive: 0 stays 0, NaN stays NaN
-        const float2 z = __fmul2_rn(y, both(0x1p100f));
+        const float2 z = mul2(y, both(0x1p100f));
         y = make_float2(max_nan(y.x, min_nan(z.x, kE4m3Tiny)), max_nan(y.y, min_nan(z.y, kE4m3Tiny)));
       }
       c[i] = to_e4m3x2(y.x, y.y);
@@ -286,15 +292,15 @@ adamw_kernel(const __grid_constant__ Table<CAP> table, const __grid_constant__ H
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         float2 gi = make_float2(g[2 * i], g[2 * i + 1]);
-        if (scaled) gi = __fmul2_rn(gi, both(gs));
-        const float2 r0 = __fmul2_rn(v2[i], both(vs));
-        m2[i] = __fadd2_rn(__fmul2_rn(__fmul2_rn(m2[i], both(ms)), both(h.b1)), __fmul2_rn(gi, both(h.c1)));
-        const float2 sum = __fadd2_rn(__fmul2_rn(__fmul2_rn(r0, r0), both(h.b2)),
-                                      __fmul2_rn(__fmul2_rn(gi, gi), both(h.c2)));
+        if (scaled) gi = mul2(gi, both(gs));
+        const float2 r0 = mul2(v2[i], both(vs));
+        m2[i] = add2(mul2(mul2(m2[i], both(ms)), both(h.b1)), mul2(gi, both(h.c1)));
+        const float2 sum = add2(mul2(mul2(r0, r0), both(h.b2)),
+                                      mul2(mul2(gi, gi), both(h.c2)));
         v2[i] = make_float2(__fsqrt_rn(sum.x), __fsqrt_rn(sum.y));
         const float2 d = __ffma2_rn(v2[i], both(h.root_scale), both(h.eps));
-        const float2 q = __fmul2_rn(m2[i], make_float2(inverse_of(d.x), inverse_of(d.y)));
-        const float2 y = __ffma2_rn(q, both(-h.rate), __fmul2_rn(make_float2(w[2 * i], w[2 * i + 1]), both(h.keep)));
+        const float2 q = mul2(m2[i], make_float2(inverse_of(d.x), inverse_of(d.y)));
+        const float2 y = __ffma2_rn(q, both(-h.rate), mul2(make_float2(w[2 * i], w[2 * i + 1]), both(h.keep)));
         w[2 * i] = y.x;
         w[2 * i + 1] = y.y;
         if (!wide) {  // values past the end have no part in the scale
