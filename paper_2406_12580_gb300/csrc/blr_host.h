@@ -18,6 +18,17 @@ blr_status cuda_check(cudaError_t e, const char* what);
 // cuTensorMapEncodeTiled, through the runtime's driver entry point.
 blr_status tensor_map_encoder(PFN_cuTensorMapEncodeTiled_v12000* out);
 
+// Calls the driver's `encode`. A thread that has made no runtime call yet (an autograd worker whose memory
+// came from a cache) has no context to encode in: it then takes its device's.
+template <typename F>
+CUresult in_context(F encode) {
+  CUresult r = encode();
+  int device = 0;
+  if (r == CUDA_ERROR_INVALID_CONTEXT && cudaGetDevice(&device) == cudaSuccess && cudaSetDevice(device) == cudaSuccess)
+    r = encode();
+  return r;
+}
+
 inline bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
 
 inline blr_status need(const void* p, const char* name, size_t align) {
