@@ -21,7 +21,8 @@ struct DuSmem {
   static constexpr int kBytes = 2 * kQ + kO + kGates * 4 + 16;
 };
 
-// The part of dU that does not hang on later chunks, scale P^T dO, for all chunks at once.
+// The part of dU that does not hang on later chunks, scale P^T dO, for all chunks at once. Bound by memory:
+// 16384 chunks of 128 x 128, bfloat16, 170 us (1.05 GB, 154 us: 0.9 of the copy rate).
 template <typename TI, int DK, int NI, int NM>
 __global__ void __launch_bounds__(128)
 du_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restrict__ q, const TI* __restrict__ k,
@@ -112,8 +113,7 @@ struct BackSmem {
   static constexpr int kW = Tile<DK / 8, NM>::kBytes, kK = Tile<DK / 8, NI>::kBytes, kO = Tile<kO8, NI>::kBytes,
                        kU = Tile<2 * WARPS, NM>::kBytes;
   static constexpr int kStage = 2 * kK + kO + kW + kU + kGateBytes<NI>;
-  // Staged stores take a sixth off a wide block's chunk; in a narrow one, where a chunk waits for its one
-  // warp a scheduler, the staging warp's fence and issue cost more than they save (446 -> 573 us).
+  // by the rule of chain_kernel, whose stores these are
   static constexpr bool kStaged = WARPS == 4 && 2 * kStage + WARPS * ChainOut<DK, NM, true>::kBytes + 48 <= 227 * 1024;
   using Out = ChainOut<DK, NM, kStaged>;
   static constexpr int kOut = WARPS * Out::kBytes;
@@ -124,6 +124,8 @@ struct BackSmem {
 
 // The states' gradients from chunk to chunk, last to first: as chain_kernel, a warp holds dS^T of 16
 // columns in accumulators, and further warps load. MAPS: a segment's N; its phi is the forward's, transposed.
+// Bound as chain_kernel, by three dependent products a chunk: 16384 chunks in 32 heads of 128 x 128, bfloat16,
+// 620 us (2.1 GB, 309 us).
 template <typename TI, int DK, int NI, int NM, int WARPS, bool MAPS>
 __global__ void __launch_bounds__(32 * (WARPS + kLoadWarps<NI>), WARPS == 4 && NM < 3 ? 2 : 1)
 back_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restrict__ q, const TI* __restrict__ k,
@@ -376,7 +378,9 @@ __device__ __forceinline__ void zero_gradients(const Problem& P, const Where& w,
 }
 
 // Everything else, for all chunks at once. Warp (rg, pt) holds rows 16 rg .. of the chunk and one of
-// PARTS parts of the columns of each product.
+// PARTS parts of the columns of each product. For what grad_tc_kernel does not take: two planes, float32, Dv
+// above 128. Bound by the products' fragment reads and the barriers between them: 48 chunks of 64 x 128,
+// float32, take 27 us, the latency of one.
 template <typename TI, typename TG, int DK, int NI, int NM, int PARTS>
 __global__ void __launch_bounds__(128 * PARTS, PARTS == 4 || NM == 3 ? 1 : 2)
 grad_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restrict__ q, const TI* __restrict__ k, const TI* __restrict__ v,
@@ -675,7 +679,8 @@ grad_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restric
     }
 }
 
-// Gradients of shared key heads: the sum over their value heads, in head order.
+// Gradients of shared key heads: the sum over their value heads, in head order (no atomics: the same bits
+// every time). Bound by memory.
 template <typename TI>
 __global__ void __launch_bounds__(256)
 share_kernel(const float* __restrict__ pq, const float* __restrict__ pk, TI* __restrict__ dq, TI* __restrict__ dk,

@@ -108,6 +108,10 @@ struct PrepareSmem {
 // T, W = T diag(beta gamma) K (stored negated), U0 = T diag(beta) V of one chunk of one head. A warp
 // holds 16 rows of the chunk. The diagonal 16 x 16 blocks of T by substitution in float32, the rest by
 // products of two planes at least, whatever the operands of the rest.
+//
+// Bound by the latency of a chunk's steps (loads, A, substitution, the inverse's products, W and U0, each
+// behind a barrier), which four blocks an SM hide in part: 16384 chunks of 128 x 128, bfloat16, 285 us (their
+// 1.2 GB alone 185 us); 4096 single chunks of 64 x 64, 50 us (119 MB, 18 us).
 template <typename TI, int DK, int NI, int NM, bool TRAIN>
 __global__ void __launch_bounds__(128)
 prepare_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restrict__ k, const TI* __restrict__ v,
@@ -132,6 +136,10 @@ prepare_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __rest
     mbar_arrive_expect_tx(&bars[0], tma_bytes<NI>(L::kK));
   }
   load_rows<128>(tk, &M.k, &bars[0], k, P.ldk, w.hk * DK, w.t, w.b, P.L, w.rows, tid);
+  // V's place is A's, but it can come as near as L2 (61 -> 50 us of 4096 chunks with -W's part left out;
+  // where -W is computed before V is needed, it only comes between other loads: 92 -> 96 us)
+  if (NI == 1 && P.single && tid == 0)
+    for (int i = 0; i < P.Dv / 64; ++i) prefetch_rows(&M.v, w.h * P.Dv + 64 * i, w.t, w.b);
   if (warp == 0) {
     const int64_t at = w.step * P.Hv + w.h;
     load_gates<NM>(g + at, beta + at, P.Hv, w.rows, sg);
@@ -236,7 +244,7 @@ prepare_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __rest
     for (int i = 0; i < count; ++i)
       load_rows<128>(InTile<8, NI>{smem_addr(A) + i * L::kV}, &M.v, &bars[1], v, P.ldv, w.h * P.Dv + 64 * (first + i),
                      w.t, w.b, P.L, w.rows, tid);
-    if (first == 0) {  // -W, while V is on its way
+    if (first == 0 && !P.single) {  // -W, while V is on its way
       char* wt = P.W + w.nc * Tile<DK / 8, NM>::kBytes;
 #pragma unroll
       for (int half = 0; half < DK / 64; ++half) {
@@ -336,6 +344,11 @@ struct ChainSmem {
 // once: MAPS. Its Dv columns N start from zero; its phi is what becomes of the identity's Dk columns without
 // U0. combine_kernel chains the maps, and this kernel then runs every segment from the state before it:
 // three times the products of the single pass, over nseg times the warps.
+//
+// Bound by the two dependent products of a chunk, of which a scheduler has one warp's (narrow) or two (wide)
+// at a time: 16384 chunks in 32 heads of 128 x 128, bfloat16, 452 us (1.6 GB, 231 us); one row of 512 chunks
+// and 8 heads with carried states (two planes), 9 segments: maps 203 us, at 66 % of the tensor pipe's
+// cycles, then 153 us. The first form, a block a head whose warps shared the state, took 1427 us on the former.
 template <typename TI, int DK, int NI, int NM, int WARPS, bool MAPS>
 __global__ void __launch_bounds__(32 * (WARPS + kLoadWarps<NI>), WARPS == 4 && NM < 3 ? 2 : 1)
 chain_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restrict__ k, const float* __restrict__ s0,
@@ -513,7 +526,8 @@ struct CombineSmem {
 };
 
 // Chains the segments' maps of a head, 64 columns a block: S -> phi S + N (back: dS -> phi^T dS + N, last
-// segment first), and leaves the state before (after) every segment in N's place.
+// segment first), and leaves the state before (after) every segment in N's place. Serial: 3.7 us a segment
+// (9 segments of 8 heads, 128 x 128: 33 us), bound by the latency of one product and the next phi's load.
 template <int DK, int NM, bool BACK>
 __global__ void __launch_bounds__(128)
 combine_kernel(const Problem P, float* __restrict__ carry, const float* __restrict__ start) {
@@ -596,7 +610,9 @@ struct OutputSmem {
   static constexpr int kBytes = 2 * kQ + kSlots * kU + kS + kGates * 4 + 24;
 };
 
-// O = scale (diag(gamma) Q S + P U) of one chunk of one head; zero on the row's padding.
+// O = scale (diag(gamma) Q S + P U) of one chunk of one head; zero on the row's padding. The next 64 columns'
+// S and U load while these are multiplied. Bound by the latency of its loads, with three blocks an SM:
+// 16384 chunks of 128 x 128, bfloat16, 306 us (1.6 GB, 236 us: 0.77 of the copy rate).
 template <typename TI, int DK, int NI, int NM>
 __global__ void __launch_bounds__(128)
 output_kernel(const Problem P, const __grid_constant__ Maps M, const TI* __restrict__ q, const TI* __restrict__ k,

@@ -11,7 +11,8 @@
 // Tiles of the workspace (8 x 8 blocks) are operands of either major-ness without a swizzle, the callers'
 // tensors and what is written here lie under the 128-byte swizzle.
 //
-// Bound by memory at Dk = Dv = 128: 216 KB a chunk, 0.52 ms of 16384 chunks. A persistent block an SM
+// Bound by memory at Dk = Dv = 128: 216 KB a chunk, 0.52 ms of 16384 chunks, which take 0.69 ms (0.76 of
+// the copy rate). A persistent block an SM (two at Dk = Dv = 64: 4096 chunks in 108 us)
 // works on one chunk at a time; each of its buffers is refilled for the next chunk as soon as its last
 // reader is done, so the loads run beside the arithmetic on the scores and gradients (8 warps). One
 // thread issues loads, products and the gradients' stores, whose tiles are staged in buffers that are
@@ -140,7 +141,7 @@ struct TcSmem {
   static constexpr int kT8 = 8192;  // a 64 x 64 tile
   static constexpr int kS = DK * 128;
   // offsets: [Q K] per 64 columns; per part of Dv [dO dR U S dS]; P' M; dU, V per part; T
-  static constexpr int kQK = 0, kPart0 = DK / 64 * 2 * kT8, kPart = 3 * kT8 + 2 * kS;
+  static constexpr int kPart0 = DK / 64 * 2 * kT8, kPart = 3 * kT8 + 2 * kS;
   static constexpr int kP = kPart0 + DVB * kPart, kDU = kP + 2 * kT8, kV = kDU + DVB * kT8, kT = kV + DVB * kT8;
   static constexpr int kMore = kT + kT8;  // the product with T^T reads 1 KB past T
   static constexpr int kGates0 = kMore + (DK == 128 && DVB == 1 ? kT8 : 1024);

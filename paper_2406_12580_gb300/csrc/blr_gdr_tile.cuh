@@ -295,6 +295,11 @@ __device__ __forceinline__ void load_rows(const Tile<C8, 1, 1>& t, const CUtenso
           "l"(map), "r"(col + 64 * j), "r"((int)step), "r"(b), "r"(smem_addr(bar)) : "memory");
   }
 }
+// 64 rows x 64 columns of a caller's bfloat16 tensor on their way into L2.
+__device__ __forceinline__ void prefetch_rows(const CUtensorMap* map, int col, int64_t step, int b) {
+  asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global.tile [%0, {%1, %2, %3}];" ::"l"(map), "r"(col),
+               "r"((int)step), "r"(b) : "memory");
+}
 template <int THREADS, int C8>
 __device__ __forceinline__ void load_rows(const Tile<C8, 3>& t, const CUtensorMap*, uint64_t*, const float* base,
                                           int64_t ld, int col, int64_t step, int b, int64_t L, int rows, int tid) {
