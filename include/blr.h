@@ -470,6 +470,7 @@ BLR_API blr_status blr_gdr_steps(const blr_gdr_desc* desc, blr_dtype state, cons
  *   w          io == BLR_BF16: float32 master weights (updated; p becomes their
  *              rounding), in all records or in none (NULL: w is p itself)
  *   m_scale, v_scale  ceil(n / 256) scales (updated); bits == 8 only
+ * eps          > 0; below float32's smallest normal value it acts as that
  * step         1 for the first step
  * grad_scale   float32 on the device, or NULL (1): a clipping or unscaling factor
  * Pointers are aligned to their element. Tensors whose pointers are 32-byte
