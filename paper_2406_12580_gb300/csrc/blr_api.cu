@@ -164,10 +164,11 @@ blr_status make_tensor_map(CUtensorMap* map, const void* base, int io, int64_t c
   const cuuint64_t strides[2] = {(cuuint64_t)row_elems * es, (cuuint64_t)row_elems * es * (cuuint64_t)L};
   const cuuint32_t box[3] = {box_cols, (cuuint32_t)rows, 1u};
   const cuuint32_t estr[3] = {1u, 1u, 1u};
-  const CUresult r = enc(map, io == BLR_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
-                         3, const_cast<void*>(base), dims, strides, box, estr,
-                         CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
-                         CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  const CUresult r = blr::in_context([&] {
+    return enc(map, io == BLR_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3,
+               const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  });
   if (r != CUDA_SUCCESS) return fail(BLR_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
   return BLR_OK;
 }

@@ -12,6 +12,8 @@ if not torch.cuda.is_available():  # collected on CPU machines, but never run th
 from delta_common import make  # noqa: E402
 from paper_2406_12580_gb300 import (BLR_BF16, BLR_GDR_TRAIN, GDRDesc, blr_gdr_bwd, blr_gdr_fwd,  # noqa: E402
                                     blr_gdr_workspace_bytes)
+from paper_2406_12580_gb300 import inputs as I  # noqa: E402
+from paper_2406_12580_gb300.device import ScanBuffers  # noqa: E402
 
 
 def in_new_thread(call):
@@ -51,3 +53,17 @@ def test_gated_delta_rule():
     in_new_thread(lambda: bwd(outs[1]))
     for a, b in zip(*outs):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+def test_scan(io):
+    """One warp a chain: a fixed order of sums, so the outputs are the same bits."""
+    inp = I.make_scan_inputs(I.ScanConfig("thread", B=256, L=50, D=64, io=io, seed=32))
+    a, b = ScanBuffers.from_inputs(inp), ScanBuffers.from_inputs(inp)
+    stream = torch.cuda.current_stream()
+    a.fwd(stream)
+    a.bwd(stream)
+    in_new_thread(lambda: b.fwd(stream))
+    in_new_thread(lambda: b.bwd(stream))
+    for n in ("h", "h_last", "dx", "dgl", "dh0"):
+        assert torch.equal(getattr(a, n), getattr(b, n)), n
